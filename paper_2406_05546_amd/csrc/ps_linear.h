@@ -1,0 +1,526 @@
+// Dense layers on the gfx950 matrix cores (include/ps_dense.h): forward, input gradient and weight gradient, in one group
+// of rows or in many.
+//
+//   out[r][c] = sum_k R(r, k) C(c, k)
+//
+// R gives the rows of the result, C its (contiguous) columns.  Either operand lies k-contiguous ("KC": x and w of the
+// forward pass, dz of the input gradient) or row-contiguous ("RC": w of the input gradient, dz and x of the weight
+// gradient).  A block owns a BR x BC tile of the result, and its operands come in stages of 128 bytes of k (64 values of a
+// 16-bit type, 32 of fp32) through LDS; wavefronts are arranged WR x WC and multiply 16 x 16 tiles
+// (v_mfma_f32_16x16x32_bf16 / _f16, v_mfma_f32_16x16x4_f32) with C as the instruction's first operand, so that a lane
+// gets consecutive columns of one row of the result.
+#pragma once
+#include "ps_dense.h"
+
+#include <algorithm>
+
+namespace ps {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int LINEAR_XCDS = 8;
+
+// ---------------------------------------------------------------------------------------------------------------
+// Groups
+
+// Where the rows of the groups are, and which matrix each uses.  Offsets come from device memory and are whatever they
+// are: every one is taken into 0 .. rows, a group that ends before it begins is empty.
+struct Groups {
+    const int32_t* offsets;  // [n + 1], or null: one group of all rows
+    const int32_t* index;    // [n], or null: group g uses matrix g
+    int32_t n, n_weights, rows;
+};
+
+struct GroupRows {
+    int g, begin, end;
+};
+
+#if defined(__HIPCC__)
+
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+__device__ __forceinline__ GroupRows group_rows(const Groups& gs, int g)
+{
+    if (!gs.offsets) return {g, 0, gs.rows};
+    const int begin = min(max(gs.offsets[g], 0), gs.rows), end = min(max(gs.offsets[g + 1], begin), gs.rows);
+    return {g, begin, end};
+}
+
+__device__ __forceinline__ int group_matrix(const Groups& gs, int g)
+{
+    const int i = gs.index ? gs.index[g] : g;
+    return min(max(i, 0), gs.n_weights - 1);
+}
+
+// The group and the first row of the `tile`-th piece of `size` rows when the groups are cut up one after the other; false
+// if there are not so many.  Every wavefront looks for itself, 64 groups at a time.
+__device__ __forceinline__ bool find_rows(const Groups& gs, int tile, int size, GroupRows& found, int& first)
+{
+    if (!gs.offsets) {
+        first = tile * size;
+        found = {0, 0, gs.rows};
+        return first < gs.rows;
+    }
+    const int lane = threadIdx.x & 63;
+    int before = 0;  // tiles of the groups passed; stays at most `tile`
+    for (int g0 = 0; g0 < gs.n; g0 += 64) {
+        GroupRows r = {g0 + lane, 0, 0};
+        if (r.g < gs.n) r = group_rows(gs, r.g);
+        const int own = (r.end - r.begin + size - 1) / size;
+        // Rows are at most 2^28 and tiles at least 16 rows, so that 64 groups (which may overlap, if the offsets are no
+        // offsets) stay below 2^30 tiles.
+        int upto = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += other;
+        }
+        const unsigned long long beyond = __ballot(upto > tile - before);
+        if (beyond) {
+            const int l = __builtin_ctzll(beyond);
+            found.g = scalar(g0 + l);
+            found.begin = __builtin_amdgcn_readlane(r.begin, l);
+            found.end = __builtin_amdgcn_readlane(r.end, l);
+            first = found.begin + (tile - before - __builtin_amdgcn_readlane(upto - own, l)) * size;
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Activations
+
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == PS_ACT_RELU) return z <= 0.f ? 0.f : z;
+    if (act == PS_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);  // erfc: 1 + erf has no bits left where z is very negative
+    if (act == PS_ACT_SILU) return z / (1.f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ float activation_slope(float z, int act)
+{
+    if (act == PS_ACT_RELU) return z <= 0.f ? 0.f : 1.f;
+    if (act == PS_ACT_GELU) return 0.5f * erfcf(-0.70710678f * z) + z * 0.39894228f * __expf(-0.5f * z * z);
+    if (act == PS_ACT_SILU) {
+        const float s = 1.f / (1.f + __expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Matrix instructions: what 16 bytes of k of a row times 16 bytes of k of a column give.
+
+template <class T>
+struct Mma;
+template <>
+struct Mma<bf16_t> {
+    static constexpr int E = 8;  // values in 16 bytes
+    static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
+    {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, c), __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<f16_t> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
+    {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, c), __builtin_bit_cast(f16x8, r), acc, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
+    {
+        // one k of each 16 bytes at a time
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(c[i]), __uint_as_float(r[i]), acc, 0, 0, 0);
+    }
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// One operand's tile in LDS: ROWS rows (or columns) of the result and 128 bytes of k, ROWS * 128 bytes.
+//
+// KC: row r at r * 128, its 16-byte pieces exchanged by a function of the row, so that 16 lanes that read the same piece
+// of 16 rows, and 8 lanes that read it of 8, use all banks once.  RC: k at k * ROWS * sizeof(T), 32-byte groups (16 columns
+// of a 16-bit type; 64 bytes of fp32) exchanged by a function of k for the same reason; the transposing LDS read
+// (ds_read_b64_tr_b16: 16 lanes read 16 columns of four k, and each gets the four k of its column) turns 16-bit types.
+// COLS: the operand that is the result's columns.  If it is KC, row 4q + e of the MFMA tiles 2t and 2t + 1 is column
+// 32 t + 8 q + e and + 4, so that a lane ends up with eight consecutive columns.
+//
+// NT threads bring it, 16 bytes at a time.  DIRECT: memory to LDS without registers; rows start at multiples of 16 bytes
+// and have multiples of 16 bytes, buffer bounds give zeros past the last row.  Else through registers, at any alignment.
+template <class T, bool KC, bool COLS, int ROWS, int NT, bool DIRECT>
+struct Operand {
+    static constexpr int SIZE = sizeof(T), E = 16 / SIZE, BK = 128 / SIZE;
+    static constexpr int BYTES = ROWS * 128, LOADS = BYTES / (NT * 16);
+    static_assert(LOADS * NT * 16 == BYTES, "every thread brings the same number of pieces");
+    static constexpr int PIECES = ROWS / E;  // RC: pieces of one k
+    static constexpr bool PERMUTED = KC && COLS;
+    static constexpr int SUBS = 2;           // reads of 16 bytes of k for each of the four lane groups
+
+    const char* base;  // of this tile's first row (KC) or column (RC) and the first k of the next stage to be brought
+    int64_t step;      // bytes from stage to stage
+    int32_t pitch;     // bytes from row to row (KC) or from k to k (RC)
+    int32_t left;      // k still to be brought
+    int32_t rows;      // KC: valid rows of the tile; RC: valid columns
+    uintx4 reg[DIRECT ? 1 : LOADS];
+
+    static __device__ __forceinline__ int kc_swap(int row)
+    {
+        return PERMUTED ? (row >> 1 & 1) | (row >> 3 & 1) << 1 | ((row ^ row >> 4) & 1) << 2 : (row >> 1 & 3) | ((row ^ row >> 3) & 1) << 2;
+    }
+    static __device__ __forceinline__ int rc_swap(int k)  // in 16-byte pieces
+    {
+        if (SIZE == 4) return (k >> 2 & 3) << 2;
+        return ROWS >= 128 ? ((k & 3) | (k >> 3 & 1) << 2) << 1 : ((k >> 1 & 1) | (k >> 3 & 1) << 1) << 1;
+    }
+    // Piece i of thread t: its row (KC) or k (RC), and its 16-byte piece within
+    static __device__ __forceinline__ void place(int i, int t, int& line, int& piece)
+    {
+        const int f = i * NT + t;
+        if (KC) {
+            line = f >> 3;
+            piece = (f & 7) ^ kc_swap(line);
+        } else {
+            line = f / PIECES;
+            piece = (f & (PIECES - 1)) ^ rc_swap(line);
+        }
+    }
+
+    // first: element of the tile's first row or column and the first k
+    __device__ __forceinline__ void init(const T* first, int64_t stride, int valid, int depth)
+    {
+        base = reinterpret_cast<const char*>(first);
+        pitch = (int32_t)(stride * SIZE);
+        step = KC ? 128 : (int64_t)pitch * BK;
+        left = depth;
+        rows = min(valid, ROWS);
+    }
+
+    __device__ __forceinline__ void bring(char* tile, int t)
+    {
+        if constexpr (DIRECT) {
+            // Last byte that may be read: KC, of the last row (what is past its end in the last stage is left out below); RC,
+            // of the last k.
+            const int lines = KC ? rows : min(left, BK);
+            const uint32_t bytes = lines > 0 ? (uint32_t)(lines - 1) * (uint32_t)pitch + (uint32_t)(KC ? min(left, BK) : rows) * SIZE : 0u;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                int line, piece;
+                place(i, t, line, piece);
+                uint32_t offset = (uint32_t)line * (uint32_t)pitch + piece * 16;
+                if (KC && piece * E >= left) offset = 0xfffffff0u;  // past the end of the row: beyond `bytes`, and so zero
+                char* to = tile + (i * NT + (t & ~63)) * 16;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, (int)offset, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                int line, piece;
+                place(i, t, line, piece);
+                const int n = KC ? (line < rows ? left - piece * E : 0) : (line < left ? rows - piece * E : 0);
+                const char* p = base + (int64_t)line * pitch + piece * 16;
+                reg[i] = uintx4{0, 0, 0, 0};
+                if (n >= E) {
+                    __builtin_memcpy(&reg[i], p, 16);
+                } else if (n > 0) {
+                    const T* q = reinterpret_cast<const T*>(p);
+#pragma unroll
+                    for (int e = 0; e < E - 1; ++e) {
+                        if (e >= n) continue;
+                        if constexpr (SIZE == 4)
+                            reg[i][e] = __float_as_uint(q[e]);
+                        else
+                            reg[i][e / 2] |= (uint32_t)q[e].bits << (16 * (e & 1));
+                    }
+                }
+            }
+        }
+        base += step;
+        left -= BK;
+    }
+    __device__ __forceinline__ void put(char* tile, int t) const
+    {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) *reinterpret_cast<uintx4*>(tile + (i * NT + t) * 16) = reg[i];
+        }
+    }
+
+    // 16 bytes of k of the lane's row in MFMA tile `tile16` (rows 16 tile16 ..) of the rows from `first` (a multiple of 16,
+    // or of 32 if permuted) on: k = (sub * 4 + lane / 16) * E ..
+    static __device__ __forceinline__ uintx4 fetch(const char* tile, int first, int tile16, int sub, int lane)
+    {
+        const int l = lane & 15, q = lane >> 4;
+        if constexpr (KC) {
+            const int row = PERMUTED ? first + 32 * (tile16 >> 1) + 8 * (l >> 2) + 4 * (tile16 & 1) + (l & 3) : first + 16 * tile16 + l;
+            return *reinterpret_cast<const uintx4*>(tile + row * 128 + (((sub * 4 + q) ^ kc_swap(row)) << 4));
+        } else if constexpr (SIZE == 2) {
+            typedef short shortx4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) shortx4* LdsPtr;
+            const int k = 32 * sub + 8 * q + (l >> 2);
+            const int piece = (2 * (first / 16 + tile16)) ^ rc_swap(k);
+            const char* p = tile + k * (ROWS * 2) + piece * 16 + (l & 3) * 8;
+            const uintx2 a = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(shortx4*)p));
+            const uintx2 b = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(shortx4*)(p + 4 * ROWS * 2)));
+            return uintx4{a[0], a[1], b[0], b[1]};
+        } else {
+            uintx4 v;
+            const int col = first + 16 * tile16 + l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int k = 16 * sub + 4 * q + e;
+                v[e] = *reinterpret_cast<const uint32_t*>(tile + k * (ROWS * 4) + (((col >> 2) ^ rc_swap(k)) << 4) + (col & 3) * 4);
+            }
+            return v;
+        }
+    }
+};
+
+#endif  // __HIPCC__
+
+// ---------------------------------------------------------------------------------------------------------------
+// What becomes of the sums
+
+struct Epilogue {
+    // forward: y = act(sum + bias) + residual, pre = sum + bias; gradients: out = sum
+    void* out;
+    const void* bias;
+    const void* residual;
+    void* pre;
+    int64_t out_row, residual_row, pre_row, bias_matrix, out_matrix;  // elements
+    int32_t act;
+    float* partial;  // if not null the sums go there instead, one result for each part of the contraction: [part][rows][cols]
+};
+
+#if defined(__HIPCC__)
+
+// N consecutive columns of one row, of which `valid` exist.
+template <class T, int N>
+__device__ __forceinline__ void finish(const Epilogue& e, int matrix, int group, int64_t row, int col, int valid, float (&v)[N])
+{
+    if (valid <= 0) return;
+    const bool whole = valid >= N;
+    auto load = [&](const void* base, int64_t at, float (&x)[N]) {
+        const T* p = static_cast<const T*>(base) + at;
+        if (whole)
+            load_n(p, x);
+        else
+            load_some(p, valid, x);
+    };
+    auto store = [&](void* base, int64_t at, const float (&x)[N]) {
+        T* p = static_cast<T*>(base) + at;
+        if (whole)
+            store_n(p, x);
+        else
+            store_some(p, valid, x);
+    };
+    float x[N];
+    if (e.bias) {
+        load(e.bias, matrix * e.bias_matrix + col, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += x[i];
+    }
+    if (e.pre) store(e.pre, row * e.pre_row + col, v);
+    if (e.act != PS_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = activate(v[i], e.act);
+    }
+    if (e.residual) {
+        load(e.residual, row * e.residual_row + col, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += x[i];
+    }
+    store(e.out, group * e.out_matrix + row * e.out_row + col, v);
+}
+
+#endif
+
+// ---------------------------------------------------------------------------------------------------------------
+// The kernel
+
+struct Product {
+    const void *r, *c;                       // operands
+    int64_t r_row, c_row, c_matrix;          // strides in elements; c_matrix between the matrices of C
+    int32_t rows, cols, depth;               // of the result (RAGGED_K: per group) and of the contraction (RAGGED_K: of all groups)
+    int32_t tiles_r, tiles_c;                // tiles along the rows (RAGGED_K: of all groups together) and columns
+    int32_t parts, part_stages;              // the contraction in parts of so many stages each
+    Groups groups;
+    Epilogue epi;
+};
+
+// Which operand is ragged: rows of the result in groups (forward, input gradient), or the contraction (weight gradient).
+enum { RAGGED_R = 0, RAGGED_K = 1 };
+
+#if defined(__HIPCC__)
+
+// Blocks are handed to the eight XCDs in turn; each XCD walks a contiguous range of tiles, in patches of `PATCH` tiles of
+// rows, so that the tiles that run at the same time share their operands in the XCD's L2.
+constexpr int PATCH = 8;
+__device__ __forceinline__ bool tile_of_block(const Product& p, int block, int& tr, int& tc, int& part)
+{
+    const int per_part = p.tiles_r * p.tiles_c, total = per_part * p.parts;
+    const int per_xcd = (total + LINEAR_XCDS - 1) / LINEAR_XCDS;
+    int v = block % LINEAR_XCDS * per_xcd + block / LINEAR_XCDS;
+    if (v >= total) return false;
+    part = v / per_part;
+    v -= part * per_part;
+    const int band = v / (PATCH * p.tiles_c), first = band * PATCH, high = min(PATCH, p.tiles_r - first);
+    v -= band * PATCH * p.tiles_c;
+    tr = first + v % high;
+    tc = v / high;
+    return true;
+}
+
+template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DIRECT, int RAGGED>
+__global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_kernel(Product p)
+{
+    constexpr int NT = 64 * WR * WC, TR = BR / WR / 16, TC = BC / WC / 16;
+    using OpR = Operand<T, R_KC, false, BR, NT, DIRECT>;
+    using OpC = Operand<T, C_KC, true, BC, NT, DIRECT>;
+    constexpr int BK = OpR::BK, SUBS = OpR::SUBS;
+    static_assert(!OpC::PERMUTED || TC % 2 == 0, "permuted columns come in pairs of tiles");
+    __shared__ __attribute__((aligned(256))) char lds[2][OpR::BYTES + OpC::BYTES];
+
+    int tr, tc, part;
+    if (!tile_of_block(p, blockIdx.x, tr, tc, part)) return;
+    GroupRows rows;
+    int r0, depth = p.depth, r_valid, k_first = 0;
+    if (RAGGED == RAGGED_R) {
+        if (!find_rows(p.groups, tr, BR, rows, r0)) return;
+        r_valid = rows.end - r0;
+    } else {
+        const int per_group = (p.rows + BR - 1) / BR;
+        rows = group_rows(p.groups, tr / per_group);
+        r0 = tr % per_group * BR;
+        r_valid = p.rows - r0;
+        k_first = rows.begin;
+        depth = rows.end - rows.begin;
+    }
+    const int matrix = RAGGED == RAGGED_R ? group_matrix(p.groups, rows.g) : 0;
+    const int c0 = tc * BC, c_valid = p.cols - c0;
+    if (p.parts > 1) {
+        const int from = min(part * p.part_stages * BK, depth);
+        k_first += from;
+        depth = min(depth - from, p.part_stages * BK);
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
+    const int wr = wave % WR, wc = wave / WR;
+
+    OpR opr;
+    OpC opc;
+    opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)r0 * p.r_row + k_first : (int64_t)k_first * p.r_row + r0), p.r_row, r_valid, depth);
+    opc.init(static_cast<const T*>(p.c) + matrix * p.c_matrix + (C_KC ? (int64_t)c0 * p.c_row + k_first : (int64_t)k_first * p.c_row + c0), p.c_row, c_valid, depth);
+
+    floatx4 acc[TR][TC];
+#pragma unroll
+    for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < TC; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    const int stages = (depth + BK - 1) / BK;
+    if (stages > 0) {
+        opr.bring(lds[0], tid);
+        opc.bring(lds[0] + OpR::BYTES, tid);
+        opr.put(lds[0], tid);
+        opc.put(lds[0] + OpR::BYTES, tid);
+    }
+    __syncthreads();
+    for (int s = 0; s < stages; ++s) {
+        const char* now = lds[s & 1];
+        char* next = lds[~s & 1];
+        if (s + 1 < stages) {
+            opr.bring(next, tid);
+            opc.bring(next + OpR::BYTES, tid);
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            uintx4 fr[TR], fc[TC];
+#pragma unroll
+            for (int j = 0; j < TC; ++j) fc[j] = OpC::fetch(now + OpR::BYTES, wc * TC * 16, j, sub, lane);
+#pragma unroll
+            for (int i = 0; i < TR; ++i) fr[i] = OpR::fetch(now, wr * TR * 16, i, sub, lane);
+#pragma unroll
+            for (int i = 0; i < TR; ++i)
+#pragma unroll
+                for (int j = 0; j < TC; ++j) Mma<T>::add(fc[j], fr[i], acc[i][j]);
+        }
+        if (s + 1 < stages) {
+            opr.put(next, tid);
+            opc.put(next + OpR::BYTES, tid);
+        }
+        __syncthreads();
+    }
+
+    // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.
+    const int l = lane & 15, q = lane >> 4;
+    constexpr int N = OpC::PERMUTED ? 8 : 4;
+#pragma unroll
+    for (int i = 0; i < TR; ++i) {
+        const int r = (wr * TR + i) * 16 + l;
+#pragma unroll
+        for (int j = 0; j < TC; j += N / 4) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = acc[i][j + e / 4][e & 3];
+            const int c = wc * TC * 16 + (OpC::PERMUTED ? 16 * j + 8 * q : 16 * j + 4 * q);
+            const int valid = r < r_valid ? c_valid - c : 0;
+            if (p.epi.partial) {
+                float* to = p.epi.partial + ((int64_t)part * p.rows + (r0 + r)) * p.cols + c0 + c;
+                if (valid >= N)
+                    store_n(to, v);
+                else if (valid > 0)
+                    store_some(to, valid, v);
+            } else {
+                finish<T>(p.epi, matrix, RAGGED == RAGGED_K ? rows.g : 0, r0 + r, c0 + c, valid, v);
+            }
+        }
+    }
+}
+
+#endif
+
+// Launchers, one file each (kinds of operands): forward, input gradient, weight gradient.
+void launch_linear_forward(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
+void launch_linear_dx(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
+void launch_linear_dw(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
+
+// Sizes of square tiles, by number.
+constexpr int LINEAR_TILE[3] = {64, 128, 256};
+
+#if defined(__HIPCC__)
+template <class T, bool R_KC, bool C_KC, bool DIRECT, int RAGGED>
+void start_linear(const Product& p, int tile, hipStream_t s)
+{
+    const int total = p.tiles_r * p.tiles_c * p.parts;
+    const dim3 grid((total + LINEAR_XCDS - 1) / LINEAR_XCDS * LINEAR_XCDS);
+    if (tile == 0)
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 64, 64, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
+    else if (tile == 1 || !DIRECT || sizeof(T) == 4)
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 128, 128, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
+    else if constexpr (DIRECT && sizeof(T) == 2)
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), grid, dim3(512), 0, s, p);
+}
+template <bool R_KC, bool C_KC, int RAGGED>
+void start_linear_typed(const Product& p, int dtype, bool direct, int tile, hipStream_t s)
+{
+    if (dtype == PS_F32)
+        direct ? start_linear<float, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<float, R_KC, C_KC, false, RAGGED>(p, tile, s);
+    else if (dtype == PS_BF16)
+        direct ? start_linear<bf16_t, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<bf16_t, R_KC, C_KC, false, RAGGED>(p, tile, s);
+    else
+        direct ? start_linear<f16_t, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<f16_t, R_KC, C_KC, false, RAGGED>(p, tile, s);
+}
+#endif
+
+}  // namespace ps

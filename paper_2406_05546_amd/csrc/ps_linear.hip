@@ -1,0 +1,418 @@
+// Entry points of the dense layers (include/ps_dense.h): checks, choice of tiles, workspaces, and the kernels around the
+// products of ps_linear.h.
+#include "ps_linear.h"
+
+#include <cstdarg>
+#include <cstdio>
+
+namespace ps {
+
+namespace {
+thread_local char dense_error[256] = "";
+}
+
+ps_status dense_fail(ps_status st, const char* format, ...)
+{
+    va_list args;
+    va_start(args, format);
+    std::vsnprintf(dense_error, sizeof(dense_error), format, args);
+    va_end(args);
+    return st;
+}
+
+namespace {
+
+constexpr int COMPUTE_UNITS = 256;
+
+// ---- dz = dy act'(z), and the sums over rows that are the bias's gradient ------------------------------------------
+
+struct SlopeArgs {
+    const void *dy, *pre;  // pre null: no activation
+    void* dz;              // null: only the sums
+    int64_t dy_row, pre_row, dz_row;
+    int32_t act, cols, parts;
+    float* partial;  // [group][part][cols], or null: no sums
+    Groups groups;
+};
+
+// A block takes 512 columns (a lane eight consecutive ones) of one part of a group's rows, its four wavefronts every
+// fourth row each; their sums meet in LDS in order.
+constexpr int SLOPE_COLS = 512;
+
+template <class T>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+{
+    __shared__ float meet[3][64][9];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int g = blockIdx.y / a.parts, part = blockIdx.y % a.parts;
+    const GroupRows rows = group_rows(a.groups, g);
+    const int each = (rows.end - rows.begin + a.parts - 1) / a.parts;
+    const int begin = min(rows.begin + part * each, rows.end), end = min(begin + each, rows.end);
+    const int col = blockIdx.x * SLOPE_COLS + lane * 8, n = min(8, a.cols - col);
+    float sum[8] = {};
+    if (n > 0) {
+        for (int64_t r = begin + wave; r < end; r += 4) {
+            float d[8], z[8];
+            const T* dy = static_cast<const T*>(a.dy) + r * a.dy_row + col;
+            if (n == 8)
+                load_n(dy, d);
+            else
+                load_some(dy, n, d);
+            if (a.pre) {
+                const T* pre = static_cast<const T*>(a.pre) + r * a.pre_row + col;
+                if (n == 8)
+                    load_n(pre, z);
+                else
+                    load_some(pre, n, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= activation_slope(z[i], a.act);
+            }
+            if (a.dz) {
+                T* dz = static_cast<T*>(a.dz) + r * a.dz_row + col;
+                if (n == 8)
+                    store_n(dz, d);
+                else
+                    store_some(dz, n, d);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += d[i];
+        }
+    }
+    if (!a.partial) return;
+    if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) meet[wave - 1][lane][i] = sum[i];
+    }
+    __syncthreads();
+    if (wave == 0 && n > 0) {
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += meet[w][lane][i];
+        float* to = a.partial + ((int64_t)g * a.parts + part) * a.cols + col;
+        if (n == 8)
+            store_n(to, sum);
+        else
+            store_some(to, n, sum);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, T* __restrict__ db, int64_t db_matrix, int cols, int parts)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+    if (c >= cols) return;
+    float s = 0.f;
+    for (int k = 0; k < parts; ++k) s += partial[((int64_t)g * parts + k) * cols + c];
+    db[g * db_matrix + c] = from_float<T>(s);
+}
+
+// Adds up the parts of a contraction, in order, and finishes the sums.
+template <class T>
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int parts, int rows, int cols, Epilogue epi)
+{
+    const int per_row = (cols + 7) / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+    if (row >= rows) return;
+    const int col = (int)(i % per_row) * 8, n = min(8, cols - col);
+    float v[8], x[8];
+    for (int k = 0; k < parts; ++k) {
+        const float* p = partial + ((int64_t)k * rows + row) * cols + col;
+        if (n == 8)
+            load_n(p, x);
+        else
+            load_some(p, n, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k ? v[e] + x[e] : x[e];
+    }
+    finish<T>(epi, 0, 0, row, col, n, v);
+}
+
+// ---- plans ---------------------------------------------------------------------------------------------------------
+
+enum { FORWARD, DX, DW };
+
+struct Plan {
+    int tile, parts, part_stages;
+    int64_t tiles_r, tiles_c;
+    uint64_t partial_bytes;
+};
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Plan plan_product(const ps_linear& l, int kind, bool direct)
+{
+    const int64_t rows = kind == DW ? l.out_features : l.rows, cols = kind == FORWARD ? l.out_features : l.in_features;
+    const int64_t depth = kind == FORWARD ? l.in_features : kind == DX ? l.out_features : l.rows;
+    const bool one = !l.offsets_dev;
+    Plan best{};
+    for (int tile = l.dtype == PS_F32 || !direct ? 1 : 2; tile >= 0; --tile) {
+        const int size = LINEAR_TILE[tile];
+        Plan p{};
+        p.tile = tile;
+        p.parts = 1;
+        // groups that are cut up separately have at most one tile more each than all rows together
+        p.tiles_r = kind == DW ? up(rows, size) * l.n_groups : up(rows, size) + (one ? 0 : l.n_groups);
+        p.tiles_c = up(cols, size);
+        best = p;
+        if (p.tiles_r * p.tiles_c >= COMPUTE_UNITS) break;
+    }
+    const int stages = (int)up(depth, 128 / dtype_size(l.dtype));
+    best.part_stages = stages;
+    const int64_t tiles = best.tiles_r * best.tiles_c;
+    if (one && tiles > 0 && tiles < COMPUTE_UNITS && stages >= 8) {
+        const int parts = (int)std::min<int64_t>(std::min<int64_t>(2 * COMPUTE_UNITS / tiles, stages / 4), 32);
+        if (parts > 1) {
+            best.part_stages = (int)up(stages, parts);
+            best.parts = (int)up(stages, best.part_stages);
+            best.partial_bytes = (uint64_t)best.parts * rows * cols * 4;
+        }
+    }
+    return best;
+}
+
+int slope_parts(const ps_linear& l)
+{
+    const int64_t blocks = up(l.out_features, SLOPE_COLS) * l.n_groups;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(up(8 * COMPUTE_UNITS, blocks), up(up(l.rows, l.n_groups), 16)), 65535 / std::min<int64_t>(l.n_groups, 65535)));
+}
+
+struct BackwardSpace {
+    uint64_t dz, bias, partial, total;
+    int64_t dz_row;
+    int parts;
+};
+
+uint64_t up256(uint64_t b) { return (b + 255) / 256 * 256; }
+
+bool direct_possible(const ps_linear& l, int kind)
+{
+    const int64_t e = 16 / dtype_size(l.dtype);
+    return l.in_features % e == 0 && (kind == FORWARD || l.out_features % e == 0);
+}
+
+BackwardSpace backward_space(const ps_linear& l)
+{
+    BackwardSpace b{};
+    const int size = dtype_size(l.dtype);
+    b.dz_row = up(l.out_features, 16 / size) * (16 / size);
+    b.parts = slope_parts(l);
+    const uint64_t dz = l.activation != PS_ACT_NONE ? up256((uint64_t)l.rows * b.dz_row * size) : 0;
+    const uint64_t bias = up256((uint64_t)l.n_groups * b.parts * l.out_features * 4);
+    uint64_t partial = 0;
+    for (int kind : {DX, DW})
+        for (bool direct : {true, false}) partial = std::max(partial, plan_product(l, kind, direct).partial_bytes);
+    b.dz = 0;
+    b.bias = dz;
+    b.partial = dz + bias;
+    b.total = b.partial + up256(partial);
+    return b;
+}
+
+uint64_t forward_space(const ps_linear& l)
+{
+    return up256(std::max(plan_product(l, FORWARD, true).partial_bytes, plan_product(l, FORWARD, false).partial_bytes));
+}
+
+// ---- checks --------------------------------------------------------------------------------------------------------
+
+ps_status check_layer(const char* call, const ps_linear* l)
+{
+    if (!l) return dense_fail(PS_EINVAL, "%s: no layer", call);
+    if (l->dtype != PS_F32 && l->dtype != PS_BF16 && l->dtype != PS_F16) return dense_fail(PS_EINVAL, "%s: unknown type", call);
+    if (l->activation < PS_ACT_NONE || l->activation > PS_ACT_SILU) return dense_fail(PS_EINVAL, "%s: unknown activation", call);
+    if (l->rows < 0 || l->rows > PS_DENSE_MAX_ROWS) return dense_fail(PS_EINVAL, "%s: rows outside 0 .. %d", call, PS_DENSE_MAX_ROWS);
+    if (l->in_features < 1 || l->in_features > PS_DENSE_MAX_STRIDE || l->out_features < 1 || l->out_features > PS_DENSE_MAX_STRIDE)
+        return dense_fail(PS_EINVAL, "%s: features outside 1 .. %d", call, PS_DENSE_MAX_STRIDE);
+    if (l->n_groups < 1 || l->n_groups > PS_DENSE_MAX_GROUPS) return dense_fail(PS_EINVAL, "%s: groups outside 1 .. %d", call, PS_DENSE_MAX_GROUPS);
+    if (!l->offsets_dev && l->n_groups != 1) return dense_fail(PS_EINVAL, "%s: several groups need offsets", call);
+    if (l->n_weights < 1 || (!l->weight_of_group_dev && l->n_weights < l->n_groups))
+        return dense_fail(PS_EINVAL, "%s: fewer weight matrices than groups, and no list of which each uses", call);
+    if ((reinterpret_cast<uintptr_t>(l->offsets_dev) & 3) || (reinterpret_cast<uintptr_t>(l->weight_of_group_dev) & 3))
+        return dense_fail(PS_EINVAL, "%s: misaligned offsets or list of weight matrices", call);
+    // Grids are counted in 32 bits.  (Results of so many tiles fit no memory, but groups without rows count as well.)
+    const int64_t by_r = up(l->rows, 64) + l->n_groups, by_in = up(l->in_features, 64), by_out = up(l->out_features, 64);
+    if (std::max({by_r * by_out, by_r * by_in, by_out * by_in * l->n_groups}) > INT32_MAX / 2) return dense_fail(PS_EINVAL, "%s: too many tiles", call);
+    return PS_OK;
+}
+
+// m may be null if it need not be there.
+ps_status check_matrix(const char* call, const char* name, const ps_linear& l, const ps_matrix* m, bool needed, int64_t rows, int64_t cols, int64_t matrices)
+{
+    if (!m || (!m->data_dev && rows)) return needed && rows ? dense_fail(PS_EINVAL, "%s: %s is missing", call, name) : PS_OK;
+    const int size = dtype_size(l.dtype);
+    if (reinterpret_cast<uintptr_t>(m->data_dev) & (size - 1)) return dense_fail(PS_EINVAL, "%s: %s is not aligned to its elements", call, name);
+    if (rows > 1 && (m->row < cols || m->row > PS_DENSE_MAX_STRIDE)) return dense_fail(PS_EINVAL, "%s: %s has rows that overlap or are too far apart", call, name);
+    if (matrices > 1 && m->matrix < (rows - 1) * m->row + cols) return dense_fail(PS_EINVAL, "%s: %s has matrices that overlap", call, name);
+    return PS_OK;
+}
+
+bool there(const ps_matrix* m) { return m && m->data_dev; }
+
+// Base, rows and matrices at multiples of 16 bytes
+bool aligned16(const ps_linear& l, const void* data, int64_t row, int64_t matrix, bool one_row, bool one_matrix)
+{
+    const int64_t e = 16 / dtype_size(l.dtype);
+    return (reinterpret_cast<uintptr_t>(data) & 15) == 0 && (one_row || row % e == 0) && (one_matrix || matrix % e == 0);
+}
+bool aligned16(const ps_linear& l, const ps_matrix& m, int64_t rows, int64_t matrices)
+{
+    return aligned16(l, m.data_dev, m.row, m.matrix, rows <= 1, matrices <= 1);
+}
+
+Groups groups_of(const ps_linear& l) { return Groups{l.offsets_dev, l.weight_of_group_dev, l.n_groups, l.n_weights, (int32_t)l.rows}; }
+
+template <class F>
+void with_type(int dtype, F f)
+{
+    if (dtype == PS_F32)
+        f(float{});
+    else if (dtype == PS_BF16)
+        f(bf16_t{});
+    else
+        f(f16_t{});
+}
+
+void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, const ps_matrix& c, Epilogue epi, float* partial, hipStream_t s)
+{
+    const Plan plan = plan_product(l, kind, direct);
+    Product p{};
+    p.r = r.data_dev;
+    p.c = c.data_dev;
+    p.r_row = r.row;
+    p.c_row = c.row;
+    p.c_matrix = c.matrix;
+    p.rows = (int32_t)(kind == DW ? l.out_features : l.rows);
+    p.cols = (int32_t)(kind == FORWARD ? l.out_features : l.in_features);
+    p.depth = (int32_t)(kind == FORWARD ? l.in_features : kind == DX ? l.out_features : l.rows);
+    p.tiles_r = (int32_t)plan.tiles_r;
+    p.tiles_c = (int32_t)plan.tiles_c;
+    p.parts = plan.parts;
+    p.part_stages = plan.part_stages;
+    p.groups = groups_of(l);
+    p.epi = epi;
+    if (plan.parts > 1) p.epi.partial = partial;
+    (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
+    if (plan.parts > 1) {
+        const int64_t threads = up(p.cols, 8) * p.rows;
+        with_type(l.dtype, [&](auto t) {
+            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.rows, p.cols, epi);
+        });
+    }
+}
+
+ps_status launched(const char* call)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PS_OK : dense_fail(PS_EDEVICE, "%s: %s", call, hipGetErrorString(e));
+}
+
+}  // namespace
+}  // namespace ps
+
+extern "C" const char* ps_dense_last_error(void) { return ps::dense_error; }
+
+extern "C" ps_status ps_linear_workspace_bytes(const ps_linear* l, int32_t backward, uint64_t* bytes_out)
+{
+    using namespace ps;
+    const ps_status st = check_layer("ps_linear_workspace_bytes", l);
+    if (st != PS_OK) return st;
+    if (!bytes_out) return dense_fail(PS_EINVAL, "ps_linear_workspace_bytes: no place for the result");
+    *bytes_out = backward ? backward_space(*l).total : forward_space(*l);
+    return PS_OK;
+}
+
+extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias, const ps_matrix* residual,
+                                       const ps_matrix* y, const ps_matrix* pre, void* workspace, uint64_t workspace_bytes, void* hip_stream)
+{
+    using namespace ps;
+    static const char call[] = "ps_linear_forward";
+    ps_status st = check_layer(call, l);
+    if (st != PS_OK) return st;
+    if ((st = check_matrix(call, "x", *l, x, true, l->rows, l->in_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "w", *l, w, true, l->out_features, l->in_features, l->n_weights)) != PS_OK) return st;
+    if ((st = check_matrix(call, "bias", *l, bias, false, 1, l->out_features, l->n_weights)) != PS_OK) return st;
+    if ((st = check_matrix(call, "residual", *l, residual, false, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "y", *l, y, true, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "pre", *l, pre, false, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if (!l->rows) return PS_OK;
+    const uint64_t need = forward_space(*l);
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
+    if (workspace_bytes < need) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    Epilogue e{};
+    e.out = y->data_dev;
+    e.out_row = y->row;
+    if (there(bias)) e.bias = bias->data_dev, e.bias_matrix = bias->matrix;
+    if (there(residual)) e.residual = residual->data_dev, e.residual_row = residual->row;
+    if (there(pre)) e.pre = pre->data_dev, e.pre_row = pre->row;
+    e.act = l->activation;
+    const bool direct = direct_possible(*l, FORWARD) && aligned16(*l, *x, l->rows, 1) && aligned16(*l, *w, l->out_features, l->n_weights);
+    run_product(*l, FORWARD, direct, *x, *w, e, static_cast<float*>(workspace), s);
+    return launched(call);
+}
+
+extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy, const ps_matrix* x, const ps_matrix* w, const ps_matrix* pre,
+                                        const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db, void* workspace, uint64_t workspace_bytes,
+                                        void* hip_stream)
+{
+    using namespace ps;
+    static const char call[] = "ps_linear_backward";
+    ps_status st = check_layer(call, l);
+    if (st != PS_OK) return st;
+    const bool act = l->activation != PS_ACT_NONE, want_dx = there(dx), want_dw = there(dw), want_db = there(db);
+    if ((st = check_matrix(call, "dy", *l, dy, true, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "x", *l, x, want_dw, l->rows, l->in_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "w", *l, w, want_dx, l->out_features, l->in_features, l->n_weights)) != PS_OK) return st;
+    if ((st = check_matrix(call, "pre", *l, pre, act, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "dx", *l, dx, false, l->rows, l->in_features, 1)) != PS_OK) return st;
+    if ((st = check_matrix(call, "dw", *l, dw, false, l->out_features, l->in_features, l->n_groups)) != PS_OK) return st;
+    if ((st = check_matrix(call, "db", *l, db, false, 1, l->out_features, l->n_groups)) != PS_OK) return st;
+    if (!want_dx && !want_dw && !want_db) return PS_OK;
+    const BackwardSpace space = backward_space(*l);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
+    if (workspace_bytes < space.total) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    char* const base = static_cast<char*>(workspace);
+    const ps_matrix none{nullptr, 0, 0};
+    ps_matrix dz = dy ? *dy : none;
+    if (act) dz = ps_matrix{base + space.dz, space.dz_row, 0};
+    if (act || want_db) {
+        SlopeArgs a{};
+        a.dy = dy ? dy->data_dev : nullptr;
+        a.dy_row = dy ? dy->row : 0;
+        if (act && there(pre)) a.pre = pre->data_dev, a.pre_row = pre->row;
+        if (act && (want_dx || want_dw)) a.dz = dz.data_dev, a.dz_row = dz.row;
+        a.act = l->activation;
+        a.cols = (int32_t)l->out_features;
+        a.parts = space.parts;
+        a.groups = groups_of(*l);
+        if (want_db) a.partial = reinterpret_cast<float*>(base + space.bias);
+        const int64_t many = (int64_t)l->n_groups * space.parts;
+        with_type(l->dtype, [&](auto t) {
+            using T = decltype(t);
+            hipLaunchKernelGGL(slope_kernel<T>, dim3((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many), dim3(256), 0, s, a);
+            if (want_db)
+                hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)up(l->out_features, 256), l->n_groups), dim3(256), 0, s, a.partial,
+                                   static_cast<T*>(db->data_dev), db->matrix, (int)l->out_features, space.parts);
+        });
+    }
+    float* const partial = reinterpret_cast<float*>(base + space.partial);
+    if (want_dx && l->rows) {
+        Epilogue e{};
+        e.out = dx->data_dev;
+        e.out_row = dx->row;
+        const bool direct = direct_possible(*l, DX) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, *w, l->out_features, l->n_weights);
+        run_product(*l, DX, direct, dz, *w, e, partial, s);
+    }
+    if (want_dw) {
+        Epilogue e{};
+        e.out = dw->data_dev;
+        e.out_row = dw->row;
+        e.out_matrix = dw->matrix;
+        const ps_matrix xm = x ? *x : none;
+        const bool direct = direct_possible(*l, DW) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, xm, l->rows, 1);
+        run_product(*l, DW, direct, dz, xm, e, partial, s);
+    }
+    return launched(call);
+}

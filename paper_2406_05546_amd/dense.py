@@ -1,0 +1,323 @@
+"""ctypes binding of the dense-layer and optimizer operators of libps_hotpath.so (include/ps_dense.h): same names,
+argument checks and marshalling only.  Tensors are torch cuda tensors; work runs on torch's current stream of their device, and results
+and workspaces come from torch's allocator on that stream.  There is no fallback: a missing library or a refused call
+raises an exception."""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass, field
+from typing import List, Optional, Sequence, Tuple
+
+from .binding import PS_EINVAL, PS_OK, PsError, load_library
+
+PS_F32, PS_BF16, PS_F16 = range(3)
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+ADAMW_BLOCK = 256
+
+EXPORTS = ["ps_linear_workspace_bytes", "ps_linear_forward", "ps_linear_backward", "ps_adamw_workspace_bytes", "ps_adamw_create",
+           "ps_adamw_destroy", "ps_adamw_step", "ps_dense_last_error"]
+
+
+class ps_matrix(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("row", ctypes.c_int64), ("matrix", ctypes.c_int64)]
+
+
+class ps_linear(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("rows", ctypes.c_int64), ("in_features", ctypes.c_int64),
+                ("out_features", ctypes.c_int64), ("n_groups", ctypes.c_int32), ("n_weights", ctypes.c_int32),
+                ("offsets_dev", ctypes.c_void_p), ("weight_of_group_dev", ctypes.c_void_p)]
+
+
+class ps_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param_dev", ctypes.c_void_p), ("grad_dev", ctypes.c_void_p), ("copy_dev", ctypes.c_void_p), ("m_dev", ctypes.c_void_p),
+                ("v_dev", ctypes.c_void_p), ("m_scale_dev", ctypes.c_void_p), ("v_scale_dev", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("grad_row", ctypes.c_int64), ("grad_rows", ctypes.c_int32), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("copy_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("weight_decay", ctypes.c_float)]
+
+
+class ps_adamw_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64), ("n_rows", ctypes.c_int32)]
+
+
+_lib = None
+
+
+def _library() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        lib = load_library()
+        vp, i32, u64, p = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.POINTER
+        mats = [p(ps_matrix)]
+        for name, args in {
+                "ps_linear_workspace_bytes": [p(ps_linear), i32, p(u64)],
+                "ps_linear_forward": [p(ps_linear)] + 6 * mats + [vp, u64, vp],
+                "ps_linear_backward": [p(ps_linear)] + 7 * mats + [vp, u64, vp],
+                "ps_adamw_workspace_bytes": [p(ps_adamw_tensor), i32, p(u64)],
+                "ps_adamw_create": [p(vp), p(ps_adamw_tensor), i32, vp, u64, vp],
+                "ps_adamw_destroy": [vp],
+                "ps_adamw_step": [vp, p(ps_adamw_options), vp]}.items():
+            fn = getattr(lib, name)
+            fn.argtypes, fn.restype = args, ctypes.c_int
+        lib.ps_dense_last_error.argtypes, lib.ps_dense_last_error.restype = [], ctypes.c_char_p
+        _lib = lib
+    return _lib
+
+
+def _check(call: str, status: int) -> None:
+    if status != PS_OK:
+        raise PsError(call, status, (_library().ps_dense_last_error() or b"").decode())
+
+
+def _refuse(call: str, why: str) -> None:
+    raise PsError(call, PS_EINVAL, f"{call}: {why}")
+
+
+def _dtype(call: str, name: str, t) -> int:
+    import torch
+    code = {torch.float32: PS_F32, torch.bfloat16: PS_BF16, torch.float16: PS_F16}.get(t.dtype)
+    if code is None:
+        _refuse(call, f"{name} is {t.dtype}, not float32, bfloat16 or float16")
+    return code
+
+
+def _matrix(call: str, name: str, t, like, shape: Tuple[int, ...], matrices: bool = False) -> Optional[ps_matrix]:
+    """Checks that `t` has this shape and like's type and device; its pointer and strides."""
+    if t is None:
+        return None
+    if t.device != like.device or not t.is_cuda:
+        _refuse(call, f"{name} is on {t.device}, not on {like.device if like.is_cuda else 'a GPU'}")
+    if t.dtype != like.dtype:
+        _refuse(call, f"{name} is {t.dtype}, not {like.dtype}")
+    if tuple(t.shape) != shape:
+        _refuse(call, f"{name} has the shape {tuple(t.shape)}, not {shape}")
+    if shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+        _refuse(call, f"{name}'s rows are not contiguous")
+    rows = shape[-2] if len(shape) - (1 if matrices else 0) > 1 else 1
+    row = t.stride(-2) if rows > 1 else shape[-1]
+    return ps_matrix(t.data_ptr(), row, t.stride(0) if matrices and shape[0] > 1 else rows * row)
+
+
+def _ints(call: str, name: str, t, like, n: Optional[int] = None):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != like.device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse(call, f"{name} is a contiguous int32 tensor" + (f" of {n} elements" if n is not None else "") + " next to the others")
+    return t.data_ptr()
+
+
+def _layer(call: str, x, w, activation: str, offsets, weight_of_group):
+    grouped = offsets is not None
+    if activation not in ACTIVATIONS:
+        _refuse(call, f"unknown activation {activation!r}")
+    if x.dim() != 2 or w.dim() != (3 if grouped else 2):
+        _refuse(call, "x is [rows, in] and w " + ("[matrices, out, in]" if grouped else "[out, in]"))
+    _ints(call, "offsets", offsets, x)
+    n_groups = offsets.numel() - 1 if grouped else 1
+    if n_groups < 1:
+        _refuse(call, "offsets has one element more than there are groups, of which there is at least one")
+    index = _ints(call, "weight_of_group", weight_of_group, x, n_groups)
+    return ps_linear(_dtype(call, "x", x), ACTIVATIONS[activation], x.shape[0], x.shape[1], w.shape[-2], n_groups, w.shape[0] if grouped else 1,
+                     offsets.data_ptr() if grouped else None, index)
+
+
+def _ref(m: Optional[ps_matrix]):
+    return None if m is None else ctypes.byref(m)
+
+
+def _workspace(call: str, layer: ps_linear, backward: bool, device):
+    import torch
+    n = ctypes.c_uint64(0)
+    _check(call, _library().ps_linear_workspace_bytes(ctypes.byref(layer), 1 if backward else 0, ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def _call(call: str, layer: ps_linear, backward: bool, device, matrices) -> None:
+    import torch
+    if not device.type == "cuda":
+        _refuse(call, "tensors are on the GPU")
+    with torch.cuda.device(device):
+        ws = _workspace(call, layer, backward, device)
+        stream = torch.cuda.current_stream(device).cuda_stream
+        _check(call, getattr(_library(), call)(ctypes.byref(layer), *[_ref(m) for m in matrices], None if ws is None else ctypes.c_void_p(ws.data_ptr()),
+                                               0 if ws is None else ws.numel(), ctypes.c_void_p(stream)))
+
+
+def _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out):
+    import torch
+    call = "ps_linear_forward"
+    grouped = offsets is not None
+    layer = _layer(call, x, w, activation, offsets, weight_of_group)
+    rows, fin, fout, mats = x.shape[0], x.shape[1], w.shape[-2], (w.shape[0],) if grouped else ()
+    mx, mw = _matrix(call, "x", x, x, (rows, fin)), _matrix(call, "w", w, x, mats + (fout, fin), grouped)
+    mb = _matrix(call, "bias", bias, x, mats + (fout,), grouped)
+    mr, mp = _matrix(call, "residual", residual, x, (rows, fout)), _matrix(call, "pre", pre, x, (rows, fout))
+    y = torch.empty(rows, fout, dtype=x.dtype, device=x.device) if out is None else out
+    _call(call, layer, False, x.device, [mx, mw, mb, mr, _matrix(call, "out", y, x, (rows, fout)), mp])
+    return y
+
+
+def ps_linear_forward(x, w, bias=None, residual=None, activation: str = "none", pre=None, out=None):
+    """act(x w^T + bias) + residual.  x [rows, in], w [out, in], bias [out], residual [rows, out], all of one type
+    (float32, bfloat16, float16) with contiguous rows; activation "none", "relu", "gelu" or "silu".  pre [rows, out]
+    receives the value before the activation, which the backward pass reads.  out may be the residual.  Returns out."""
+    return _forward(x, None, w, bias, residual, activation, None, pre, out)
+
+
+def ps_grouped_linear_forward(x, offsets, w, bias=None, residual=None, activation: str = "none", weight_of_group=None, pre=None, out=None):
+    """The same for rows in groups: group g has rows offsets[g] .. offsets[g + 1] - 1 (int32 on the GPU) and uses matrix
+    weight_of_group[g] (or g) of w [matrices, out, in] and of bias [matrices, out].  Rows in no group are left as they are."""
+    return _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out)
+
+
+def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need, outs):
+    import torch
+    call = "ps_linear_backward"
+    grouped = offsets is not None
+    layer = _layer(call, x, w, activation, offsets, weight_of_group)
+    rows, fin, fout = x.shape[0], x.shape[1], w.shape[-2]
+    shapes = {"dx": (rows, fin), "dw": (fout, fin), "db": (fout,)}
+    if grouped:
+        shapes["dw"], shapes["db"] = (layer.n_groups, fout, fin), (layer.n_groups, fout)
+    mats = [_matrix(call, "dy", dy, x, (rows, fout)), _matrix(call, "x", x, x, (rows, fin)),
+            _matrix(call, "w", w, x, ((w.shape[0],) if grouped else ()) + (fout, fin), grouped), _matrix(call, "pre", pre, x, (rows, fout))]
+    got = []
+    for name, shape in shapes.items():
+        t = outs[name]
+        if t is None and need[name]:
+            t = torch.empty(shape, dtype=x.dtype, device=x.device)
+        got.append(t)
+        mats.append(_matrix(call, name, t, x, shape, grouped and name != "dx"))
+    _call(call, layer, True, x.device, mats)
+    return tuple(got)
+
+
+def ps_linear_backward(dy, x, w, activation: str = "none", pre=None, need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
+                       dx=None, dw=None, db=None):
+    """Gradients (dx, dw, db) of ps_linear_forward for dy [rows, out]; pre as the forward pass wrote it, not needed without
+    an activation.  What is not needed is None; dx, dw and db may be given tensors.  The residual's gradient is dy."""
+    return _backward(dy, x, None, w, activation, pre, None, dict(dx=need_dx, dw=need_dw, db=need_db), dict(dx=dx, dw=dw, db=db))
+
+
+def ps_grouped_linear_backward(dy, x, offsets, w, activation: str = "none", pre=None, weight_of_group=None, need_dx: bool = True,
+                               need_dw: bool = True, need_db: bool = True, dx=None, dw=None, db=None):
+    """The same for rows in groups: dw [groups, out, in] and db [groups, out] are every group's own (of a worker, say, whatever
+    matrix it used), zeros for a group without rows.  dw and db may be views into wider rows, for instance of a gradient buffer."""
+    return _backward(dy, x, offsets, w, activation, pre, weight_of_group, dict(dx=need_dx, dw=need_dw, db=need_db), dict(dx=dx, dw=dw, db=db))
+
+
+@dataclass
+class AdamW:
+    """Handle of one table of tensors, and what it refers to: the weights, gradients and states stay alive with it."""
+    handle: ctypes.c_void_p
+    device: object
+    state_bits: int
+    params: List[object]
+    grads: List[object]
+    m: List[object]
+    v: List[object]
+    m_scale: List[object]
+    v_scale: List[object]
+    copies: List[object]
+    workspace: object = None
+    closed: bool = field(default=False)
+
+    def __del__(self):
+        if not self.closed and self.handle and _lib is not None:
+            self.closed = True
+            _lib.ps_adamw_destroy(self.handle)
+
+
+def ps_adamw_create(params: Sequence, grads: Sequence, state_bits: int = 32, weight_decay=0.0, copies: Optional[Sequence] = None,
+                    m: Optional[Sequence] = None, v: Optional[Sequence] = None, m_scale: Optional[Sequence] = None,
+                    v_scale: Optional[Sequence] = None) -> AdamW:
+    """The table of an AdamW step over `params` (contiguous cuda tensors of float32, bfloat16 or float16).  grads[i]: a
+    gradient of params[i]'s shape, or buffered rows of it [rows, numel] whose rows may be any distance apart.  weight_decay: a
+    number, or one for each tensor.  copies[i] (or None) receives the new weights in its own type.  The states are made as zeros
+    unless given: float32 of the parameter's size, or with 8 bits uint8 or float8_e4m3fn codes and float32 scales, one for
+    256 elements.  Waits for the table's copy to the GPU."""
+    import torch
+    call = "ps_adamw_create"
+    params, grads = list(params), list(grads)
+    n = len(params)
+    decay = [float(weight_decay)] * n if not isinstance(weight_decay, (list, tuple)) else [float(d) for d in weight_decay]
+    copies = [None] * n if copies is None else list(copies)
+    if state_bits not in (8, 32):
+        _refuse(call, "states have 8 or 32 bits")
+    if n == 0:
+        _refuse(call, "no tensors")
+    device = params[0].device
+    if device.type != "cuda":
+        _refuse(call, "tensors are on the GPU")
+    given = {"m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale}
+    states = {}
+    for name, lst in given.items():
+        if lst is None:
+            if name.endswith("scale"):
+                lst = [torch.zeros(-(-p.numel() // ADAMW_BLOCK) if state_bits == 8 else 0, device=device) for p in params]
+            else:
+                lst = [torch.zeros(p.numel(), device=device, dtype=torch.uint8 if state_bits == 8 else torch.float32) for p in params]
+        states[name] = list(lst)
+    if any(len(lst) != n for lst in (grads, decay, copies, *states.values())):
+        _refuse(call, "one gradient, decay, copy and state for each tensor")
+    table = (ps_adamw_tensor * n)()
+    for i, p in enumerate(params):
+        g, c = grads[i], copies[i]
+        if p.device != device or not p.is_contiguous():
+            _refuse(call, f"tensor {i} is not contiguous, or on another device")
+        rows = g.dim() == 2 and tuple(g.shape) != tuple(p.shape) and g.shape[1] == p.numel()
+        if g.device != device or not (rows or tuple(g.shape) == tuple(p.shape)) or not (g.is_contiguous() if not rows else g.shape[1] <= 1 or g.stride(1) == 1):
+            _refuse(call, f"gradient {i} has neither tensor {i}'s shape nor rows of its {p.numel()} elements, or is not contiguous, or on another device")
+        if c is not None and (c.device != device or c.numel() != p.numel() or not c.is_contiguous()):
+            _refuse(call, f"copy {i} does not fit tensor {i}")
+        for name, lst in states.items():
+            s = lst[i]
+            scale = name.endswith("scale")
+            size = (-(-p.numel() // ADAMW_BLOCK) if state_bits == 8 else 0) if scale else p.numel()
+            types = (torch.float32,) if scale or state_bits == 32 else (torch.uint8, torch.float8_e4m3fn)
+            if s.device != device or not s.is_contiguous() or s.numel() != size or s.dtype not in types:
+                _refuse(call, f"{name}[{i}] does not fit tensor {i}")
+        table[i] = ps_adamw_tensor(p.data_ptr(), g.data_ptr(), None if c is None else c.data_ptr(), states["m"][i].data_ptr(), states["v"][i].data_ptr(),
+                                   states["m_scale"][i].data_ptr() or None, states["v_scale"][i].data_ptr() or None, p.numel(),
+                                   g.stride(0) if rows and g.shape[0] > 1 else p.numel(), g.shape[0] if rows else 1, _dtype(call, f"tensor {i}", p),
+                                   _dtype(call, f"gradient {i}", g), 0 if c is None else _dtype(call, f"copy {i}", c), state_bits, decay[i])
+    lib = _library()
+    size = ctypes.c_uint64(0)
+    handle = ctypes.c_void_p()
+    with torch.cuda.device(device):
+        _check(call, lib.ps_adamw_workspace_bytes(table, n, ctypes.byref(size)))
+        ws = torch.empty(size.value, dtype=torch.uint8, device=device)
+        _check(call, lib.ps_adamw_create(ctypes.byref(handle), table, n, ctypes.c_void_p(ws.data_ptr()), size.value,
+                                         ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
+    return AdamW(handle, device, state_bits, params, grads, states["m"], states["v"], states["m_scale"], states["v_scale"], copies, ws)
+
+
+def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
+                  n_rows: Optional[int] = None) -> None:
+    """Step number `step` (from 1) with the sum of the first n_rows gradient rows (all that every tensor has, if not given)."""
+    import torch
+    call = "ps_adamw_step"
+    if opt.closed:
+        _refuse(call, "the table was destroyed")
+    if n_rows is None:
+        n_rows = min(g.shape[0] if tuple(g.shape) != tuple(p.shape) else 1 for p, g in zip(opt.params, opt.grads))
+    o = ps_adamw_options(lr, beta1, beta2, eps, grad_scale, step, n_rows)
+    with torch.cuda.device(opt.device):
+        _check(call, _library().ps_adamw_step(opt.handle, ctypes.byref(o), ctypes.c_void_p(torch.cuda.current_stream(opt.device).cuda_stream)))
+
+
+def ps_adamw_state(opt: AdamW, i: int):
+    """Both moments of tensor i, as float32 values."""
+    import torch
+    if opt.state_bits == 32:
+        return opt.m[i], opt.v[i]
+    def values(codes, scale):
+        return codes.view(torch.float8_e4m3fn).float() * scale.repeat_interleave(ADAMW_BLOCK)[:codes.numel()]
+    return values(opt.m[i], opt.m_scale[i]), values(opt.v[i], opt.v_scale[i]).square()
+
+
+def ps_adamw_destroy(opt: AdamW) -> None:
+    if not opt.closed:
+        opt.closed = True
+        _check("ps_adamw_destroy", _library().ps_adamw_destroy(opt.handle))
