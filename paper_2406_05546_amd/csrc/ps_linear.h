@@ -121,7 +121,8 @@ template <class T>
 struct Mma;
 template <>
 struct Mma<bf16_t> {
-    static constexpr int E = 8;  // values in 16 bytes
+    static constexpr int E = 8;      // values in 16 bytes
+    static constexpr int STEPS = 1;  // instructions
     static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
     {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, c), __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
@@ -129,7 +130,7 @@ struct Mma<bf16_t> {
 };
 template <>
 struct Mma<f16_t> {
-    static constexpr int E = 8;
+    static constexpr int E = 8, STEPS = 1;
     static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
     {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, c), __builtin_bit_cast(f16x8, r), acc, 0, 0, 0);
@@ -137,7 +138,7 @@ struct Mma<f16_t> {
 };
 template <>
 struct Mma<float> {
-    static constexpr int E = 4;
+    static constexpr int E = 4, STEPS = 4;
     static __device__ __forceinline__ void add(const uintx4& c, const uintx4& r, floatx4& acc)
     {
         // one k of each 16 bytes at a time
@@ -147,31 +148,48 @@ struct Mma<float> {
 };
 
 // ---------------------------------------------------------------------------------------------------------------
-// One operand's tile in LDS: ROWS rows (or columns) of the result and 128 bytes of k, ROWS * 128 bytes.
+// 16 bytes for every lane from memory straight to LDS, one behind the other from `to` on (the same for all lanes).  Written as
+// it is and not by its builtin, because the compiler has every transposing LDS read wait for all such loads that it knows of;
+// it has no result that could be overwritten, and whoever reads what it brings waits for vmcnt himself.
+__device__ __forceinline__ void load_to_lds(uintx4 descriptor, uint32_t offset, int to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(descriptor), "s"(to) : "memory");
+}
+__device__ __forceinline__ int lds_address(const char* p) { return scalar((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p); }
+
+// ---------------------------------------------------------------------------------------------------------------
+// One operand's tile in LDS: ROWS rows (or columns) of the result, shared by W wavefronts along them, and 128 bytes of k;
+// in HALVES pieces that are brought and read one after the other, each with its part of every wavefront's rows:
+// row w * ROWS / W + h * EACH + i of the tile is row w * EACH + i of half h.
 //
-// KC: row r at r * 128, its 16-byte pieces exchanged by a function of the row, so that 16 lanes that read the same piece
-// of 16 rows, and 8 lanes that read it of 8, use all banks once.  RC: k at k * ROWS * sizeof(T), 32-byte groups (16 columns
-// of a 16-bit type; 64 bytes of fp32) exchanged by a function of k for the same reason; the transposing LDS read
+// KC: row r of a half at r * 128, its 16-byte pieces exchanged by a function of the row, so that 16 lanes that read the same
+// piece of 16 rows, and 8 lanes that read it of 8, use all banks once.  RC: k at k * HROWS * sizeof(T), 32-byte groups
+// (16 columns of a 16-bit type; 64 bytes of fp32) exchanged by a function of k for the same reason; the transposing LDS read
 // (ds_read_b64_tr_b16: 16 lanes read 16 columns of four k, and each gets the four k of its column) turns 16-bit types.
 // COLS: the operand that is the result's columns.  If it is KC, row 4q + e of the MFMA tiles 2t and 2t + 1 is column
 // 32 t + 8 q + e and + 4, so that a lane ends up with eight consecutive columns.
 //
 // NT threads bring it, 16 bytes at a time.  DIRECT: memory to LDS without registers; rows start at multiples of 16 bytes
 // and have multiples of 16 bytes, buffer bounds give zeros past the last row.  Else through registers, at any alignment.
-template <class T, bool KC, bool COLS, int ROWS, int NT, bool DIRECT>
+template <class T, bool KC, bool COLS, int ROWS, int W, int HALVES, int NT, bool DIRECT>
 struct Operand {
     static constexpr int SIZE = sizeof(T), E = 16 / SIZE, BK = 128 / SIZE;
-    static constexpr int BYTES = ROWS * 128, LOADS = BYTES / (NT * 16);
-    static_assert(LOADS * NT * 16 == BYTES, "every thread brings the same number of pieces");
-    static constexpr int PIECES = ROWS / E;  // RC: pieces of one k
+    static constexpr int HROWS = ROWS / HALVES, EACH = HROWS / W;  // rows of a half, and of one wavefront in it
+    static constexpr int HBYTES = HROWS * 128, BYTES = ROWS * 128, LOADS = HBYTES / (NT * 16);  // LOADS: instructions of a half
+    static_assert(LOADS * NT * 16 == HBYTES, "every thread brings the same number of pieces");
+    static constexpr int PIECES = HROWS / E;  // RC: pieces of one k
     static constexpr bool PERMUTED = KC && COLS;
-    static constexpr int SUBS = 2;           // reads of 16 bytes of k for each of the four lane groups
+    static_assert(EACH % (PERMUTED ? 32 : 16) == 0, "whole MFMA tiles, or pairs of them");
+    static_assert(!DIRECT || (KC ? NT / 8 % 32 == 0 && (NT / 8 % EACH == 0 || EACH % (NT / 8) == 0) : NT / PIECES % 16 == 0), "the loads' places differ by the same for every thread");
+    static constexpr int SUBS = 2;                            // reads of 16 bytes of k for each of the four lane groups
+    static constexpr int READS = KC ? 1 : SIZE == 2 ? 2 : 4;  // LDS instructions of one
 
-    const char* base;  // of this tile's first row (KC) or column (RC) and the first k of the next stage to be brought
+    const char* base;  // of the tile's first row (KC) or column (RC) and the first k of the next stage to be brought
     int64_t step;      // bytes from stage to stage
     int32_t pitch;     // bytes from row to row (KC) or from k to k (RC)
     int32_t left;      // k still to be brought
     int32_t rows;      // KC: valid rows of the tile; RC: valid columns
+    int32_t own_offset, own_element;  // of this thread's piece in the first load of the first half: byte from `base`, and see `place`
     uintx4 reg[DIRECT ? 1 : LOADS];
 
     static __device__ __forceinline__ int kc_swap(int row)
@@ -181,87 +199,102 @@ struct Operand {
     static __device__ __forceinline__ int rc_swap(int k)  // in 16-byte pieces
     {
         if (SIZE == 4) return (k >> 2 & 3) << 2;
-        return ROWS >= 128 ? ((k & 3) | (k >> 3 & 1) << 2) << 1 : ((k >> 1 & 1) | (k >> 3 & 1) << 1) << 1;
+        return HROWS >= 128 ? ((k & 3) | (k >> 3 & 1) << 2) << 1 : ((k >> 1 & 1) | (k >> 3 & 1) << 1) << 1;
     }
-    // Piece i of thread t: its row (KC) or k (RC), and its 16-byte piece within
-    static __device__ __forceinline__ void place(int i, int t, int& line, int& piece)
+    // Piece i of thread t of a half: row (KC) or k (RC) of the tile, and element of k (KC) or column (RC) of the tile
+    static __device__ __forceinline__ void place(int half, int i, int t, int& line, int& element)
     {
         const int f = i * NT + t;
         if (KC) {
-            line = f >> 3;
-            piece = (f & 7) ^ kc_swap(line);
+            const int r = f >> 3;
+            line = r / EACH * (EACH * HALVES) + half * EACH + r % EACH;
+            element = ((f & 7) ^ kc_swap(r)) * E;
         } else {
             line = f / PIECES;
-            piece = (f & (PIECES - 1)) ^ rc_swap(line);
+            const int c = ((f & (PIECES - 1)) ^ rc_swap(line)) * E;
+            element = c / EACH * (EACH * HALVES) + half * EACH + c % EACH;
         }
     }
 
     // first: element of the tile's first row or column and the first k
-    __device__ __forceinline__ void init(const T* first, int64_t stride, int valid, int depth)
+    __device__ __forceinline__ void init(const T* first, int64_t stride, int valid, int depth, int t)
     {
         base = reinterpret_cast<const char*>(first);
         pitch = (int32_t)(stride * SIZE);
         step = KC ? 128 : (int64_t)pitch * BK;
         left = depth;
         rows = min(valid, ROWS);
+        int line;
+        place(0, 0, t, line, own_element);
+        own_offset = line * pitch + own_element * SIZE;
     }
 
-    __device__ __forceinline__ void bring(char* tile, int t)
+    // DIRECT: load i of a half of the next stage, or nothing past the last one, to the LDS address `tile` (of that half).  wave: a scalar.
+    __device__ __forceinline__ void bring(int half, int i, int tile, int wave) const
     {
-        if constexpr (DIRECT) {
-            // Last byte that may be read: KC, of the last row (what is past its end in the last stage is left out below); RC,
-            // of the last k.
-            const int lines = KC ? rows : min(left, BK);
-            const uint32_t bytes = lines > 0 ? (uint32_t)(lines - 1) * (uint32_t)pitch + (uint32_t)(KC ? min(left, BK) : rows) * SIZE : 0u;
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
+        // A load is at the same place for every thread but for what is the same for all of them, by which the descriptor's
+        // base is moved.  What may be read ends, KC, with the last row (what is past its end in the last stage is left out
+        // below); RC, with the last k.
+        const int lines = KC ? rows : min(left, BK), last = (KC ? min(left, BK) : rows) * SIZE;
+        const int bytes = (lines - 1) * pitch + last;  // without lines not above 0: they are no closer than they are long
+        const uint32_t offset = KC && own_element >= left ? 0xfffffff0u : (uint32_t)own_offset;  // past a row's end: nowhere, which reads as zero
+        int line, element;
+        place(half, i, 0, line, element);
+        const int moved = line * pitch + element * SIZE;  // of thread 0, which is at 0 in the first load of the first half
+        const uint64_t from = reinterpret_cast<uint64_t>(base + moved);
+        load_to_lds(uintx4{(uint32_t)scalar((int)from), (uint32_t)scalar((int)(from >> 32)) & 0xffffu, (uint32_t)scalar(max(bytes - moved, 0)), 0x00020000u}, offset,
+                    tile + (i * NT + wave * 64) * 16);
+    }
+    // All of it
+    __device__ __forceinline__ void bring(int half, int tile, int wave) const
+    {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                int line, piece;
-                place(i, t, line, piece);
-                uint32_t offset = (uint32_t)line * (uint32_t)pitch + piece * 16;
-                if (KC && piece * E >= left) offset = 0xfffffff0u;  // past the end of the row: beyond `bytes`, and so zero
-                char* to = tile + (i * NT + (t & ~63)) * 16;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, (int)offset, 0, 0, 0);
-            }
-        } else {
+        for (int i = 0; i < LOADS; ++i) bring(half, i, tile, wave);
+    }
+    // Through registers: the whole next stage.
+    __device__ __forceinline__ void load(int t)
+    {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                int line, piece;
-                place(i, t, line, piece);
-                const int n = KC ? (line < rows ? left - piece * E : 0) : (line < left ? rows - piece * E : 0);
-                const char* p = base + (int64_t)line * pitch + piece * 16;
-                reg[i] = uintx4{0, 0, 0, 0};
-                if (n >= E) {
-                    __builtin_memcpy(&reg[i], p, 16);
-                } else if (n > 0) {
-                    const T* q = reinterpret_cast<const T*>(p);
+        for (int i = 0; i < LOADS; ++i) {
+            int line, element;
+            place(0, i, t, line, element);
+            const int n = KC ? (line < rows ? left - element : 0) : (line < left ? rows - element : 0);
+            const char* p = base + (int64_t)line * pitch + element * SIZE;
+            uintx4 v = {0, 0, 0, 0};
+            if (n >= E) {
+                __builtin_memcpy(&v, p, 16);
+            } else if (n > 0) {
+                const T* q = reinterpret_cast<const T*>(p);
 #pragma unroll
-                    for (int e = 0; e < E - 1; ++e) {
-                        if (e >= n) continue;
-                        if constexpr (SIZE == 4)
-                            reg[i][e] = __float_as_uint(q[e]);
-                        else
-                            reg[i][e / 2] |= (uint32_t)q[e].bits << (16 * (e & 1));
-                    }
+                for (int e = 0; e < E - 1; ++e) {
+                    if (e >= n) continue;
+                    if constexpr (SIZE == 4)
+                        v[e] = __float_as_uint(q[e]);
+                    else
+                        v[e / 2] |= (uint32_t)q[e].bits << (16 * (e & 1));
                 }
             }
+            reg[i] = v;
         }
+    }
+    __device__ __forceinline__ void next_stage()
+    {
         base += step;
-        left -= BK;
+        left = max(left - BK, 0);
     }
     __device__ __forceinline__ void put(char* tile, int t) const
     {
+        static_assert(DIRECT || HALVES == 1, "operands through registers come whole");
         if constexpr (!DIRECT) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) *reinterpret_cast<uintx4*>(tile + (i * NT + t) * 16) = reg[i];
         }
     }
 
-    // 16 bytes of k of the lane's row in MFMA tile `tile16` (rows 16 tile16 ..) of the rows from `first` (a multiple of 16,
-    // or of 32 if permuted) on: k = (sub * 4 + lane / 16) * E ..
-    static __device__ __forceinline__ uintx4 fetch(const char* tile, int first, int tile16, int sub, int lane)
+    // 16 bytes of k of the lane's row in MFMA tile `tile16` of wavefront w's rows of a half, `tile`: k = (sub * 4 + lane / 16) * E ..
+    static __device__ __forceinline__ uintx4 fetch(const char* tile, int w, int tile16, int sub, int lane)
     {
-        const int l = lane & 15, q = lane >> 4;
+        const int l = lane & 15, q = lane >> 4, first = w * EACH;
         if constexpr (KC) {
             const int row = PERMUTED ? first + 32 * (tile16 >> 1) + 8 * (l >> 2) + 4 * (tile16 & 1) + (l & 3) : first + 16 * tile16 + l;
             return *reinterpret_cast<const uintx4*>(tile + row * 128 + (((sub * 4 + q) ^ kc_swap(row)) << 4));
@@ -270,9 +303,9 @@ struct Operand {
             typedef __attribute__((address_space(3))) shortx4* LdsPtr;
             const int k = 32 * sub + 8 * q + (l >> 2);
             const int piece = (2 * (first / 16 + tile16)) ^ rc_swap(k);
-            const char* p = tile + k * (ROWS * 2) + piece * 16 + (l & 3) * 8;
+            const char* p = tile + k * (HROWS * 2) + piece * 16 + (l & 3) * 8;
             const uintx2 a = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(shortx4*)p));
-            const uintx2 b = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(shortx4*)(p + 4 * ROWS * 2)));
+            const uintx2 b = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(shortx4*)(p + 4 * HROWS * 2)));
             return uintx4{a[0], a[1], b[0], b[1]};
         } else {
             uintx4 v;
@@ -280,7 +313,7 @@ struct Operand {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int k = 16 * sub + 4 * q + e;
-                v[e] = *reinterpret_cast<const uint32_t*>(tile + k * (ROWS * 4) + (((col >> 2) ^ rc_swap(k)) << 4) + (col & 3) * 4);
+                v[e] = *reinterpret_cast<const uint32_t*>(tile + k * (HROWS * 4) + (((col >> 2) ^ rc_swap(k)) << 4) + (col & 3) * 4);
             }
             return v;
         }
@@ -382,15 +415,31 @@ __device__ __forceinline__ bool tile_of_block(const Product& p, int block, int& 
     return true;
 }
 
+// s_waitcnt's argument: all but `n` of the wavefront's loads are done; everything of it is done.
+constexpr int wait_vm(int n) { return (n & 15) | (n >> 4) << 14 | 0xf70; }
+constexpr int WAIT_ALL = 0x0070;
+
+// A barrier that waits for nothing in flight; no memory access is moved across it.
+__device__ __forceinline__ void block_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DIRECT, int RAGGED>
 __global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_kernel(Product p)
 {
     constexpr int NT = 64 * WR * WC, TR = BR / WR / 16, TC = BC / WC / 16;
-    using OpR = Operand<T, R_KC, false, BR, NT, DIRECT>;
-    using OpC = Operand<T, C_KC, true, BC, NT, DIRECT>;
-    constexpr int BK = OpR::BK, SUBS = OpR::SUBS;
-    static_assert(!OpC::PERMUTED || TC % 2 == 0, "permuted columns come in pairs of tiles");
-    __shared__ __attribute__((aligned(256))) char lds[2][OpR::BYTES + OpC::BYTES];
+    constexpr int HALVES = DIRECT && TR >= 4 && TC >= 4 ? 2 : 1, HR = TR / HALVES, HC = TC / HALVES;
+    using OpR = Operand<T, R_KC, false, BR, WR, HALVES, NT, DIRECT>;
+    using OpC = Operand<T, C_KC, true, BC, WC, HALVES, NT, DIRECT>;
+    constexpr int BK = OpR::BK, SUBS = OpR::SUBS, STEPS = Mma<T>::STEPS;
+    // One array: where there are several, the compiler keeps account of what comes into which, and waits for more than it must.
+    __shared__ __attribute__((aligned(256))) char lds[2 * (OpR::BYTES + OpC::BYTES)];
+    constexpr int BUFFER = OpR::BYTES + OpC::BYTES;
+    char *const r00 = lds, *const r01 = r00 + OpR::HBYTES, *const c00 = lds + OpR::BYTES, *const c01 = c00 + OpC::HBYTES;
+    char *const r10 = r00 + BUFFER, *const c10 = c00 + BUFFER;
 
     int tr, tc, part;
     if (!tile_of_block(p, blockIdx.x, tr, tc, part)) return;
@@ -419,8 +468,8 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_ker
 
     OpR opr;
     OpC opc;
-    opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)r0 * p.r_row + k_first : (int64_t)k_first * p.r_row + r0), p.r_row, r_valid, depth);
-    opc.init(static_cast<const T*>(p.c) + matrix * p.c_matrix + (C_KC ? (int64_t)c0 * p.c_row + k_first : (int64_t)k_first * p.c_row + c0), p.c_row, c_valid, depth);
+    opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)r0 * p.r_row + k_first : (int64_t)k_first * p.r_row + r0), p.r_row, r_valid, depth, tid);
+    opc.init(static_cast<const T*>(p.c) + matrix * p.c_matrix + (C_KC ? (int64_t)c0 * p.c_row + k_first : (int64_t)k_first * p.c_row + c0), p.c_row, c_valid, depth, tid);
 
     floatx4 acc[TR][TC];
 #pragma unroll
@@ -429,37 +478,166 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_ker
         for (int j = 0; j < TC; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
     const int stages = (depth + BK - 1) / BK;
-    if (stages > 0) {
-        opr.bring(lds[0], tid);
-        opc.bring(lds[0] + OpR::BYTES, tid);
-        opr.put(lds[0], tid);
-        opc.put(lds[0] + OpR::BYTES, tid);
-    }
-    __syncthreads();
-    for (int s = 0; s < stages; ++s) {
-        const char* now = lds[s & 1];
-        char* next = lds[~s & 1];
-        if (s + 1 < stages) {
-            opr.bring(next, tid);
-            opc.bring(next + OpR::BYTES, tid);
+    uintx4 fr[HALVES][HR][SUBS], fc[HALVES][HC][SUBS];
+    // LDS addresses of the halves in the first buffer
+    const int to_r[2] = {lds_address(lds), lds_address(lds) + OpR::HBYTES}, to_c[2] = {to_r[0] + OpR::BYTES, to_r[0] + OpR::BYTES + OpC::HBYTES};
+    auto bring_r = [&](int h, int buffer) __attribute__((always_inline)) { opr.bring(h, to_r[h] + buffer * BUFFER, wave); };
+    auto bring_c = [&](int h, int buffer) __attribute__((always_inline)) { opc.bring(h, to_c[h] + buffer * BUFFER, wave); };
+    auto fetch_r = [&](int h, const char* from, int sub) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < HR; ++i) fr[h][i][sub] = OpR::fetch(from, wr, i, sub, lane);
+    };
+    auto fetch_c = [&](const char* from, int sub, int set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < HC; ++j) fc[set][j][sub] = OpC::fetch(from, wc, j, sub, lane);
+    };
+    auto multiply = [&](int hr, int hc, int sub, int set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < HR; ++i)
+#pragma unroll
+            for (int j = 0; j < HC; ++j) Mma<T>::add(fc[set][j][sub], fr[hr][i][sub], acc[hr * HR + i][hc * HC + j]);
+    };
+    if constexpr (HALVES == 2) {
+        // A stage in four phases, a quarter of the products each, in an order in which each phase needs one more half of an
+        // operand: it is read from LDS in the phase before.
+        //     products   R0 C0   R0 C1   R1 C1   R1 C0
+        //     reads      C1      R1      R0'     C0'      (') of the next stage
+        //     brings     R0"     C0"     C1"     R1"      (") of the stage after that, into this one's buffer
+        // Two barriers a stage, behind the second and the fourth phase: past them everybody's part of what is read next is in
+        // LDS, and nobody reads any more what is replaced next.  So a load has a stage and a half to arrive (with whole
+        // operands and one barrier it had one).
+        constexpr int FLIGHT = 2 * (OpR::LOADS + OpC::LOADS);
+        static_assert(OpR::LOADS == 2 && OpC::LOADS == 2, "a phase places two loads");
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            bring_r(0, b);
+            bring_c(0, b);
+            bring_c(1, b);
+            bring_r(1, b);
+            opr.next_stage();
+            opc.next_stage();
         }
+        __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT));
+        block_barrier();
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            uintx4 fr[TR], fc[TC];
-#pragma unroll
-            for (int j = 0; j < TC; ++j) fc[j] = OpC::fetch(now + OpR::BYTES, wc * TC * 16, j, sub, lane);
-#pragma unroll
-            for (int i = 0; i < TR; ++i) fr[i] = OpR::fetch(now, wr * TR * 16, i, sub, lane);
-#pragma unroll
-            for (int i = 0; i < TR; ++i)
-#pragma unroll
-                for (int j = 0; j < TC; ++j) Mma<T>::add(fc[j], fr[i], acc[i][j]);
+            fetch_c(c00, sub, 0);
+            fetch_r(0, r00, sub);
         }
-        if (s + 1 < stages) {
-            opr.put(next, tid);
-            opc.put(next + OpR::BYTES, tid);
+        __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT) & ~0xf00);
+        block_barrier();
+        // A phase: the products of two halves, the reads of a third (`fetch`), and two loads, each behind a half of the products
+        auto phase = [&](int hr, int hc, int set, auto fetch, auto load) __attribute__((always_inline)) {
+            fetch();
+            multiply(hr, hc, 0, set);
+#pragma unroll
+            for (int i = 0; i < HR * HC; ++i) {  // the reads among the products
+                __builtin_amdgcn_sched_group_barrier(0x008, STEPS, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, std::max(HR * OpR::READS, HC * OpC::READS) * SUBS / (HR * HC), 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load(0);
+            multiply(hr, hc, 1, set);
+            __builtin_amdgcn_sched_barrier(0);
+            load(1);
+        };
+        // c0: the registers that hold C0 (those of C1 are free for the next stage's C0 when that is read)
+        auto stage = [&](int buffer, int c0) __attribute__((always_inline)) {
+            // unknown to the compiler, which would keep addresses for either buffer in registers, and have too few
+            int from = buffer * BUFFER, from_next = BUFFER - from;
+            asm volatile("" : "+s"(from), "+s"(from_next));
+            const int to = buffer * BUFFER;
+            phase(0, 0, c0, [&]() __attribute__((always_inline)) {
+                fetch_c(c01 + from, 0, c0 ^ 1);
+                fetch_c(c01 + from, 1, c0 ^ 1);
+            }, [&](int i) __attribute__((always_inline)) { opr.bring(0, i, to_r[0] + to, wave); });
+            phase(0, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
+                fetch_r(1, r01 + from, 0);
+                fetch_r(1, r01 + from, 1);
+            }, [&](int i) __attribute__((always_inline)) { opc.bring(0, i, to_c[0] + to, wave); });
+            __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT) & ~0xf00);
+            block_barrier();
+            phase(1, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
+                fetch_r(0, r00 + from_next, 0);  // behind the last stage what lay there before, which nobody uses
+                fetch_r(0, r00 + from_next, 1);
+            }, [&](int i) __attribute__((always_inline)) { opc.bring(1, i, to_c[1] + to, wave); });
+            phase(1, 0, c0, [&]() __attribute__((always_inline)) {
+                fetch_c(c00 + from_next, 0, c0 ^ 1);
+                fetch_c(c00 + from_next, 1, c0 ^ 1);
+            }, [&](int i) __attribute__((always_inline)) { opr.bring(1, i, to_r[1] + to, wave); });
+            opr.next_stage();
+            opc.next_stage();
+            __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT) & ~0xf00);
+            block_barrier();
+        };
+        for (int s = 0; s < stages; s += 2) {
+            stage(0, 0);
+            if (s + 1 < stages) stage(1, 1);
+        }
+        __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+    } else if constexpr (DIRECT) {
+        // While the products of one half of a stage's k are formed, the operands of the next half are on their way from LDS to
+        // registers, and those of the next stage from memory to LDS.  One barrier a stage, in its middle: past it everybody's
+        // part of the next stage is in LDS, and nobody reads this one's buffer any more, which then takes the stage after next.
+        auto bring = [&](int buffer) __attribute__((always_inline)) {
+            bring_r(0, buffer);
+            bring_c(0, buffer);
+            opr.next_stage();
+            opc.next_stage();
+        };
+        auto fetch = [&](const char* r, const char* c, int sub) __attribute__((always_inline)) {
+            fetch_c(c, sub, 0);
+            fetch_r(0, r, sub);
+        };
+        constexpr int LOADS = OpR::LOADS + OpC::LOADS;
+        bring(0);
+        bring(1);
+        __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
+        block_barrier();
+        fetch(r00, c00, 0);
+        auto stage = [&](int buffer) __attribute__((always_inline)) {
+            fetch(buffer ? r10 : r00, buffer ? c10 : c00, 1);
+            multiply(0, 0, 0, 0);
+            __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+            block_barrier();
+            fetch(buffer ? r00 : r10, buffer ? c00 : c10, 0);  // behind the last stage what lay there before, which nobody uses
+            multiply(0, 0, 1, 0);
+            bring(buffer);
+        };
+        for (int s = 0; s < stages; s += 2) {
+            stage(0);
+            if (s + 1 < stages) stage(1);
+        }
+        __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+    } else {
+        if (stages > 0) {
+            opr.load(tid);
+            opc.load(tid);
+            opr.put(r00, tid);
+            opc.put(c00, tid);
         }
         __syncthreads();
+        for (int s = 0; s < stages; ++s) {
+            const char *r = s & 1 ? r10 : r00, *c = s & 1 ? c10 : c00;
+            char *r_next = s & 1 ? r00 : r10, *c_next = s & 1 ? c00 : c10;
+            if (s + 1 < stages) {
+                opr.next_stage();
+                opc.next_stage();
+                opr.load(tid);
+                opc.load(tid);
+            }
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                fetch_c(c, sub, 0);
+                fetch_r(0, r, sub);
+                multiply(0, 0, sub, 0);
+            }
+            if (s + 1 < stages) {
+                opr.put(r_next, tid);
+                opc.put(c_next, tid);
+            }
+            __syncthreads();
+        }
     }
 
     // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.

@@ -279,8 +279,9 @@ void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, 
     Product p{};
     p.r = r.data_dev;
     p.c = c.data_dev;
-    p.r_row = r.row;
-    p.c_row = c.row;
+    // a single row's distance to the next may be anything, but the kernels multiply with it
+    p.r_row = l.rows > 1 ? r.row : kind == FORWARD ? l.in_features : l.out_features;
+    p.c_row = (kind == DW ? l.rows : l.out_features) > 1 ? c.row : l.in_features;
     p.c_matrix = c.matrix;
     p.rows = (int32_t)(kind == DW ? l.out_features : l.rows);
     p.cols = (int32_t)(kind == FORWARD ? l.out_features : l.in_features);
