@@ -22,8 +22,6 @@ ps_status dense_fail(ps_status st, const char* format, ...)
 
 namespace {
 
-constexpr int COMPUTE_UNITS = 256;
-
 // ---- dz = dy act'(z), and the sums over rows that are the bias's gradient ------------------------------------------
 
 struct SlopeArgs {
