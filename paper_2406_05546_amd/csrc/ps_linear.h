@@ -759,6 +759,9 @@ void launch_linear_forward(const Product& p, int dtype, bool direct, int tile, h
 void launch_linear_dx(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 void launch_linear_dw(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 
+// Forward pass for few rows, 16 * row_tiles of a group (1, 2 or 4) to a block; tiles_r counts these, tiles_c 16 columns each.
+void launch_linear_few(const Product& p, int dtype, int row_tiles, hipStream_t s);
+
 // Sizes of square tiles, by number.
 constexpr int LINEAR_TILE[3] = {64, 128, 256};
 

@@ -131,6 +131,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
 enum { FORWARD, DX, DW };
 
 struct Plan {
+    int few;  // if not 0: forward pass for few rows, so many times 16 of a group to a block
     int tile, parts, part_stages;
     int64_t tiles_r, tiles_c;
     uint64_t partial_bytes;
@@ -144,6 +145,15 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
     const int64_t depth = kind == FORWARD ? l.in_features : kind == DX ? l.out_features : l.rows;
     const bool one = !l.offsets_dev;
     Plan best{};
+    const int64_t each = up(l.rows, l.n_groups);
+    if (kind == FORWARD && each <= 64) {
+        best.few = each <= 16 ? 1 : each <= 32 ? 2 : 4;
+        best.parts = 1;
+        best.tiles_r = up(l.rows, 16 * best.few) + (one ? 0 : l.n_groups);
+        best.tiles_c = up(l.out_features, 16);
+        if (best.tiles_r * best.tiles_c <= INT32_MAX) return best;
+        best = Plan{};
+    }
     for (int tile = l.dtype == PS_F32 || !direct ? 1 : 2; tile >= 0; --tile) {
         const int size = LINEAR_TILE[tile];
         Plan p{};
@@ -291,6 +301,7 @@ void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, 
     p.groups = groups_of(l);
     p.epi = epi;
     if (plan.parts > 1) p.epi.partial = partial;
+    if (plan.few) return launch_linear_few(p, l.dtype, plan.few, s);
     (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
     if (plan.parts > 1) {
         const int64_t threads = up(p.cols, 8) * p.rows;

@@ -1,0 +1,123 @@
+// Forward pass for few rows (a token, a few sequences, few rows of each of many groups): bound by reading the weights
+// once, so these go straight to registers, and all wavefronts of a block read the same 16 columns' weights, each its share
+// of k.
+#include "ps_linear.h"
+
+namespace ps {
+
+namespace {
+
+// A block: 16 columns, 16 * TR rows of a group.  128 bytes of k of each column make a step (a lane 32 bytes of its column, so that
+// a load instruction touches half cache lines in pairs, whole ones together), and wavefront w takes every WAVES-th step.  Which
+// k a lane's values have does not matter as long as both operands agree.  The wavefronts' sums are added up in order.
+template <class T, int TR, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
+{
+    constexpr int E = Mma<T>::E, STEP = 8 * E, AHEAD = TR > 2 ? 2 : 4;
+    __shared__ floatx4 meet[WAVES][TR][64];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), l = lane & 15, q = lane >> 4;
+    const int tc = blockIdx.x % p.tiles_c, tr = blockIdx.x / p.tiles_c;
+    GroupRows rows;
+    int r0;
+    if (!find_rows(p.groups, tr, 16 * TR, rows, r0)) return;
+    const int matrix = group_matrix(p.groups, rows.g), c0 = tc * 16;
+
+    // Rows and columns past the end read the last ones again; nobody stores them.
+    const T* c = static_cast<const T*>(p.c) + matrix * p.c_matrix + (int64_t)min(c0 + l, p.cols - 1) * p.c_row;
+    const T* r[TR];
+#pragma unroll
+    for (int i = 0; i < TR; ++i) r[i] = static_cast<const T*>(p.r) + (int64_t)min(r0 + 16 * i + l, rows.end - 1) * p.r_row;
+
+    floatx4 acc[TR];
+#pragma unroll
+    for (int i = 0; i < TR; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    struct Pair {
+        uintx4 v[2];
+    };
+    auto whole = [&](const T* row, int k) __attribute__((always_inline)) {
+        Pair x;
+        __builtin_memcpy(&x, row + k, 32);
+        return x;
+    };
+    auto some = [&](const T* row, int k) __attribute__((always_inline)) {  // zeros past the end of the row
+        Pair x = {};
+        T e[2 * E];
+        __builtin_memcpy(e, &x, 32);
+#pragma unroll
+        for (int i = 0; i < 2 * E; ++i)
+            if (k + i < p.depth) e[i] = row[k + i];
+        __builtin_memcpy(&x, e, 32);
+        return x;
+    };
+    auto multiply = [&](const Pair& a, const Pair (&b)[TR]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < TR; ++i) Mma<T>::add(a.v[h], b[i].v[h], acc[i]);
+    };
+    const int steps = p.depth / STEP;  // whole ones
+    int s = wave;
+    for (; s + (AHEAD - 1) * WAVES < steps; s += AHEAD * WAVES) {
+        Pair a[AHEAD], b[AHEAD][TR];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) a[u] = whole(c, (s + u * WAVES) * STEP + q * 2 * E);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < TR; ++i) b[u][i] = whole(r[i], (s + u * WAVES) * STEP + q * 2 * E);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) multiply(a[u], b[u]);
+    }
+    for (; s < steps; s += WAVES) {
+        Pair b[TR];
+        const Pair a = whole(c, s * STEP + q * 2 * E);
+#pragma unroll
+        for (int i = 0; i < TR; ++i) b[i] = whole(r[i], s * STEP + q * 2 * E);
+        multiply(a, b);
+    }
+    if (s == steps && steps * STEP < p.depth) {
+        Pair b[TR];
+        const Pair a = some(c, s * STEP + q * 2 * E);
+#pragma unroll
+        for (int i = 0; i < TR; ++i) b[i] = some(r[i], s * STEP + q * 2 * E);
+        multiply(a, b);
+    }
+#pragma unroll
+    for (int i = 0; i < TR; ++i) meet[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= TR) return;
+    // lane (q, l) has row l, columns 4q .. 4q + 3 of the tile
+    floatx4 sum = meet[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += meet[w][wave][lane];
+    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    const int row = r0 + 16 * wave + l, col = c0 + 4 * q;
+    finish<T>(p.epi, matrix, 0, row, col, row < rows.end ? p.cols - col : 0, v);
+}
+
+template <class T>
+void start_few(const Product& p, int row_tiles, hipStream_t s)
+{
+    const dim3 grid(p.tiles_r * p.tiles_c);
+    // K in eighths: 16 columns of 4096 values are then eight steps of each wavefront
+    if (row_tiles == 1)
+        hipLaunchKernelGGL((linear_few_kernel<T, 1, 8>), grid, dim3(512), 0, s, p);
+    else if (row_tiles == 2)
+        hipLaunchKernelGGL((linear_few_kernel<T, 2, 8>), grid, dim3(512), 0, s, p);
+    else
+        hipLaunchKernelGGL((linear_few_kernel<T, 4, 8>), grid, dim3(512), 0, s, p);
+}
+
+}  // namespace
+
+void launch_linear_few(const Product& p, int dtype, int row_tiles, hipStream_t s)
+{
+    if (dtype == PS_F32)
+        start_few<float>(p, row_tiles, s);
+    else if (dtype == PS_BF16)
+        start_few<bf16_t>(p, row_tiles, s);
+    else
+        start_few<f16_t>(p, row_tiles, s);
+}
+
+}  // namespace ps

@@ -5,8 +5,12 @@ raises an exception."""
 from __future__ import annotations
 
 import ctypes
+import struct
+import threading
 from dataclasses import dataclass, field
 from typing import List, Optional, Sequence, Tuple
+
+import torch
 
 from .binding import PS_EINVAL, PS_OK, PsError, load_library
 
@@ -48,11 +52,10 @@ def _library() -> ctypes.CDLL:
     if _lib is None:
         lib = load_library()
         vp, i32, u64, p = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.POINTER
-        mats = [p(ps_matrix)]
         for name, args in {
-                "ps_linear_workspace_bytes": [p(ps_linear), i32, p(u64)],
-                "ps_linear_forward": [p(ps_linear)] + 6 * mats + [vp, u64, vp],
-                "ps_linear_backward": [p(ps_linear)] + 7 * mats + [vp, u64, vp],
+                "ps_linear_workspace_bytes": [vp, i32, vp],
+                "ps_linear_forward": 8 * [vp] + [u64, vp],
+                "ps_linear_backward": 9 * [vp] + [u64, vp],
                 "ps_adamw_workspace_bytes": [p(ps_adamw_tensor), i32, p(u64)],
                 "ps_adamw_create": [p(vp), p(ps_adamw_tensor), i32, vp, u64, vp],
                 "ps_adamw_destroy": [vp],
@@ -73,88 +76,118 @@ def _refuse(call: str, why: str) -> None:
     raise PsError(call, PS_EINVAL, f"{call}: {why}")
 
 
+_DTYPES = {torch.float32: PS_F32, torch.bfloat16: PS_BF16, torch.float16: PS_F16}
+
+
 def _dtype(call: str, name: str, t) -> int:
-    import torch
-    code = {torch.float32: PS_F32, torch.bfloat16: PS_BF16, torch.float16: PS_F16}.get(t.dtype)
+    code = _DTYPES.get(t.dtype)
     if code is None:
         _refuse(call, f"{name} is {t.dtype}, not float32, bfloat16 or float16")
     return code
 
 
-def _matrix(call: str, name: str, t, like, shape: Tuple[int, ...], matrices: bool = False) -> Optional[ps_matrix]:
-    """Checks that `t` has this shape and like's type and device; its pointer and strides."""
-    if t is None:
-        return None
-    if t.device != like.device or not t.is_cuda:
-        _refuse(call, f"{name} is on {t.device}, not on {like.device if like.is_cuda else 'a GPU'}")
-    if t.dtype != like.dtype:
-        _refuse(call, f"{name} is {t.dtype}, not {like.dtype}")
-    if tuple(t.shape) != shape:
+def _matrix(call: str, name: str, t, device, dtype, shape: Tuple[int, ...], matrices: bool = False) -> Tuple[int, int, int]:
+    """Checks that `t` has this shape, type and device; the fields of its ps_matrix."""
+    if t.dtype is not dtype or t.device != device:
+        _refuse(call, f"{name} is {t.dtype} on {t.device}, not {dtype} on {device}")
+    if t.shape != shape:
         _refuse(call, f"{name} has the shape {tuple(t.shape)}, not {shape}")
-    if shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+    stride = t.stride()
+    cols = shape[-1]
+    if cols > 1 and stride[-1] != 1 and t.numel():
         _refuse(call, f"{name}'s rows are not contiguous")
-    rows = shape[-2] if len(shape) - (1 if matrices else 0) > 1 else 1
-    row = t.stride(-2) if rows > 1 else shape[-1]
-    return ps_matrix(t.data_ptr(), row, t.stride(0) if matrices and shape[0] > 1 else rows * row)
+    if matrices:
+        rows = shape[1] if len(shape) == 3 else 1
+        row = stride[1] if rows > 1 else cols
+        return t.data_ptr(), row, stride[0] if shape[0] > 1 else rows * row
+    return t.data_ptr(), stride[0] if len(shape) == 2 and shape[0] > 1 else cols, 0
 
 
-def _ints(call: str, name: str, t, like, n: Optional[int] = None):
-    import torch
+def _ints(call: str, name: str, t, device, n: Optional[int] = None) -> int:
     if t is None:
-        return None
-    if t.dtype != torch.int32 or t.device != like.device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        return 0
+    if t.dtype is not torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
         _refuse(call, f"{name} is a contiguous int32 tensor" + (f" of {n} elements" if n is not None else "") + " next to the others")
     return t.data_ptr()
 
 
-def _layer(call: str, x, w, activation: str, offsets, weight_of_group):
+# The arguments of a call, written in one go: a ps_linear and one ps_matrix for each operand (ctypes structures, made one by one, take
+# most of the time of a small layer).
+_LAYER, _MATRIX = "<iiqqqiiQQ", "Qqq"
+_LAYER_BYTES, _MATRIX_BYTES = struct.calcsize(_LAYER), struct.calcsize("<" + _MATRIX)
+assert _LAYER_BYTES == ctypes.sizeof(ps_linear) and _MATRIX_BYTES == ctypes.sizeof(ps_matrix)
+_PACK = {n: struct.Struct(_LAYER + n * _MATRIX).pack_into for n in (6, 7)}
+_ABSENT = (0, 0, 0)
+
+
+class _Arguments(threading.local):
+    def __init__(self):
+        self.memory = ctypes.create_string_buffer(_LAYER_BYTES + 7 * _MATRIX_BYTES)
+        self.need = ctypes.c_uint64(0)
+        self.at = ctypes.addressof(self.memory)
+        self.at_need = ctypes.addressof(self.need)
+
+
+_arguments = _Arguments()
+
+
+def _layer(call: str, x, w, activation: str, offsets, weight_of_group) -> Tuple[int, ...]:
+    """The fields of the call's ps_linear."""
     grouped = offsets is not None
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         _refuse(call, f"unknown activation {activation!r}")
     if x.dim() != 2 or w.dim() != (3 if grouped else 2):
         _refuse(call, "x is [rows, in] and w " + ("[matrices, out, in]" if grouped else "[out, in]"))
-    _ints(call, "offsets", offsets, x)
-    n_groups = offsets.numel() - 1 if grouped else 1
+    dtype, device = _dtype(call, "x", x), x.device
+    if device.type != "cuda":
+        _refuse(call, f"x is on {device}, not on a GPU")
+    rows, fin = x.shape
+    if not grouped:
+        return dtype, act, rows, fin, w.shape[0], 1, 1, 0, 0
+    at = _ints(call, "offsets", offsets, device)
+    n_groups = offsets.numel() - 1
     if n_groups < 1:
         _refuse(call, "offsets has one element more than there are groups, of which there is at least one")
-    index = _ints(call, "weight_of_group", weight_of_group, x, n_groups)
-    return ps_linear(_dtype(call, "x", x), ACTIVATIONS[activation], x.shape[0], x.shape[1], w.shape[-2], n_groups, w.shape[0] if grouped else 1,
-                     offsets.data_ptr() if grouped else None, index)
+    return dtype, act, rows, fin, w.shape[1], n_groups, w.shape[0], at, _ints(call, "weight_of_group", weight_of_group, device, n_groups)
 
 
-def _ref(m: Optional[ps_matrix]):
-    return None if m is None else ctypes.byref(m)
-
-
-def _workspace(call: str, layer: ps_linear, backward: bool, device):
-    import torch
-    n = ctypes.c_uint64(0)
-    _check(call, _library().ps_linear_workspace_bytes(ctypes.byref(layer), 1 if backward else 0, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
-
-
-def _call(call: str, layer: ps_linear, backward: bool, device, matrices) -> None:
-    import torch
-    if not device.type == "cuda":
-        _refuse(call, "tensors are on the GPU")
-    with torch.cuda.device(device):
-        ws = _workspace(call, layer, backward, device)
-        stream = torch.cuda.current_stream(device).cuda_stream
-        _check(call, getattr(_library(), call)(ctypes.byref(layer), *[_ref(m) for m in matrices], None if ws is None else ctypes.c_void_p(ws.data_ptr()),
-                                               0 if ws is None else ws.numel(), ctypes.c_void_p(stream)))
+def _run(call: str, layer: Tuple[int, ...], backward: int, device, matrices) -> None:
+    """Calls the library with what `_layer` and `_matrix` (or None) gave."""
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run(call, layer, backward, device, matrices)
+    lib, a, n = _library(), _arguments, len(matrices)
+    fields = list(layer)
+    for m in matrices:
+        fields += m or _ABSENT
+    _PACK[n](a.memory, 0, *fields)
+    st = lib.ps_linear_workspace_bytes(a.at, backward, a.at_need)
+    if st != PS_OK:
+        _check(call, st)
+    need = a.need.value
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    first = a.at + _LAYER_BYTES
+    refs = [None if m is None else first + i * _MATRIX_BYTES for i, m in enumerate(matrices)]
+    st = (lib.ps_linear_backward if backward else lib.ps_linear_forward)(a.at, *refs, None if ws is None else ws.data_ptr(), need,
+                                                                         torch._C._cuda_getCurrentRawStream(index))
+    if st != PS_OK:
+        _check(call, st)
 
 
 def _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out):
-    import torch
     call = "ps_linear_forward"
-    grouped = offsets is not None
     layer = _layer(call, x, w, activation, offsets, weight_of_group)
-    rows, fin, fout, mats = x.shape[0], x.shape[1], w.shape[-2], (w.shape[0],) if grouped else ()
-    mx, mw = _matrix(call, "x", x, x, (rows, fin)), _matrix(call, "w", w, x, mats + (fout, fin), grouped)
-    mb = _matrix(call, "bias", bias, x, mats + (fout,), grouped)
-    mr, mp = _matrix(call, "residual", residual, x, (rows, fout)), _matrix(call, "pre", pre, x, (rows, fout))
-    y = torch.empty(rows, fout, dtype=x.dtype, device=x.device) if out is None else out
-    _call(call, layer, False, x.device, [mx, mw, mb, mr, _matrix(call, "out", y, x, (rows, fout)), mp])
+    grouped, device, dtype, rows, fin, fout = offsets is not None, x.device, x.dtype, layer[2], layer[3], layer[4]
+    mats = (w.shape[0],) if grouped else ()
+    of_out = (rows, fout)
+    y = torch.empty(of_out, dtype=dtype, device=device) if out is None else out
+    _run(call, layer, 0, device, [
+        _matrix(call, "x", x, device, dtype, (rows, fin)), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
+        None if bias is None else _matrix(call, "bias", bias, device, dtype, mats + (fout,), grouped),
+        None if residual is None else _matrix(call, "residual", residual, device, dtype, of_out), _matrix(call, "out", y, device, dtype, of_out),
+        None if pre is None else _matrix(call, "pre", pre, device, dtype, of_out)])
     return y
 
 
@@ -171,40 +204,37 @@ def ps_grouped_linear_forward(x, offsets, w, bias=None, residual=None, activatio
     return _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out)
 
 
-def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need, outs):
-    import torch
+def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db):
     call = "ps_linear_backward"
-    grouped = offsets is not None
     layer = _layer(call, x, w, activation, offsets, weight_of_group)
-    rows, fin, fout = x.shape[0], x.shape[1], w.shape[-2]
-    shapes = {"dx": (rows, fin), "dw": (fout, fin), "db": (fout,)}
-    if grouped:
-        shapes["dw"], shapes["db"] = (layer.n_groups, fout, fin), (layer.n_groups, fout)
-    mats = [_matrix(call, "dy", dy, x, (rows, fout)), _matrix(call, "x", x, x, (rows, fin)),
-            _matrix(call, "w", w, x, ((w.shape[0],) if grouped else ()) + (fout, fin), grouped), _matrix(call, "pre", pre, x, (rows, fout))]
-    got = []
-    for name, shape in shapes.items():
-        t = outs[name]
-        if t is None and need[name]:
-            t = torch.empty(shape, dtype=x.dtype, device=x.device)
-        got.append(t)
-        mats.append(_matrix(call, name, t, x, shape, grouped and name != "dx"))
-    _call(call, layer, True, x.device, mats)
-    return tuple(got)
+    grouped, device, dtype, rows, fin, fout, groups = offsets is not None, x.device, x.dtype, layer[2], layer[3], layer[4], layer[5]
+    mats, of = ((w.shape[0],), (groups,)) if grouped else ((), ())
+    of_in, of_out, of_w, of_b = (rows, fin), (rows, fout), of + (fout, fin), of + (fout,)
+    if dx is None and need_dx:
+        dx = torch.empty(of_in, dtype=dtype, device=device)
+    if dw is None and need_dw:
+        dw = torch.empty(of_w, dtype=dtype, device=device)
+    if db is None and need_db:
+        db = torch.empty(of_b, dtype=dtype, device=device)
+    _run(call, layer, 1, device, [
+        _matrix(call, "dy", dy, device, dtype, of_out), _matrix(call, "x", x, device, dtype, of_in), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
+        None if pre is None else _matrix(call, "pre", pre, device, dtype, of_out), None if dx is None else _matrix(call, "dx", dx, device, dtype, of_in),
+        None if dw is None else _matrix(call, "dw", dw, device, dtype, of_w, grouped), None if db is None else _matrix(call, "db", db, device, dtype, of_b, grouped)])
+    return dx, dw, db
 
 
 def ps_linear_backward(dy, x, w, activation: str = "none", pre=None, need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
                        dx=None, dw=None, db=None):
     """Gradients (dx, dw, db) of ps_linear_forward for dy [rows, out]; pre as the forward pass wrote it, not needed without
     an activation.  What is not needed is None; dx, dw and db may be given tensors.  The residual's gradient is dy."""
-    return _backward(dy, x, None, w, activation, pre, None, dict(dx=need_dx, dw=need_dw, db=need_db), dict(dx=dx, dw=dw, db=db))
+    return _backward(dy, x, None, w, activation, pre, None, need_dx, need_dw, need_db, dx, dw, db)
 
 
 def ps_grouped_linear_backward(dy, x, offsets, w, activation: str = "none", pre=None, weight_of_group=None, need_dx: bool = True,
                                need_dw: bool = True, need_db: bool = True, dx=None, dw=None, db=None):
     """The same for rows in groups: dw [groups, out, in] and db [groups, out] are every group's own (of a worker, say, whatever
     matrix it used), zeros for a group without rows.  dw and db may be views into wider rows, for instance of a gradient buffer."""
-    return _backward(dy, x, offsets, w, activation, pre, weight_of_group, dict(dx=need_dx, dw=need_dw, db=need_db), dict(dx=dx, dw=dw, db=db))
+    return _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db)
 
 
 @dataclass
@@ -221,6 +251,8 @@ class AdamW:
     v_scale: List[object]
     copies: List[object]
     workspace: object = None
+    rows: int = 1                    # gradient rows that every tensor has
+    options: ps_adamw_options = field(default_factory=ps_adamw_options)
     closed: bool = field(default=False)
 
     def __del__(self):
@@ -237,7 +269,6 @@ def ps_adamw_create(params: Sequence, grads: Sequence, state_bits: int = 32, wei
     number, or one for each tensor.  copies[i] (or None) receives the new weights in its own type.  The states are made as zeros
     unless given: float32 of the parameter's size, or with 8 bits uint8 or float8_e4m3fn codes and float32 scales, one for
     256 elements.  Waits for the table's copy to the GPU."""
-    import torch
     call = "ps_adamw_create"
     params, grads = list(params), list(grads)
     n = len(params)
@@ -290,26 +321,29 @@ def ps_adamw_create(params: Sequence, grads: Sequence, state_bits: int = 32, wei
         ws = torch.empty(size.value, dtype=torch.uint8, device=device)
         _check(call, lib.ps_adamw_create(ctypes.byref(handle), table, n, ctypes.c_void_p(ws.data_ptr()), size.value,
                                          ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
-    return AdamW(handle, device, state_bits, params, grads, states["m"], states["v"], states["m_scale"], states["v_scale"], copies, ws)
+    return AdamW(handle, device, state_bits, params, grads, states["m"], states["v"], states["m_scale"], states["v_scale"], copies, ws,
+                 min(t.grad_rows for t in table))
 
 
 def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
                   n_rows: Optional[int] = None) -> None:
     """Step number `step` (from 1) with the sum of the first n_rows gradient rows (all that every tensor has, if not given)."""
-    import torch
     call = "ps_adamw_step"
     if opt.closed:
         _refuse(call, "the table was destroyed")
-    if n_rows is None:
-        n_rows = min(g.shape[0] if tuple(g.shape) != tuple(p.shape) else 1 for p, g in zip(opt.params, opt.grads))
-    o = ps_adamw_options(lr, beta1, beta2, eps, grad_scale, step, n_rows)
-    with torch.cuda.device(opt.device):
-        _check(call, _library().ps_adamw_step(opt.handle, ctypes.byref(o), ctypes.c_void_p(torch.cuda.current_stream(opt.device).cuda_stream)))
+    index = opt.device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return ps_adamw_step(opt, step, lr, beta1, beta2, eps, grad_scale, n_rows)
+    o = opt.options
+    o.lr, o.beta1, o.beta2, o.eps, o.grad_scale, o.step, o.n_rows = lr, beta1, beta2, eps, grad_scale, step, opt.rows if n_rows is None else n_rows
+    st = _library().ps_adamw_step(opt.handle, ctypes.byref(o), torch._C._cuda_getCurrentRawStream(index))
+    if st != PS_OK:
+        _check(call, st)
 
 
 def ps_adamw_state(opt: AdamW, i: int):
     """Both moments of tensor i, as float32 values."""
-    import torch
     if opt.state_bits == 32:
         return opt.m[i], opt.v[i]
     def values(codes, scale):
