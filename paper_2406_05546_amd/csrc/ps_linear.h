@@ -11,15 +11,14 @@
 // gets consecutive columns of one row of the result.
 #pragma once
 #include "ps_dense.h"
+#include "ps_split.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ps {
 
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int LINEAR_XCDS = 8, COMPUTE_UNITS = 256;
@@ -530,9 +529,10 @@ __device__ __forceinline__ void block_barrier_after_reads()
 }
 
 template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DIRECT, int RAGGED>
-__global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_kernel(Product p)
+__global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 {
     constexpr int NT = 64 * WR * WC, TR = BR / WR / 16, TC = BC / WC / 16;
+    constexpr bool SPLIT = sizeof(T) == 4;
     constexpr int HALVES = DIRECT && TR >= 4 && TC >= 4 ? 2 : 1, HR = TR / HALVES, HC = TC / HALVES;
     using OpR = Operand<T, R_KC, false, BR, WR, HALVES, NT, DIRECT>;
     using OpC = Operand<T, C_KC, true, BC, WC, HALVES, NT, DIRECT>;
@@ -550,17 +550,23 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_ker
     if (!find_tile<BR, BC, BK, RAGGED>(p, tiles_r, blockIdx.x, tile)) return;
     OpR opr;
     OpC opc;
-    opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)tile.r0 * p.r_row + tile.k_first : (int64_t)tile.k_first * p.r_row + tile.r0), p.r_row, tile.r_valid,
-                 tile.depth, tid);
-    opc.init(static_cast<const T*>(p.c) + tile.matrix * p.c_matrix + (C_KC ? (int64_t)tile.c0 * p.c_row + tile.k_first : (int64_t)tile.k_first * p.c_row + tile.c0),
-                 p.c_row, tile.c_valid, tile.depth, tid);
+    auto begin = [&]() __attribute__((always_inline)) {
+        opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)tile.r0 * p.r_row + tile.k_first : (int64_t)tile.k_first * p.r_row + tile.r0), p.r_row, tile.r_valid,
+                     tile.depth, tid);
+        opc.init(static_cast<const T*>(p.c) + tile.matrix * p.c_matrix + (C_KC ? (int64_t)tile.c0 * p.c_row + tile.k_first : (int64_t)tile.k_first * p.c_row + tile.c0),
+                     p.c_row, tile.c_valid, tile.depth, tid);
+    };
+    begin();
 
     floatx4 acc[TR][TC];
-#pragma unroll
-    for (int i = 0; i < TR; ++i)
-#pragma unroll
-        for (int j = 0; j < TC; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto clear = [](auto& sums) __attribute__((always_inline)) {
+        for (auto& row : sums)
+            for (auto& sum : row) sum = floatx4{0.f, 0.f, 0.f, 0.f};
+    };
+    clear(acc);
     const int stages = (tile.depth + BK - 1) / BK;
+    // fp32: the small terms of the split products, and whether the sums are to be formed without the split
+    floatx4 small[SPLIT ? TR : 1][SPLIT ? TC : 1];
     uintx4 fr[HALVES][HR][SUBS], fc[HALVES][HC][SUBS];
     // LDS addresses of the halves in the first buffer
     const int to_r[2] = {lds_address(lds), lds_address(lds) + OpR::HBYTES}, to_c[2] = {to_r[0] + OpR::BYTES, to_r[0] + OpR::BYTES + OpC::HBYTES};
@@ -580,7 +586,115 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC >= 8 ? 2 : 1) void linear_ker
 #pragma unroll
             for (int j = 0; j < HC; ++j) Mma<T>::add(fc[set][j][sub], fr[hr][i][sub], acc[hr * HR + i][hc * HC + j]);
     };
-    if constexpr (HALVES == 2) {
+    if constexpr (SPLIT) {
+        // fp32 products on the bf16 matrix instructions, operands split in three (ps_split.h), which are read as they are and split
+        // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Bound by the vector
+        // ALU that splits: 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
+        // instructions for each of the products that they enter.  A block whose sums the split may not hold (ps_split.h: not finite, or
+        // not zero and below 2^-80) forms them all again with fp32 matrix instructions.
+        auto pass = [&](auto form) __attribute__((always_inline)) {
+            constexpr bool exact = decltype(form)::value;
+            auto products = [&](const char* r, const char* c) __attribute__((always_inline)) {
+                if constexpr (exact) {
+#pragma unroll
+                    for (int sub = 0; sub < SUBS; ++sub) {
+#pragma unroll
+                        for (int h = 0; h < HALVES; ++h) {
+                            fetch_c(c + h * OpC::HBYTES, sub, h);
+                            fetch_r(h, r + h * OpR::HBYTES, sub);
+                        }
+#pragma unroll
+                        for (int h = 0; h < HALVES * HALVES; ++h) multiply(h / HALVES, h % HALVES, sub, h % HALVES);
+                    }
+                } else {
+                    auto parts = [](const uintx4& x, const uintx4& y) __attribute__((always_inline)) {
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? x[e] : y[e - 4]);
+                        return split8(v);
+                    };
+                    auto of_c = [&](int j, int sub) __attribute__((always_inline)) { return OpC::fetch(c + j / HC * OpC::HBYTES, wc, j % HC, sub, lane); };
+                    auto of_r = [&](int i, int sub) __attribute__((always_inline)) { return OpR::fetch(r + i / HR * OpR::HBYTES, wr, i % HR, sub, lane); };
+                    Split8 sc[TC];
+#pragma unroll
+                    for (int j = 0; j < TC; ++j) sc[j] = parts(of_c(j, 0), of_c(j, 1));
+                    uintx4 x[2] = {of_r(0, 0), of_r(0, 1)};
+#pragma unroll
+                    for (int i = 0; i < TR; ++i) {
+                        const Split8 sr = parts(x[0], x[1]);
+                        if (i + 1 < TR) {
+                            x[0] = of_r(i + 1, 0);
+                            x[1] = of_r(i + 1, 1);
+                        }
+#pragma unroll
+                        for (int t = 0; t <= SPLIT_SMALL; ++t)
+#pragma unroll
+                            for (int j = 0; j < TC; ++j) {
+                                floatx4& to = t < SPLIT_SMALL ? small[i][j] : acc[i][j];
+                                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sc[j].part(TERM_A[t]), sr.part(TERM_B[t]), to, 0, 0, 0);
+                            }
+                        __builtin_amdgcn_sched_barrier(0);  // or all rows are fetched and split ahead, and registers run out
+                    }
+                }
+            };
+            if constexpr (DIRECT) {
+                constexpr int LOADS = HALVES * (OpR::LOADS + OpC::LOADS);
+                auto bring = [&](int buffer) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) {
+                        bring_r(h, buffer);
+                        bring_c(h, buffer);
+                    }
+                    opr.next_stage(tid);
+                    opc.next_stage(tid);
+                };
+                bring(0);
+                bring(1);
+#pragma unroll 1
+                for (int s = 0; s < stages; ++s) {
+                    int from = (s & 1) * BUFFER;  // unknown to the compiler, which would keep addresses for either buffer in registers
+                    asm volatile("" : "+s"(from));
+                    __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
+                    block_barrier();
+                    products(r00 + from, c00 + from);
+                    block_barrier_after_reads();
+                    bring(s & 1);
+                }
+                __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+            } else {
+                for (int s = 0; s < stages; ++s) {
+                    char *const r = s & 1 ? r10 : r00, *const c = s & 1 ? c10 : c00;
+                    opr.load(tid);
+                    opc.load(tid);
+                    opr.put(r, tid);
+                    opc.put(c, tid);
+                    opr.next_stage(tid);
+                    opc.next_stage(tid);
+                    __syncthreads();
+                    products(r, c);
+                }
+            }
+        };
+        clear(small);
+        pass(std::false_type{});
+        bool lost = false;
+#pragma unroll
+        for (int i = 0; i < TR; ++i)
+#pragma unroll
+            for (int j = 0; j < TC; ++j) {
+                acc[i][j] += small[i][j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float m = fabsf(acc[i][j][e]);
+                    lost |= !(m < INFINITY) || (m < SPLIT_TINY && m > 0.f);
+                }
+            }
+        if (__syncthreads_or(lost)) {
+            begin();
+            clear(acc);
+            pass(std::true_type{});
+        }
+    } else if constexpr (HALVES == 2) {
         // A stage in four phases, a quarter of the products each, in an order in which each phase needs one more half of an
         // operand: it is read from LDS in the phase before.
         //     products   R0 C0   R0 C1   R1 C1   R1 C0

@@ -35,7 +35,7 @@ struct SlopeArgs {
 
 // A block takes 512 columns (a lane eight consecutive ones) of one part of a group's rows, its four wavefronts every
 // fourth row each; their sums meet in LDS in order.
-constexpr int SLOPE_COLS = 512;
+constexpr int SLOPE_COLS = 512, SLOPE_AHEAD = 4;  // rows of a wavefront on their way at once
 
 template <class T>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
@@ -48,32 +48,47 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     const int begin = min(rows.begin + part * each, rows.end), end = min(begin + each, rows.end);
     const int col = blockIdx.x * SLOPE_COLS + lane * 8, n = min(8, a.cols - col);
     float sum[8] = {};
-    if (n > 0) {
-        for (int64_t r = begin + wave; r < end; r += 4) {
-            float d[8], z[8];
-            const T* dy = static_cast<const T*>(a.dy) + r * a.dy_row + col;
+    auto take = [&](int64_t r, float (&d)[8], float (&z)[8]) __attribute__((always_inline)) {
+        const T* dy = static_cast<const T*>(a.dy) + r * a.dy_row + col;
+        if (n == 8)
+            load_n(dy, d);
+        else
+            load_some(dy, n, d);
+        if (!a.pre) return;
+        const T* pre = static_cast<const T*>(a.pre) + r * a.pre_row + col;
+        if (n == 8)
+            load_n(pre, z);
+        else
+            load_some(pre, n, z);
+    };
+    auto give = [&](int64_t r, float (&d)[8], const float (&z)[8]) __attribute__((always_inline)) {
+        if (a.pre) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] *= activation_slope(z[i], a.act);
+        }
+        if (a.dz) {
+            T* dz = static_cast<T*>(a.dz) + r * a.dz_row + col;
             if (n == 8)
-                load_n(dy, d);
+                store_n(dz, d);
             else
-                load_some(dy, n, d);
-            if (a.pre) {
-                const T* pre = static_cast<const T*>(a.pre) + r * a.pre_row + col;
-                if (n == 8)
-                    load_n(pre, z);
-                else
-                    load_some(pre, n, z);
+                store_some(dz, n, d);
+        }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= activation_slope(z[i], a.act);
-            }
-            if (a.dz) {
-                T* dz = static_cast<T*>(a.dz) + r * a.dz_row + col;
-                if (n == 8)
-                    store_n(dz, d);
-                else
-                    store_some(dz, n, d);
-            }
+        for (int i = 0; i < 8; ++i) sum[i] += d[i];
+    };
+    if (n > 0) {
+        int64_t r = begin + wave;
+        for (; r + 4 * (SLOPE_AHEAD - 1) < end; r += 4 * SLOPE_AHEAD) {
+            float d[SLOPE_AHEAD][8], z[SLOPE_AHEAD][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += d[i];
+            for (int u = 0; u < SLOPE_AHEAD; ++u) take(r + 4 * u, d[u], z[u]);
+#pragma unroll
+            for (int u = 0; u < SLOPE_AHEAD; ++u) give(r + 4 * u, d[u], z[u]);
+        }
+        for (; r < end; r += 4) {
+            float d[8], z[8];
+            take(r, d, z);
+            give(r, d, z);
         }
     }
     if (!a.partial) return;
@@ -95,13 +110,25 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     }
 }
 
+// Adds up the parts: a block takes 32 columns, each sixteenth of its threads a sixteenth of the parts, whose sums meet in order.
+constexpr int BIAS_COLS = 32, BIAS_SHARES = 16;
 template <class T>
-__global__ __launch_bounds__(256) void bias_sum_kernel(const float* __restrict__ partial, T* __restrict__ db, int64_t db_matrix, int cols, int parts)
+__global__ __launch_bounds__(BIAS_COLS * BIAS_SHARES) void bias_sum_kernel(const float* __restrict__ partial, T* __restrict__ db, int64_t db_matrix, int cols, int parts)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
-    if (c >= cols) return;
+    __shared__ float meet[BIAS_SHARES][BIAS_COLS];
+    const int i = threadIdx.x % BIAS_COLS, share = threadIdx.x / BIAS_COLS, g = blockIdx.x / ((cols + BIAS_COLS - 1) / BIAS_COLS);
+    const int c = (blockIdx.x - g * ((cols + BIAS_COLS - 1) / BIAS_COLS)) * BIAS_COLS + i;
+    const int each = (parts + BIAS_SHARES - 1) / BIAS_SHARES, first = share * each, last = min(first + each, parts);
     float s = 0.f;
-    for (int k = 0; k < parts; ++k) s += partial[((int64_t)g * parts + k) * cols + c];
+    if (c < cols) {
+#pragma unroll 4
+        for (int k = first; k < last; ++k) s += partial[((int64_t)g * parts + k) * cols + c];
+    }
+    meet[share][i] = s;
+    __syncthreads();
+    if (share || c >= cols) return;
+#pragma unroll
+    for (int k = 1; k < BIAS_SHARES; ++k) s += meet[k][i];
     db[g * db_matrix + c] = from_float<T>(s);
 }
 
@@ -182,7 +209,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
 int slope_parts(const ps_linear& l)
 {
     const int64_t blocks = up(l.out_features, SLOPE_COLS) * l.n_groups;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(up(8 * COMPUTE_UNITS, blocks), up(up(l.rows, l.n_groups), 16)), 65535 / std::min<int64_t>(l.n_groups, 65535)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(up(4 * COMPUTE_UNITS, blocks), up(up(l.rows, l.n_groups), 16)), 65535 / std::min<int64_t>(l.n_groups, 65535)));
 }
 
 struct BackwardSpace {
@@ -403,7 +430,7 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
             using T = decltype(t);
             hipLaunchKernelGGL(slope_kernel<T>, dim3((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many), dim3(256), 0, s, a);
             if (want_db)
-                hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)up(l->out_features, 256), l->n_groups), dim3(256), 0, s, a.partial,
+                hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)(up(l->out_features, BIAS_COLS) * l->n_groups)), dim3(BIAS_COLS * BIAS_SHARES), 0, s, a.partial,
                                    static_cast<T*>(db->data_dev), db->matrix, (int)l->out_features, space.parts);
         });
     }
