@@ -545,7 +545,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 
     const int tiles_r = RAGGED == RAGGED_R ? count_tiles(p.groups, BR, p.tiles_r) : p.tiles_r;
     const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
-    const int wr = wave % WR, wc = wave / WR;
+    const int wr = wave / WC, wc = wave % WC;  // of eight wavefronts, two that share a SIMD have different rows
     Tile tile;
     if (!find_tile<BR, BC, BK, RAGGED>(p, tiles_r, blockIdx.x, tile)) return;
     OpR opr;
@@ -770,9 +770,24 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             fetch_r(0, r00, sub);
         }
         block_barrier_after_reads();
-        for (int s = 0; s < stages; s += 2) {
-            stage(0, 0);
-            if (s + 1 < stages) stage(1, 1);
+        // In a tile that is not whole, a wavefront without rows or columns of the result brings its share and no more.
+        if (wr * (BR / WR) < tile.r_valid && wc * (BC / WC) < tile.c_valid) {
+            for (int s = 0; s < stages; s += 2) {
+                stage(0, 0);
+                if (s + 1 < stages) stage(1, 1);
+            }
+        } else {
+#pragma unroll 1
+            for (int s = 0; s < stages; ++s) {
+                bring_r(0, s & 1);
+                bring_c(0, s & 1);
+                arrived();
+                bring_c(1, s & 1);
+                bring_r(1, s & 1);
+                opr.next_stage(tid);
+                opc.next_stage(tid);
+                arrived();
+            }
         }
         __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
     } else if constexpr (DIRECT) {

@@ -181,26 +181,40 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         if (best.tiles_r * best.tiles_c <= INT32_MAX) return best;
         best = Plan{};
     }
-    for (int tile = l.dtype == PS_F32 || !direct ? 1 : 2; tile >= 0; --tile) {
-        const int size = LINEAR_TILE[tile];
+    // The form that should take least, by what its blocks take when one, or as many as there is room for, are on a compute
+    // unit.  What that chooses, in us against the other tiles (256, 128, 64; bf16 if not said): 4096^3 256: 110, 133, 194; 8192 rows
+    // 1568 -> 512 128: 53, 20, 27; 1024^3 64: 27, 20, 10; 256 rows 4096 -> 4096 128 in parts: 35, 24, 32; weight gradient of
+    // 8192 rows 1568 -> 512 128 in parts: 53, 30, 38, in fp32 128 in parts: -, 92, 146.
+    const int stages = (int)up(depth, 128 / dtype_size(l.dtype));
+    const bool wide = l.dtype == PS_F32;
+    double least = 0;
+    for (int tile = wide || !direct ? 1 : 2; tile >= 0; --tile) {
+        const int size = LINEAR_TILE[tile], room = tile == 2 ? 1 : tile == 1 ? 2 : 4;  // blocks to a compute unit
+        const double through = direct ? 1 : tile ? 2 : 1.6;  // operands through registers
+        const double alone = (wide ? (tile ? 1.6 : 0.6) : tile == 2 ? 1.6 : tile == 1 ? 0.6 : 0.35) * through;  // us a stage
+        const double full = (wide ? (tile ? 2.8 : 1.6) : tile == 2 ? 1.6 : tile == 1 ? 1.0 : 0.75) * through;
+        const double around = tile == 2 ? 7 : 3.5;  // us of a block's first loads and its stores
         Plan p{};
         p.tile = tile;
-        p.parts = 1;
         // groups that are cut up separately have at most one tile more each than all rows together
         p.tiles_r = kind == DW ? up(rows, size) * l.n_groups : up(rows, size) + (one ? 0 : l.n_groups);
         p.tiles_c = up(cols, size);
-        best = p;
-        if (p.tiles_r * p.tiles_c >= COMPUTE_UNITS) break;
-    }
-    const int stages = (int)up(depth, 128 / dtype_size(l.dtype));
-    best.part_stages = stages;
-    const int64_t tiles = best.tiles_r * best.tiles_c;
-    if (one && tiles > 0 && tiles < COMPUTE_UNITS && stages >= 8) {
-        const int parts = (int)std::min<int64_t>(std::min<int64_t>(2 * COMPUTE_UNITS / tiles, stages / 4), 32);
-        if (parts > 1) {
-            best.part_stages = (int)up(stages, parts);
-            best.parts = (int)up(stages, best.part_stages);
-            best.partial_bytes = (uint64_t)best.parts * rows * cols * 4;
+        const int64_t likely = (kind == DW ? p.tiles_r : up(rows, size) + (one ? 0 : l.n_groups / 2)) * p.tiles_c;  // half a tile more each
+        const int of_group = (int)(kind == DW ? std::max<int64_t>(1, stages / l.n_groups) : stages);
+        for (int parts = 1; parts <= 32; parts *= 2) {
+            if (parts > 1 && (!one || stages < 4 * parts || p.tiles_r * p.tiles_c * parts > 2 * room * COMPUTE_UNITS)) break;
+            p.part_stages = (int)up(stages, parts);
+            p.parts = (int)up(std::max(stages, 1), std::max(p.part_stages, 1));
+            p.partial_bytes = parts > 1 ? (uint64_t)p.parts * rows * cols * 4 : 0;
+            const int64_t blocks = likely * p.parts, rounds = up(blocks, (int64_t)room * COMPUTE_UNITS);
+            const double on_a_unit = std::min<double>(room, (double)up(blocks, COMPUTE_UNITS));
+            const double stage = room > 1 ? alone + (full - alone) * (on_a_unit - 1) / (room - 1) : full;
+            double us = (double)rounds * (around + stage * std::min(of_group, std::max(p.part_stages, 1)));
+            if (parts > 1) us += 4 + (double)p.partial_bytes * 1.5 / 4e6;  // written, read and joined
+            if (!best.tiles_r || us < least) {
+                best = p;
+                least = us;
+            }
         }
     }
     return best;
