@@ -290,8 +290,8 @@ struct Operand {
         }
     }
 
-    // DIRECT: load i of a half of the next stage, or nothing past the last one, to the LDS address `tile` (of that half).  wave: a scalar.
-    __device__ __forceinline__ void bring(int half, int i, int tile, int wave) const
+    // DIRECT: load i of a half of the next stage, or nothing past the last one, to the LDS address `tile` (of that half, and the wavefront's first piece).
+    __device__ __forceinline__ void bring(int half, int i, int tile) const
     {
         // A load is at the same place for every thread but for what is the same for all of them, by which the descriptor's
         // base is moved.  What may be read ends, KC, with the last row; RC, with the last k.
@@ -300,15 +300,15 @@ struct Operand {
         int line, element;
         place(half, i, 0, line, element);
         const int moved = line * pitch + element * SIZE;  // of thread 0, which is at 0 in the first load of the first half
-        const uint64_t from = reinterpret_cast<uint64_t>(base + moved);
+        const uint64_t from = reinterpret_cast<uint64_t>(base) + (uint32_t)moved;
         load_to_lds(uintx4{(uint32_t)scalar((int)from), (uint32_t)scalar((int)(from >> 32)) & 0xffffu, (uint32_t)scalar(max(bytes - moved, 0)), 0x00020000u}, own_offset,
-                    tile + (i * NT + wave * 64) * 16);
+                    tile + i * NT * 16);
     }
     // All of it
-    __device__ __forceinline__ void bring(int half, int tile, int wave) const
+    __device__ __forceinline__ void bring(int half, int tile) const
     {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) bring(half, i, tile, wave);
+        for (int i = 0; i < LOADS; ++i) bring(half, i, tile);
     }
     // Through registers: the whole next stage.
     __device__ __forceinline__ void load(int t)
@@ -510,6 +510,15 @@ __device__ __forceinline__ bool find_tile(const Product& p, int tiles_r, int blo
     return true;
 }
 
+// The kernel's argument, read where it is used: the compiler would keep all of it in scalar registers, and have too few.
+__device__ __forceinline__ const Product& argument()
+{
+    typedef const __attribute__((address_space(4))) Product* Constant;
+    Constant p = (Constant)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Product*)p;
+}
+
 // s_waitcnt's argument: all but `n` of the wavefront's loads are done; everything of it is done.
 constexpr int wait_vm(int n) { return (n & 15) | (n >> 4) << 14 | 0xf70; }
 constexpr int WAIT_ALL = 0x0070;
@@ -551,6 +560,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
     OpR opr;
     OpC opc;
     auto begin = [&]() __attribute__((always_inline)) {
+        const Product& p = argument();
         opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)tile.r0 * p.r_row + tile.k_first : (int64_t)tile.k_first * p.r_row + tile.r0), p.r_row, tile.r_valid,
                      tile.depth, tid);
         opc.init(static_cast<const T*>(p.c) + tile.matrix * p.c_matrix + (C_KC ? (int64_t)tile.c0 * p.c_row + tile.k_first : (int64_t)tile.k_first * p.c_row + tile.c0),
@@ -568,10 +578,11 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
     // fp32: the small terms of the split products, and whether the sums are to be formed without the split
     floatx4 small[SPLIT ? TR : 1][SPLIT ? TC : 1];
     uintx4 fr[HALVES][HR][SUBS], fc[HALVES][HC][SUBS];
-    // LDS addresses of the halves in the first buffer
-    const int to_r[2] = {lds_address(lds), lds_address(lds) + OpR::HBYTES}, to_c[2] = {to_r[0] + OpR::BYTES, to_r[0] + OpR::BYTES + OpC::HBYTES};
-    auto bring_r = [&](int h, int buffer) __attribute__((always_inline)) { opr.bring(h, to_r[h] + buffer * BUFFER, wave); };
-    auto bring_c = [&](int h, int buffer) __attribute__((always_inline)) { opc.bring(h, to_c[h] + buffer * BUFFER, wave); };
+    // where the wavefront's first piece of the first half comes in LDS, and the halves from there on
+    const int to_first = lds_address(lds) + wave * 1024;
+    constexpr int to_r[2] = {0, OpR::HBYTES}, to_c[2] = {OpR::BYTES, OpR::BYTES + OpC::HBYTES};
+    auto bring_r = [&](int h, int buffer) __attribute__((always_inline)) { opr.bring(h, to_first + to_r[h] + buffer * BUFFER); };
+    auto bring_c = [&](int h, int buffer) __attribute__((always_inline)) { opc.bring(h, to_first + to_c[h] + buffer * BUFFER); };
     auto fetch_r = [&](int h, const char* from, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < HR; ++i) fr[h][i][sub] = OpR::fetch(from, wr, i, sub, lane);
@@ -738,26 +749,25 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         // c0: the registers that hold C0 (those of C1 are free for the next stage's C0 when that is read)
         auto stage = [&](int buffer, int c0) __attribute__((always_inline)) {
             // unknown to the compiler, which would keep addresses for either buffer in registers, and have too few
-            int from = buffer * BUFFER, from_next = BUFFER - from;
-            asm volatile("" : "+s"(from), "+s"(from_next));
-            const int to = buffer * BUFFER;
+            int from = buffer * BUFFER, from_next = BUFFER - from, to = to_first + from;
+            asm volatile("" : "+s"(from), "+s"(from_next), "+s"(to));
             phase(0, 0, c0, [&]() __attribute__((always_inline)) {
                 fetch_c(c01 + from, 0, c0 ^ 1);
                 fetch_c(c01 + from, 1, c0 ^ 1);
-            }, [&](int i) __attribute__((always_inline)) { opr.bring(0, i, to_r[0] + to, wave); });
+            }, [&](int i) __attribute__((always_inline)) { opr.bring(0, i, to_r[0] + to); });
             phase(0, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
                 fetch_r(1, r01 + from, 0);
                 fetch_r(1, r01 + from, 1);
-            }, [&](int i) __attribute__((always_inline)) { opc.bring(0, i, to_c[0] + to, wave); });
+            }, [&](int i) __attribute__((always_inline)) { opc.bring(0, i, to_c[0] + to); });
             arrived();
             phase(1, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
                 fetch_r(0, r00 + from_next, 0);  // behind the last stage what lay there before, which nobody uses
                 fetch_r(0, r00 + from_next, 1);
-            }, [&](int i) __attribute__((always_inline)) { opc.bring(1, i, to_c[1] + to, wave); });
+            }, [&](int i) __attribute__((always_inline)) { opc.bring(1, i, to_c[1] + to); });
             phase(1, 0, c0, [&]() __attribute__((always_inline)) {
                 fetch_c(c00 + from_next, 0, c0 ^ 1);
                 fetch_c(c00 + from_next, 1, c0 ^ 1);
-            }, [&](int i) __attribute__((always_inline)) { opr.bring(1, i, to_r[1] + to, wave); });
+            }, [&](int i) __attribute__((always_inline)) { opr.bring(1, i, to_r[1] + to); });
             opr.next_stage(tid);
             opc.next_stage(tid);
             arrived();
@@ -855,28 +865,52 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         }
     }
 
-    // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.
-    const int l = lane & 15, q = lane >> 4;
-    constexpr int N = OpC::PERMUTED ? 8 : 4;
+    // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.  The sums go through
+    // LDS, 16 rows of a wavefront at a time, so that it stores whole cache lines, and the code that finishes them, of which only
+    // one way is taken, is there once (a copy for every MFMA tile made 150 KB, and its way through the instruction cache
+    // took 5 us a tile).
+    {
+        const Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
+        const int rows = argument().rows, cols = argument().cols;
+        constexpr int PIECES = TC * 4, LANES = TC * 2, AT_ONCE = 64 / LANES;  // 16-byte pieces and lanes of a row, rows at once
+        block_barrier();                                                      // nobody reads what these take the place of
+        char* const mine = lds + wave * (16 * PIECES * 16);
+        const int l = lane & 15, q = lane >> 4;
+#pragma unroll 1
+        for (int i = 0; i < TR; ++i) {
 #pragma unroll
-    for (int i = 0; i < TR; ++i) {
-        const int r = (wr * TR + i) * 16 + l;
+            for (int k = 0; k < TR; ++k) {
+                if (k != i) continue;  // the registers of a row of tiles have to be named
 #pragma unroll
-        for (int j = 0; j < TC; j += N / 4) {
-            float v[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = acc[i][j + e / 4][e & 3];
-            const int c = wc * TC * 16 + (OpC::PERMUTED ? 16 * j + 8 * q : 16 * j + 4 * q);
-            const int valid = r < tile.r_valid ? tile.c_valid - c : 0;
-            if (p.epi.partial) {
-                float* to = p.epi.partial + ((int64_t)tile.part * p.rows + (tile.r0 + r)) * p.cols + tile.c0 + c;
-                if (valid >= N)
-                    store_n(to, v);
-                else if (valid > 0)
-                    store_some(to, valid, v);
-            } else {
-                finish<T>(p.epi, tile.matrix, RAGGED == RAGGED_K ? tile.group : 0, tile.r0 + r, tile.c0 + c, valid, v);
+                for (int j = 0; j < TC; ++j) {
+                    const int piece = OpC::PERMUTED ? 8 * (j / 2) + 2 * q + (j & 1) : 4 * j + q;
+                    *reinterpret_cast<floatx4*>(mine + l * (PIECES * 16) + ((piece ^ (l & (PIECES - 1))) << 4)) = acc[k][j];
+                }
             }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+            for (int h = 0; h < 16; h += AT_ONCE) {
+                const int row = h + lane / LANES, at = lane % LANES;  // eight columns of a row
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const floatx4 x = *reinterpret_cast<const floatx4*>(mine + row * (PIECES * 16) + (((2 * at + e) ^ (row & (PIECES - 1))) << 4));
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) v[4 * e + n] = x[n];
+                }
+                const int r = (wr * TR + i) * 16 + row, c = wc * TC * 16 + 8 * at;
+                const int valid = r < tile.r_valid ? tile.c_valid - c : 0;
+                if (epi.partial) {
+                    float* to = epi.partial + ((int64_t)tile.part * rows + (tile.r0 + r)) * cols + tile.c0 + c;
+                    if (valid >= 8)
+                        store_n(to, v);
+                    else if (valid > 0)
+                        store_some(to, valid, v);
+                } else {
+                    finish<T>(epi, tile.matrix, RAGGED == RAGGED_K ? tile.group : 0, tile.r0 + r, tile.c0 + c, valid, v);
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written
         }
     }
 }
