@@ -9,6 +9,9 @@
 // 16-bit type, 32 of fp32) through LDS; wavefronts are arranged WR x WC and multiply 16 x 16 tiles
 // (v_mfma_f32_16x16x32_bf16 / _f16, v_mfma_f32_16x16x4_f32) with C as the instruction's first operand, so that a lane
 // gets consecutive columns of one row of the result.
+//
+// Bound by the matrix cores (and the chip's power) where rows are many: bf16 8192^3 1380-1410 TFLOP/s in all three kinds, the
+// library's product of two row-major matrices 1320, of their transposed forms 1150 and 1020; by memory where they are few.
 #pragma once
 #include "ps_dense.h"
 #include "ps_split.h"
@@ -139,14 +142,15 @@ __device__ __forceinline__ NormalTail normal_tail(float z)
 }
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-__device__ __forceinline__ float activate(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
 {
-    if (act == PS_ACT_RELU) return z <= 0.f ? 0.f : z;
-    if (act == PS_ACT_GELU) {
+    if constexpr (ACT == PS_ACT_RELU) return z <= 0.f ? 0.f : z;
+    if constexpr (ACT == PS_ACT_GELU) {
         const NormalTail n = normal_tail(z);
         return z * (z < 0.f ? n.tail : 1.f - n.tail);
     }
-    if (act == PS_ACT_SILU) return z * logistic(z);
+    if constexpr (ACT == PS_ACT_SILU) return z * logistic(z);
     return z;
 }
 __device__ __forceinline__ float activation_slope(float z, int act)
@@ -398,43 +402,58 @@ struct Epilogue {
 
 #if defined(__HIPCC__)
 
-// N consecutive columns of one row, of which `valid` exist.
+// N consecutive columns of one row, of which `valid` exist: what is added to them (nothing is read where there is none),
+// and what becomes of them.
 template <class T, int N>
-__device__ __forceinline__ void finish(const Epilogue& e, int matrix, int group, int64_t row, int col, int valid, float (&v)[N])
+__device__ __forceinline__ void load_columns(const void* base, int64_t at, int valid, float (&x)[N])
+{
+    const T* p = static_cast<const T*>(base) + at;
+    if (valid >= N)
+        load_n(p, x);
+    else
+        load_some(p, valid, x);
+}
+template <class T, int N>
+__device__ __forceinline__ void load_bias(const Epilogue& e, int matrix, int col, int valid, float (&x)[N])
+{
+    if (e.bias && valid > 0) load_columns<T>(e.bias, matrix * e.bias_matrix + col, valid, x);
+}
+template <class T, int N>
+__device__ __forceinline__ void load_residual(const Epilogue& e, int64_t row, int col, int valid, float (&x)[N])
+{
+    if (e.residual && valid > 0) load_columns<T>(e.residual, row * e.residual_row + col, valid, x);
+}
+template <class T, int N>
+__device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int group, int64_t row, int col, int valid, float (&v)[N])
 {
     if (valid <= 0) return;
-    const bool whole = valid >= N;
-    auto load = [&](const void* base, int64_t at, float (&x)[N]) {
-        const T* p = static_cast<const T*>(base) + at;
-        if (whole)
-            load_n(p, x);
-        else
-            load_some(p, valid, x);
-    };
-    auto store = [&](void* base, int64_t at, const float (&x)[N]) {
+    auto store = [&](void* base, int64_t at) __attribute__((always_inline)) {
         T* p = static_cast<T*>(base) + at;
-        if (whole)
-            store_n(p, x);
+        if (valid >= N)
+            store_n(p, v);
         else
-            store_some(p, valid, x);
+            store_some(p, valid, v);
     };
-    float x[N];
     if (e.bias) {
-        load(e.bias, matrix * e.bias_matrix + col, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += x[i];
+        for (int i = 0; i < N; ++i) v[i] += bias[i];
     }
-    if (e.pre) store(e.pre, row * e.pre_row + col, v);
-    if (e.act != PS_ACT_NONE) {
+    if (e.pre) store(e.pre, row * e.pre_row + col);
+    if (e.act == PS_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = activate(v[i], e.act);
+        for (int i = 0; i < N; ++i) v[i] = activate<PS_ACT_RELU>(v[i]);
+    } else if (e.act == PS_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = activate<PS_ACT_GELU>(v[i]);
+    } else if (e.act == PS_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = activate<PS_ACT_SILU>(v[i]);
     }
     if (e.residual) {
-        load(e.residual, row * e.residual_row + col, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += x[i];
+        for (int i = 0; i < N; ++i) v[i] += residual[i];
     }
-    store(e.out, group * e.out_matrix + row * e.out_row + col, v);
+    store(e.out, group * e.out_matrix + row * e.out_row + col);
 }
 
 #endif
@@ -507,8 +526,17 @@ __device__ __forceinline__ bool find_tile(const Product& p, int tiles_r, int blo
         t.k_first += from;
         t.depth = min(t.depth - from, p.part_stages * BK);
     }
+    // the same for all lanes, which the compiler does not see behind a loop
+    for (int* v : {&t.r0, &t.r_valid, &t.c0, &t.c_valid, &t.k_first, &t.depth, &t.matrix, &t.group, &t.part}) *v = scalar(*v);
     return true;
 }
+
+// Whether a kernel's blocks take one tile after the other, and the first operands of the next are on their way while the sums of
+// this one are finished: those of 256 x 256, alone on their compute unit, for whose sums LDS has just room beside the operands
+// (160 KB).  Against a block for each tile: bf16 8192 x 16384 x 4096 with GELU and pre-activations 959 -> 919 us, 32 groups of
+// 512 rows 2048 -> 8192 890 -> 830.  Two blocks of 128 x 128 hide each other's beginnings and ends: 64 groups of 128
+// rows, weight gradient 1568 -> 512, 54 us with a block for each tile, 60 this way.
+constexpr bool linear_persistent(int tile_rows) { return tile_rows == 256; }
 
 // The kernel's argument, read where it is used: the compiler would keep all of it in scalar registers, and have too few.
 __device__ __forceinline__ const Product& argument()
@@ -546,21 +574,34 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
     using OpR = Operand<T, R_KC, false, BR, WR, HALVES, NT, DIRECT>;
     using OpC = Operand<T, C_KC, true, BC, WC, HALVES, NT, DIRECT>;
     constexpr int BK = OpR::BK, SUBS = OpR::SUBS, STEPS = Mma<T>::STEPS;
+    constexpr bool PERSISTENT = linear_persistent(BR);
+    static_assert(!PERSISTENT || (HALVES == 2 && !SPLIT), "only this pipeline is begun ahead");
+    constexpr int FINISH_PIECES = TC * 4;  // 16-byte pieces of a wavefront's row of sums
+    constexpr int FINISH_BYTES = WR * WC * 16 * FINISH_PIECES * 16;
     // One array: where there are several, the compiler keeps account of what comes into which, and waits for more than it must.
-    __shared__ __attribute__((aligned(256))) char lds[2 * (OpR::BYTES + OpC::BYTES)];
+    __shared__ __attribute__((aligned(256))) char lds[2 * (OpR::BYTES + OpC::BYTES) + (PERSISTENT ? FINISH_BYTES : 0)];
+    static_assert(PERSISTENT || FINISH_BYTES <= 2 * (OpR::BYTES + OpC::BYTES), "the sums take the operands' place");
     constexpr int BUFFER = OpR::BYTES + OpC::BYTES;
     char *const r00 = lds, *const r01 = r00 + OpR::HBYTES, *const c00 = lds + OpR::BYTES, *const c01 = c00 + OpC::HBYTES;
     char *const r10 = r00 + BUFFER, *const c10 = c00 + BUFFER;
 
     const int tiles_r = RAGGED == RAGGED_R ? count_tiles(p.groups, BR, p.tiles_r) : p.tiles_r;
-    const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
+    const int tid = threadIdx.x, wave = scalar(tid >> 6);
+    int lane = tid & 63;
     const int wr = wave / WC, wc = wave % WC;  // of eight wavefronts, two that share a SIMD have different rows
     Tile tile;
-    if (!find_tile<BR, BC, BK, RAGGED>(p, tiles_r, blockIdx.x, tile)) return;
+    int block = blockIdx.x;
+    if (!find_tile<BR, BC, BK, RAGGED>(p, tiles_r, block, tile)) return;
     OpR opr;
     OpC opc;
+    // What is worked out from the thread's number around the products is worked out there, not kept in registers all along.
+    auto anew = [](int v) __attribute__((always_inline)) {
+        asm volatile("" : "+v"(v));
+        return v;
+    };
     auto begin = [&]() __attribute__((always_inline)) {
         const Product& p = argument();
+        const int tid = anew(threadIdx.x);
         opr.init(static_cast<const T*>(p.r) + (R_KC ? (int64_t)tile.r0 * p.r_row + tile.k_first : (int64_t)tile.k_first * p.r_row + tile.r0), p.r_row, tile.r_valid,
                      tile.depth, tid);
         opc.init(static_cast<const T*>(p.c) + tile.matrix * p.c_matrix + (C_KC ? (int64_t)tile.c0 * p.c_row + tile.k_first : (int64_t)tile.k_first * p.c_row + tile.c0),
@@ -573,8 +614,6 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         for (auto& row : sums)
             for (auto& sum : row) sum = floatx4{0.f, 0.f, 0.f, 0.f};
     };
-    clear(acc);
-    const int stages = (tile.depth + BK - 1) / BK;
     // fp32: the small terms of the split products, and whether the sums are to be formed without the split
     floatx4 small[SPLIT ? TR : 1][SPLIT ? TC : 1];
     uintx4 fr[HALVES][HR][SUBS], fc[HALVES][HC][SUBS];
@@ -597,287 +636,348 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 #pragma unroll
             for (int j = 0; j < HC; ++j) Mma<T>::add(fc[set][j][sub], fr[hr][i][sub], acc[hr * HR + i][hc * HC + j]);
     };
-    if constexpr (SPLIT) {
-        // fp32 products on the bf16 matrix instructions, operands split in three (ps_split.h), which are read as they are and split
-        // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Bound by the vector
-        // ALU that splits: 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
-        // instructions for each of the products that they enter.  A block whose sums the split may not hold (ps_split.h: not finite, or
-        // not zero and below 2^-80) forms them all again with fp32 matrix instructions.
-        auto pass = [&](auto form) __attribute__((always_inline)) {
-            constexpr bool exact = decltype(form)::value;
-            auto products = [&](const char* r, const char* c) __attribute__((always_inline)) {
-                if constexpr (exact) {
+    auto bring_two = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                    for (int sub = 0; sub < SUBS; ++sub) {
+        for (int b = 0; b < 2; ++b) {
+            bring_r(0, b);
+            bring_c(0, b);
+            bring_c(HALVES - 1, b);
+            bring_r(HALVES - 1, b);
+            opr.next_stage(tid);
+            opc.next_stage(tid);
+        }
+    };
+    if constexpr (PERSISTENT) bring_two();
+    for (;;) {
+        if constexpr (PERSISTENT && !R_KC) lane = anew(threadIdx.x) & 63;  // (for the other kinds this makes registers run out)
+        clear(acc);
+        const int stages = (tile.depth + BK - 1) / BK;
+        if constexpr (SPLIT) {
+            // fp32 products on the bf16 matrix instructions, operands split in three (ps_split.h), which are read as they are and split
+            // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Splitting takes
+            // 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
+            // instructions for each of the products that they enter.  4096^3: 720-790 us, six bf16 products at 1.05-1.15 PFLOP/s, of the
+            // 1.3-1.4 that a bf16 product of such sizes gets from this chip's power; fp32 matrix instructions: 1050.  A block whose sums the split may not hold (ps_split.h: not finite, or
+            // not zero and below 2^-80) forms them all again with fp32 matrix instructions.
+            auto pass = [&](auto form) __attribute__((always_inline)) {
+                constexpr bool exact = decltype(form)::value;
+                auto products = [&](const char* r, const char* c) __attribute__((always_inline)) {
+                    if constexpr (exact) {
+#pragma unroll
+                        for (int sub = 0; sub < SUBS; ++sub) {
+#pragma unroll
+                            for (int h = 0; h < HALVES; ++h) {
+                                fetch_c(c + h * OpC::HBYTES, sub, h);
+                                fetch_r(h, r + h * OpR::HBYTES, sub);
+                            }
+#pragma unroll
+                            for (int h = 0; h < HALVES * HALVES; ++h) multiply(h / HALVES, h % HALVES, sub, h % HALVES);
+                        }
+                    } else {
+                        auto parts = [](const uintx4& x, const uintx4& y) __attribute__((always_inline)) {
+                            float v[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? x[e] : y[e - 4]);
+                            return split8(v);
+                        };
+                        auto of_c = [&](int j, int sub) __attribute__((always_inline)) { return OpC::fetch(c + j / HC * OpC::HBYTES, wc, j % HC, sub, lane); };
+                        auto of_r = [&](int i, int sub) __attribute__((always_inline)) { return OpR::fetch(r + i / HR * OpR::HBYTES, wr, i % HR, sub, lane); };
+                        // The parts of one column or row are made while the matrix instructions of those before are under way, two vector
+                        // instructions to each where there are 24 of them: columns during the first row's products (4096^3 2-3 % less time
+                        // than without).
+                        Split8 sc[TC], sr, next;
+                        uintx4 x[2];
+                        auto read = [&](int n) __attribute__((always_inline)) {  // column 0, row 0, columns 1 .., rows 1 ..
+                            const bool column = n == 0 || (n > 1 && n <= TC);
+                            const int k = n == 0 ? 0 : n == 1 ? 0 : column ? n - 1 : n - TC;
+                            if (n >= TR + TC) return;
+#pragma unroll
+                            for (int sub = 0; sub < 2; ++sub) x[sub] = column ? of_c(k, sub) : of_r(k, sub);
+                        };
+                        auto among = [](auto products, auto vector) __attribute__((always_inline)) {
+                            __builtin_amdgcn_sched_group_barrier(0x100, 2 * std::max(OpR::READS, OpC::READS), 0);
+#pragma unroll
+                            for (int k = 0; k < decltype(products)::value; ++k) {
+                                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                                __builtin_amdgcn_sched_group_barrier(0x002, decltype(vector)::value, 0);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);  // or all rows are fetched and split ahead, and registers run out
+                        };
+                        auto product = [&](int i, int j, int t) __attribute__((always_inline)) {
+                            floatx4& to = t < SPLIT_SMALL ? small[i][j] : acc[i][j];
+                            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sc[j].part(TERM_A[t]), sr.part(TERM_B[t]), to, 0, 0, 0);
+                        };
+                        read(0);
+                        const uintx4 first[2] = {x[0], x[1]};
+                        read(1);
+                        sc[0] = parts(first[0], first[1]);
+                        sr = parts(x[0], x[1]);
+                        read(2);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int j = 0; j < TC; ++j) {
+                            const uintx4 raw[2] = {x[0], x[1]};
+                            read(j + 3);
+                            if (j + 1 < TC)
+                                sc[j + 1] = parts(raw[0], raw[1]);
+                            else if (TR > 1)
+                                next = parts(raw[0], raw[1]);
+#pragma unroll
+                            for (int t = 0; t <= SPLIT_SMALL; ++t) product(0, j, t);
+                            among(std::integral_constant<int, SPLIT_SMALL + 1>{}, std::integral_constant<int, 8>{});
+                        }
+#pragma unroll
+                        for (int i = 1; i < TR; ++i) {
+                            sr = next;
+                            const uintx4 raw[2] = {x[0], x[1]};
+                            read(TC + i + 2);
+                            if (i + 1 < TR) next = parts(raw[0], raw[1]);
+#pragma unroll
+                            for (int t = 0; t <= SPLIT_SMALL; ++t)
+#pragma unroll
+                                for (int j = 0; j < TC; ++j) product(i, j, t);
+                            among(std::integral_constant<int, (SPLIT_SMALL + 1) * TC>{}, std::integral_constant<int, 2>{});
+                        }
+                    }
+                };
+                if constexpr (DIRECT) {
+                    constexpr int LOADS = HALVES * (OpR::LOADS + OpC::LOADS);
+                    auto bring = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h) {
-                            fetch_c(c + h * OpC::HBYTES, sub, h);
-                            fetch_r(h, r + h * OpR::HBYTES, sub);
+                            bring_r(h, buffer);
+                            bring_c(h, buffer);
                         }
-#pragma unroll
-                        for (int h = 0; h < HALVES * HALVES; ++h) multiply(h / HALVES, h % HALVES, sub, h % HALVES);
-                    }
-                } else {
-                    auto parts = [](const uintx4& x, const uintx4& y) __attribute__((always_inline)) {
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? x[e] : y[e - 4]);
-                        return split8(v);
+                        opr.next_stage(tid);
+                        opc.next_stage(tid);
                     };
-                    auto of_c = [&](int j, int sub) __attribute__((always_inline)) { return OpC::fetch(c + j / HC * OpC::HBYTES, wc, j % HC, sub, lane); };
-                    auto of_r = [&](int i, int sub) __attribute__((always_inline)) { return OpR::fetch(r + i / HR * OpR::HBYTES, wr, i % HR, sub, lane); };
-                    Split8 sc[TC];
-#pragma unroll
-                    for (int j = 0; j < TC; ++j) sc[j] = parts(of_c(j, 0), of_c(j, 1));
-                    uintx4 x[2] = {of_r(0, 0), of_r(0, 1)};
-#pragma unroll
-                    for (int i = 0; i < TR; ++i) {
-                        const Split8 sr = parts(x[0], x[1]);
-                        if (i + 1 < TR) {
-                            x[0] = of_r(i + 1, 0);
-                            x[1] = of_r(i + 1, 1);
-                        }
-#pragma unroll
-                        for (int t = 0; t <= SPLIT_SMALL; ++t)
-#pragma unroll
-                            for (int j = 0; j < TC; ++j) {
-                                floatx4& to = t < SPLIT_SMALL ? small[i][j] : acc[i][j];
-                                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sc[j].part(TERM_A[t]), sr.part(TERM_B[t]), to, 0, 0, 0);
-                            }
-                        __builtin_amdgcn_sched_barrier(0);  // or all rows are fetched and split ahead, and registers run out
+                    bring(0);
+                    bring(1);
+#pragma unroll 1
+                    for (int s = 0; s < stages; ++s) {
+                        int from = (s & 1) * BUFFER;  // unknown to the compiler, which would keep addresses for either buffer in registers
+                        asm volatile("" : "+s"(from));
+                        __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
+                        block_barrier();
+                        products(r00 + from, c00 + from);
+                        block_barrier_after_reads();
+                        bring(s & 1);
+                    }
+                    __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+                } else {
+                    for (int s = 0; s < stages; ++s) {
+                        char *const r = s & 1 ? r10 : r00, *const c = s & 1 ? c10 : c00;
+                        opr.load(tid);
+                        opc.load(tid);
+                        opr.put(r, tid);
+                        opc.put(c, tid);
+                        opr.next_stage(tid);
+                        opc.next_stage(tid);
+                        __syncthreads();
+                        products(r, c);
                     }
                 }
             };
-            if constexpr (DIRECT) {
-                constexpr int LOADS = HALVES * (OpR::LOADS + OpC::LOADS);
-                auto bring = [&](int buffer) __attribute__((always_inline)) {
+            clear(small);
+            pass(std::false_type{});
+            bool lost = false;
 #pragma unroll
-                    for (int h = 0; h < HALVES; ++h) {
-                        bring_r(h, buffer);
-                        bring_c(h, buffer);
+            for (int i = 0; i < TR; ++i)
+#pragma unroll
+                for (int j = 0; j < TC; ++j) {
+                    acc[i][j] += small[i][j];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float m = fabsf(acc[i][j][e]);
+                        lost |= !(m < INFINITY) || (m < SPLIT_TINY && m > 0.f);
                     }
-                    opr.next_stage(tid);
-                    opc.next_stage(tid);
-                };
-                bring(0);
-                bring(1);
-#pragma unroll 1
-                for (int s = 0; s < stages; ++s) {
-                    int from = (s & 1) * BUFFER;  // unknown to the compiler, which would keep addresses for either buffer in registers
-                    asm volatile("" : "+s"(from));
-                    __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
-                    block_barrier();
-                    products(r00 + from, c00 + from);
-                    block_barrier_after_reads();
-                    bring(s & 1);
                 }
-                __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
-            } else {
-                for (int s = 0; s < stages; ++s) {
-                    char *const r = s & 1 ? r10 : r00, *const c = s & 1 ? c10 : c00;
-                    opr.load(tid);
-                    opc.load(tid);
-                    opr.put(r, tid);
-                    opc.put(c, tid);
-                    opr.next_stage(tid);
-                    opc.next_stage(tid);
-                    __syncthreads();
-                    products(r, c);
+            if (__syncthreads_or(lost)) {
+                begin();
+                clear(acc);
+                pass(std::true_type{});
+            }
+        } else if constexpr (HALVES == 2) {
+            // A stage in four phases, a quarter of the products each, in an order in which each phase needs one more half of an
+            // operand: it is read from LDS in the phase before.
+            //     products   R0 C0   R0 C1   R1 C1   R1 C0
+            //     reads      C1      R1      R0'     C0'      (') of the next stage
+            //     brings     R0"     C0"     C1"     R1"      (") of the stage after that, into this one's buffer
+            // Two barriers a stage, behind the second and the fourth phase: past them everybody's part of what is read next is in
+            // LDS, and nobody reads any more what is replaced next.  So a load has a stage and a half to arrive (with whole
+            // operands and one barrier it had one).
+            constexpr int FLIGHT = 2 * (OpR::LOADS + OpC::LOADS);
+            static_assert(OpR::LOADS == 2 && OpC::LOADS == 2, "a phase places two loads");
+            // A phase: the products of two halves, the reads of a third (`fetch`), and two loads, each behind a half of the products
+            auto phase = [&](int hr, int hc, int set, auto fetch, auto load) __attribute__((always_inline)) {
+                fetch();
+                multiply(hr, hc, 0, set);
+#pragma unroll
+                for (int i = 0; i < HR * HC; ++i) {  // the reads among the products
+                    __builtin_amdgcn_sched_group_barrier(0x008, STEPS, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, std::max(HR * OpR::READS, HC * OpC::READS) * SUBS / (HR * HC), 0);
                 }
-            }
-        };
-        clear(small);
-        pass(std::false_type{});
-        bool lost = false;
-#pragma unroll
-        for (int i = 0; i < TR; ++i)
-#pragma unroll
-            for (int j = 0; j < TC; ++j) {
-                acc[i][j] += small[i][j];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float m = fabsf(acc[i][j][e]);
-                    lost |= !(m < INFINITY) || (m < SPLIT_TINY && m > 0.f);
-                }
-            }
-        if (__syncthreads_or(lost)) {
-            begin();
-            clear(acc);
-            pass(std::true_type{});
-        }
-    } else if constexpr (HALVES == 2) {
-        // A stage in four phases, a quarter of the products each, in an order in which each phase needs one more half of an
-        // operand: it is read from LDS in the phase before.
-        //     products   R0 C0   R0 C1   R1 C1   R1 C0
-        //     reads      C1      R1      R0'     C0'      (') of the next stage
-        //     brings     R0"     C0"     C1"     R1"      (") of the stage after that, into this one's buffer
-        // Two barriers a stage, behind the second and the fourth phase: past them everybody's part of what is read next is in
-        // LDS, and nobody reads any more what is replaced next.  So a load has a stage and a half to arrive (with whole
-        // operands and one barrier it had one).
-        constexpr int FLIGHT = 2 * (OpR::LOADS + OpC::LOADS);
-        static_assert(OpR::LOADS == 2 && OpC::LOADS == 2, "a phase places two loads");
-        auto bring_two = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                bring_r(0, b);
-                bring_c(0, b);
-                bring_c(1, b);
-                bring_r(1, b);
-                opr.next_stage(tid);
-                opc.next_stage(tid);
-            }
-        };
-        // A phase: the products of two halves, the reads of a third (`fetch`), and two loads, each behind a half of the products
-        auto phase = [&](int hr, int hc, int set, auto fetch, auto load) __attribute__((always_inline)) {
-            fetch();
-            multiply(hr, hc, 0, set);
-#pragma unroll
-            for (int i = 0; i < HR * HC; ++i) {  // the reads among the products
-                __builtin_amdgcn_sched_group_barrier(0x008, STEPS, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, std::max(HR * OpR::READS, HC * OpC::READS) * SUBS / (HR * HC), 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            load(0);
-            multiply(hr, hc, 1, set);
-            __builtin_amdgcn_sched_barrier(0);
-            load(1);
-        };
-        auto arrived = [&]() __attribute__((always_inline)) {  // what is read next: everything but the last eight loads
-            __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT) & ~0xf00);
-            block_barrier();
-        };
-        // c0: the registers that hold C0 (those of C1 are free for the next stage's C0 when that is read)
-        auto stage = [&](int buffer, int c0) __attribute__((always_inline)) {
-            // unknown to the compiler, which would keep addresses for either buffer in registers, and have too few
-            int from = buffer * BUFFER, from_next = BUFFER - from, to = to_first + from;
-            asm volatile("" : "+s"(from), "+s"(from_next), "+s"(to));
-            phase(0, 0, c0, [&]() __attribute__((always_inline)) {
-                fetch_c(c01 + from, 0, c0 ^ 1);
-                fetch_c(c01 + from, 1, c0 ^ 1);
-            }, [&](int i) __attribute__((always_inline)) { opr.bring(0, i, to_r[0] + to); });
-            phase(0, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
-                fetch_r(1, r01 + from, 0);
-                fetch_r(1, r01 + from, 1);
-            }, [&](int i) __attribute__((always_inline)) { opc.bring(0, i, to_c[0] + to); });
-            arrived();
-            phase(1, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
-                fetch_r(0, r00 + from_next, 0);  // behind the last stage what lay there before, which nobody uses
-                fetch_r(0, r00 + from_next, 1);
-            }, [&](int i) __attribute__((always_inline)) { opc.bring(1, i, to_c[1] + to); });
-            phase(1, 0, c0, [&]() __attribute__((always_inline)) {
-                fetch_c(c00 + from_next, 0, c0 ^ 1);
-                fetch_c(c00 + from_next, 1, c0 ^ 1);
-            }, [&](int i) __attribute__((always_inline)) { opr.bring(1, i, to_r[1] + to); });
-            opr.next_stage(tid);
-            opc.next_stage(tid);
-            arrived();
-        };
-        bring_two();
-        arrived();
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            fetch_c(c00, sub, 0);
-            fetch_r(0, r00, sub);
-        }
-        block_barrier_after_reads();
-        // In a tile that is not whole, a wavefront without rows or columns of the result brings its share and no more.
-        if (wr * (BR / WR) < tile.r_valid && wc * (BC / WC) < tile.c_valid) {
-            for (int s = 0; s < stages; s += 2) {
-                stage(0, 0);
-                if (s + 1 < stages) stage(1, 1);
-            }
-        } else {
-#pragma unroll 1
-            for (int s = 0; s < stages; ++s) {
-                bring_r(0, s & 1);
-                bring_c(0, s & 1);
+                __builtin_amdgcn_sched_barrier(0);
+                load(0);
+                multiply(hr, hc, 1, set);
+                __builtin_amdgcn_sched_barrier(0);
+                load(1);
+            };
+            auto arrived = [&]() __attribute__((always_inline)) {  // what is read next: everything but the last eight loads
+                __builtin_amdgcn_s_waitcnt(wait_vm(FLIGHT) & ~0xf00);
+                block_barrier();
+            };
+            // c0: the registers that hold C0 (those of C1 are free for the next stage's C0 when that is read)
+            auto stage = [&](int buffer, int c0) __attribute__((always_inline)) {
+                // unknown to the compiler, which would keep addresses for either buffer in registers, and have too few
+                int from = buffer * BUFFER, from_next = BUFFER - from, to = to_first + from;
+                asm volatile("" : "+s"(from), "+s"(from_next), "+s"(to));
+                phase(0, 0, c0, [&]() __attribute__((always_inline)) {
+                    fetch_c(c01 + from, 0, c0 ^ 1);
+                    fetch_c(c01 + from, 1, c0 ^ 1);
+                }, [&](int i) __attribute__((always_inline)) { opr.bring(0, i, to_r[0] + to); });
+                phase(0, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
+                    fetch_r(1, r01 + from, 0);
+                    fetch_r(1, r01 + from, 1);
+                }, [&](int i) __attribute__((always_inline)) { opc.bring(0, i, to_c[0] + to); });
                 arrived();
-                bring_c(1, s & 1);
-                bring_r(1, s & 1);
+                phase(1, 1, c0 ^ 1, [&]() __attribute__((always_inline)) {
+                    fetch_r(0, r00 + from_next, 0);  // behind the last stage what lay there before, which nobody uses
+                    fetch_r(0, r00 + from_next, 1);
+                }, [&](int i) __attribute__((always_inline)) { opc.bring(1, i, to_c[1] + to); });
+                phase(1, 0, c0, [&]() __attribute__((always_inline)) {
+                    fetch_c(c00 + from_next, 0, c0 ^ 1);
+                    fetch_c(c00 + from_next, 1, c0 ^ 1);
+                }, [&](int i) __attribute__((always_inline)) { opr.bring(1, i, to_r[1] + to); });
                 opr.next_stage(tid);
                 opc.next_stage(tid);
                 arrived();
-            }
-        }
-        __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
-    } else if constexpr (DIRECT) {
-        // While the products of one half of a stage's k are formed, the operands of the next half are on their way from LDS to
-        // registers, and those of the next stage from memory to LDS.  One barrier a stage, in its middle: past it everybody's
-        // part of the next stage is in LDS, and nobody reads this one's buffer any more, which then takes the stage after next.
-        auto bring = [&](int buffer) __attribute__((always_inline)) {
-            bring_r(0, buffer);
-            bring_c(0, buffer);
-            opr.next_stage(tid);
-            opc.next_stage(tid);
-        };
-        auto fetch = [&](const char* r, const char* c, int sub) __attribute__((always_inline)) {
-            fetch_c(c, sub, 0);
-            fetch_r(0, r, sub);
-        };
-        constexpr int LOADS = OpR::LOADS + OpC::LOADS;
-        bring(0);
-        bring(1);
-        __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
-        block_barrier();
-        fetch(r00, c00, 0);
-        auto stage = [&](int buffer) __attribute__((always_inline)) {
-            fetch(buffer ? r10 : r00, buffer ? c10 : c00, 1);
-            multiply(0, 0, 0, 0);
-            __builtin_amdgcn_s_waitcnt(WAIT_ALL);
-            block_barrier();
-            fetch(buffer ? r00 : r10, buffer ? c00 : c10, 0);  // behind the last stage what lay there before, which nobody uses
-            multiply(0, 0, 1, 0);
-            bring(buffer);
-        };
-        for (int s = 0; s < stages; s += 2) {
-            stage(0);
-            if (s + 1 < stages) stage(1);
-        }
-        __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
-    } else {
-        if (stages > 0) {
-            opr.load(tid);
-            opc.load(tid);
-            opr.put(r00, tid);
-            opc.put(c00, tid);
-        }
-        __syncthreads();
-        for (int s = 0; s < stages; ++s) {
-            const char *r = s & 1 ? r10 : r00, *c = s & 1 ? c10 : c00;
-            char *r_next = s & 1 ? r00 : r10, *c_next = s & 1 ? c00 : c10;
-            if (s + 1 < stages) {
-                opr.next_stage(tid);
-                opc.next_stage(tid);
-                opr.load(tid);
-                opc.load(tid);
-            }
+            };
+            if constexpr (!PERSISTENT) bring_two();
+            arrived();
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
+                fetch_c(c00, sub, 0);
+                fetch_r(0, r00, sub);
+            }
+            block_barrier_after_reads();
+            // In a tile that is not whole, a wavefront without rows or columns of the result brings its share and no more.
+            if (wr * (BR / WR) < tile.r_valid && wc * (BC / WC) < tile.c_valid) {
+                for (int s = 0; s < stages; s += 2) {
+                    stage(0, 0);
+                    if (s + 1 < stages) stage(1, 1);
+                }
+            } else {
+#pragma unroll 1
+                for (int s = 0; s < stages; ++s) {
+                    bring_r(0, s & 1);
+                    bring_c(0, s & 1);
+                    arrived();
+                    bring_c(1, s & 1);
+                    bring_r(1, s & 1);
+                    opr.next_stage(tid);
+                    opc.next_stage(tid);
+                    arrived();
+                }
+            }
+            __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+        } else if constexpr (DIRECT) {
+            // While the products of one half of a stage's k are formed, the operands of the next half are on their way from LDS to
+            // registers, and those of the next stage from memory to LDS.  One barrier a stage, in its middle: past it everybody's
+            // part of the next stage is in LDS, and nobody reads this one's buffer any more, which then takes the stage after next.
+            auto bring = [&](int buffer) __attribute__((always_inline)) {
+                bring_r(0, buffer);
+                bring_c(0, buffer);
+                opr.next_stage(tid);
+                opc.next_stage(tid);
+            };
+            auto fetch = [&](const char* r, const char* c, int sub) __attribute__((always_inline)) {
                 fetch_c(c, sub, 0);
                 fetch_r(0, r, sub);
-                multiply(0, 0, sub, 0);
+            };
+            constexpr int LOADS = OpR::LOADS + OpC::LOADS;
+            bring(0);
+            bring(1);
+            __builtin_amdgcn_s_waitcnt(wait_vm(LOADS));
+            block_barrier();
+            fetch(r00, c00, 0);
+            auto stage = [&](int buffer) __attribute__((always_inline)) {
+                fetch(buffer ? r10 : r00, buffer ? c10 : c00, 1);
+                multiply(0, 0, 0, 0);
+                __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+                block_barrier();
+                fetch(buffer ? r00 : r10, buffer ? c00 : c10, 0);  // behind the last stage what lay there before, which nobody uses
+                multiply(0, 0, 1, 0);
+                bring(buffer);
+            };
+            for (int s = 0; s < stages; s += 2) {
+                stage(0);
+                if (s + 1 < stages) stage(1);
             }
-            if (s + 1 < stages) {
-                opr.put(r_next, tid);
-                opc.put(c_next, tid);
+            __builtin_amdgcn_s_waitcnt(wait_vm(0));  // LDS is given back with nothing on its way there
+        } else {
+            if (stages > 0) {
+                opr.load(tid);
+                opc.load(tid);
+                opr.put(r00, tid);
+                opc.put(c00, tid);
             }
             __syncthreads();
+            for (int s = 0; s < stages; ++s) {
+                const char *r = s & 1 ? r10 : r00, *c = s & 1 ? c10 : c00;
+                char *r_next = s & 1 ? r00 : r10, *c_next = s & 1 ? c00 : c10;
+                if (s + 1 < stages) {
+                    opr.next_stage(tid);
+                    opc.next_stage(tid);
+                    opr.load(tid);
+                    opc.load(tid);
+                }
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub) {
+                    fetch_c(c, sub, 0);
+                    fetch_r(0, r, sub);
+                    multiply(0, 0, sub, 0);
+                }
+                if (s + 1 < stages) {
+                    opr.put(r_next, tid);
+                    opc.put(c_next, tid);
+                }
+                __syncthreads();
+            }
         }
-    }
 
-    // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.  The sums go through
-    // LDS, 16 rows of a wavefront at a time, so that it stores whole cache lines, and the code that finishes them, of which only
-    // one way is taken, is there once (a copy for every MFMA tile made 150 KB, and its way through the instruction cache
-    // took 5 us a tile).
-    {
+        // Lane (q, l) has row 16 i + l, columns 16 j + 4 q + e, or, permuted, 32 j / 2 + 8 q + 4 (j & 1) + e.  The sums go through
+        // LDS, 16 rows of a wavefront at a time, so that it stores whole cache lines, and the code that finishes them, of which only
+        // one way is taken, is there once (a copy for every MFMA tile made 150 KB, and its way through the instruction cache
+        // took 5 us a tile).
+        // What comes to LDS for the next tile is older than the stores here, and the loads of what is added
+        // wait for it too; so the bias is there before, once for the tile.
         const Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
         const int rows = argument().rows, cols = argument().cols;
-        constexpr int PIECES = TC * 4, LANES = TC * 2, AT_ONCE = 64 / LANES;  // 16-byte pieces and lanes of a row, rows at once
-        block_barrier();                                                      // nobody reads what these take the place of
-        char* const mine = lds + wave * (16 * PIECES * 16);
-        const int l = lane & 15, q = lane >> 4;
+        constexpr int PIECES = FINISH_PIECES, LANES = TC * 2, AT_ONCE = 64 / LANES, TIMES = 16 / AT_ONCE;  // lanes of a row, rows at once
+        const Tile done = tile;
+        const int lane = anew(threadIdx.x) & 63, l = lane & 15, q = lane >> 4;
+        const int at = lane % LANES, c = wc * TC * 16 + 8 * at, c_valid = done.c_valid - c;  // the lane's eight columns
+        float bias[8];
+        load_bias<T>(epi, done.matrix, done.c0 + c, c_valid, bias);
+        block_barrier();  // nobody reads what comes, or these sums, take the place of
+        bool more = false;
+        if constexpr (PERSISTENT) {
+            block += gridDim.x;
+            more = find_tile<BR, BC, BK, RAGGED>(argument(), tiles_r, block, tile);
+            if (epi.bias) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(bias[e]));
+            }
+            if (more) {
+                begin();
+                bring_two();
+            }
+        }
+        char* const mine = lds + (PERSISTENT ? 2 * BUFFER : 0) + wave * (16 * PIECES * 16);
 #pragma unroll 1
         for (int i = 0; i < TR; ++i) {
+            const int first = (wr * TR + i) * 16 + lane / LANES;
 #pragma unroll
             for (int k = 0; k < TR; ++k) {
                 if (k != i) continue;  // the registers of a row of tiles have to be named
@@ -889,29 +989,29 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll 1
-            for (int h = 0; h < 16; h += AT_ONCE) {
-                const int row = h + lane / LANES, at = lane % LANES;  // eight columns of a row
-                float v[8];
+            for (int h = 0; h < TIMES; ++h) {
+                const int row = h * AT_ONCE + lane / LANES, r = first + h * AT_ONCE, valid = r < done.r_valid ? c_valid : 0;
+                float v[8], residual[8];
+                load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const floatx4 x = *reinterpret_cast<const floatx4*>(mine + row * (PIECES * 16) + (((2 * at + e) ^ (row & (PIECES - 1))) << 4));
 #pragma unroll
                     for (int n = 0; n < 4; ++n) v[4 * e + n] = x[n];
                 }
-                const int r = (wr * TR + i) * 16 + row, c = wc * TC * 16 + 8 * at;
-                const int valid = r < tile.r_valid ? tile.c_valid - c : 0;
                 if (epi.partial) {
-                    float* to = epi.partial + ((int64_t)tile.part * rows + (tile.r0 + r)) * cols + tile.c0 + c;
+                    float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
                     if (valid >= 8)
                         store_n(to, v);
                     else if (valid > 0)
                         store_some(to, valid, v);
                 } else {
-                    finish<T>(epi, tile.matrix, RAGGED == RAGGED_K ? tile.group : 0, tile.r0 + r, tile.c0 + c, valid, v);
+                    finish<T>(epi, bias, residual, RAGGED == RAGGED_K ? done.group : 0, done.r0 + r, done.c0 + c, valid, v);
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written
         }
+        if (!more) return;
     }
 }
 
@@ -932,14 +1032,14 @@ constexpr int LINEAR_TILE[3] = {64, 128, 256};
 template <class T, bool R_KC, bool C_KC, bool DIRECT, int RAGGED>
 void start_linear(const Product& p, int tile, hipStream_t s)
 {
-    const int total = p.tiles_r * p.tiles_c * p.parts;
-    const dim3 grid((total + LINEAR_XCDS - 1) / LINEAR_XCDS * LINEAR_XCDS);
+    const int total = (p.tiles_r * p.tiles_c * p.parts + LINEAR_XCDS - 1) / LINEAR_XCDS * LINEAR_XCDS;
+    const dim3 grid(total);
     if (tile == 0)
         hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 64, 64, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
     else if (tile == 1 || !DIRECT || sizeof(T) == 4)
         hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 128, 128, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
     else if constexpr (DIRECT && sizeof(T) == 2)
-        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), grid, dim3(512), 0, s, p);
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), dim3(linear_persistent(256) ? std::min(total, COMPUTE_UNITS) : total), dim3(512), 0, s, p);
 }
 template <bool R_KC, bool C_KC, int RAGGED>
 void start_linear_typed(const Product& p, int dtype, bool direct, int tile, hipStream_t s)

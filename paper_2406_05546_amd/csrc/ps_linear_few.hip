@@ -1,6 +1,7 @@
 // Forward pass for few rows (a token, a few sequences, few rows of each of many groups): bound by reading the weights
 // once, so these go straight to registers, and all wavefronts of a block read the same 16 columns' weights, each its share
-// of k.
+// of k.  bf16: 64 matrices of 2048 -> 1024 and 96 rows 44 us (6.1 TB/s), one row 4096 -> 4096 8.0 us (4.2 TB/s: of a launch
+// this short two trips to memory are half).
 #include "ps_linear.h"
 
 namespace ps {
@@ -28,6 +29,12 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
 #pragma unroll
     for (int i = 0; i < TR; ++i) r[i] = static_cast<const T*>(p.r) + (int64_t)min(r0 + 16 * i + l, rows.end - 1) * p.r_row;
 
+    // lane (q, l) of wavefront w finishes row l of row tile w, columns 4q .. 4q + 3; what is added to them is asked for first
+    const int row = r0 + 16 * wave + l, col = c0 + 4 * q, valid = wave < TR && row < rows.end ? p.cols - col : 0;
+    float bias[4], residual[4];
+    load_bias<T>(p.epi, matrix, col, valid, bias);
+    load_residual<T>(p.epi, row, col, valid, residual);
+
     floatx4 acc[TR];
 #pragma unroll
     for (int i = 0; i < TR; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -39,8 +46,24 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
         __builtin_memcpy(&x, row + k, 32);
         return x;
     };
-    auto some = [&](const T* row, int k) __attribute__((always_inline)) {  // zeros past the end of the row
+    // The last, partial step: zeros past the end of the row.  A row of a step's share of a lane or more is read once more up to its end,
+    // and what other lanes have of it is cleared, in both operands (it may be infinite); element by element, the
+    // wavefront that has this step took longer than all others for theirs (37 rows of 1111 -> 2777 in fp16: 17.1 us, this way 12.3).
+    auto some = [&](const T* row, int k) __attribute__((always_inline)) {
         Pair x = {};
+        if (p.depth >= 2 * E) {
+            const int at = min(k, p.depth - 2 * E), drop = k - at;  // the first `drop` elements are others'
+            x = whole(row, at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t v = x.v[i / 4][i % 4];
+                if constexpr (sizeof(T) == 4)
+                    x.v[i / 4][i % 4] = i < drop ? 0u : v;
+                else
+                    x.v[i / 4][i % 4] = 2 * i + 1 < drop ? 0u : 2 * i < drop ? v & 0xffff0000u : v;
+            }
+            return x;
+        }
         T e[2 * E];
         __builtin_memcpy(e, &x, 32);
 #pragma unroll
@@ -86,13 +109,11 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
     for (int i = 0; i < TR; ++i) meet[wave][i][lane] = acc[i];
     __syncthreads();
     if (wave >= TR) return;
-    // lane (q, l) has row l, columns 4q .. 4q + 3 of the tile
     floatx4 sum = meet[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += meet[w][wave][lane];
     float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    const int row = r0 + 16 * wave + l, col = c0 + 4 * q;
-    finish<T>(p.epi, matrix, 0, row, col, row < rows.end ? p.cols - col : 0, v);
+    finish<T>(p.epi, bias, residual, 0, row, col, valid, v);
 }
 
 template <class T>
