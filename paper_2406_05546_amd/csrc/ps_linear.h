@@ -577,7 +577,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
     constexpr bool PERSISTENT = linear_persistent(BR);
     static_assert(!PERSISTENT || (HALVES == 2 && !SPLIT), "only this pipeline is begun ahead");
     constexpr int FINISH_PIECES = TC * 4;  // 16-byte pieces of a wavefront's row of sums
-    constexpr int FINISH_BYTES = WR * WC * 16 * FINISH_PIECES * 16;
+    constexpr int FINISH_BYTES = WR * WC * (PERSISTENT ? 1 : TR) * 16 * FINISH_PIECES * 16;
     // One array: where there are several, the compiler keeps account of what comes into which, and waits for more than it must.
     __shared__ __attribute__((aligned(256))) char lds[2 * (OpR::BYTES + OpC::BYTES) + (PERSISTENT ? FINISH_BYTES : 0)];
     static_assert(PERSISTENT || FINISH_BYTES <= 2 * (OpR::BYTES + OpC::BYTES), "the sums take the operands' place");
@@ -656,7 +656,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             // fp32 products on the bf16 matrix instructions, operands split in three (ps_split.h), which are read as they are and split
             // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Splitting takes
             // 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
-            // instructions for each of the products that they enter.  4096^3: 720-790 us, six bf16 products at 1.05-1.15 PFLOP/s, of the
+            // instructions for each of the products that they enter.  4096^3: 685-750 us, six bf16 products at 1.1-1.2 PFLOP/s, of the
             // 1.3-1.4 that a bf16 product of such sizes gets from this chip's power; fp32 matrix instructions: 1050.  A block whose sums the split may not hold (ps_split.h: not finite, or
             // not zero and below 2^-80) forms them all again with fp32 matrix instructions.
             auto pass = [&](auto form) __attribute__((always_inline)) {
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                         auto of_c = [&](int j, int sub) __attribute__((always_inline)) { return OpC::fetch(c + j / HC * OpC::HBYTES, wc, j % HC, sub, lane); };
                         auto of_r = [&](int i, int sub) __attribute__((always_inline)) { return OpR::fetch(r + i / HR * OpR::HBYTES, wr, i % HR, sub, lane); };
                         // The parts of one column or row are made while the matrix instructions of those before are under way, two vector
-                        // instructions to each where there are 24 of them: columns during the first row's products (4096^3 2-3 % less time
+                        // instructions to each where there are 24 of them: columns during the first row's products (4096^3 3-5 % less time
                         // than without).
                         Split8 sc[TC], sr, next;
                         uintx4 x[2];
@@ -694,8 +694,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 #pragma unroll
                             for (int sub = 0; sub < 2; ++sub) x[sub] = column ? of_c(k, sub) : of_r(k, sub);
                         };
-                        auto among = [](auto products, auto vector) __attribute__((always_inline)) {
-                            __builtin_amdgcn_sched_group_barrier(0x100, 2 * std::max(OpR::READS, OpC::READS), 0);
+                        // the read of that number, and then products with vector instructions between them
+                        auto among = [](auto products, auto vector, int reads) __attribute__((always_inline)) {
+                            if (reads < TR + TC) __builtin_amdgcn_sched_group_barrier(0x100, 2 * std::max(OpR::READS, OpC::READS), 0);
 #pragma unroll
                             for (int k = 0; k < decltype(products)::value; ++k) {
                                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                                 next = parts(raw[0], raw[1]);
 #pragma unroll
                             for (int t = 0; t <= SPLIT_SMALL; ++t) product(0, j, t);
-                            among(std::integral_constant<int, SPLIT_SMALL + 1>{}, std::integral_constant<int, 8>{});
+                            among(std::integral_constant<int, SPLIT_SMALL + 1>{}, std::integral_constant<int, 8>{}, j + 3);
                         }
 #pragma unroll
                         for (int i = 1; i < TR; ++i) {
@@ -736,7 +737,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                             for (int t = 0; t <= SPLIT_SMALL; ++t)
 #pragma unroll
                                 for (int j = 0; j < TC; ++j) product(i, j, t);
-                            among(std::integral_constant<int, (SPLIT_SMALL + 1) * TC>{}, std::integral_constant<int, 2>{});
+                            among(std::integral_constant<int, (SPLIT_SMALL + 1) * TC>{}, std::integral_constant<int, 2>{}, TC + i + 2);
                         }
                     }
                 };
@@ -954,7 +955,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         // wait for it too; so the bias is there before, once for the tile.
         const Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
         const int rows = argument().rows, cols = argument().cols;
-        constexpr int PIECES = FINISH_PIECES, LANES = TC * 2, AT_ONCE = 64 / LANES, TIMES = 16 / AT_ONCE;  // lanes of a row, rows at once
+        constexpr int PIECES = FINISH_PIECES, LANES = TC * 2, AT_ONCE = 64 / LANES;  // lanes of a row, rows at once
         const Tile done = tile;
         const int lane = anew(threadIdx.x) & 63, l = lane & 15, q = lane >> 4;
         const int at = lane % LANES, c = wc * TC * 16 + 8 * at, c_valid = done.c_valid - c;  // the lane's eight columns
@@ -974,31 +975,34 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                 bring_two();
             }
         }
-        char* const mine = lds + (PERSISTENT ? 2 * BUFFER : 0) + wave * (16 * PIECES * 16);
+        constexpr int TURN = PERSISTENT ? 1 : TR;  // MFMA tiles of rows that go through LDS at once: all, where they take the operands' place
+        char* const mine = lds + (PERSISTENT ? 2 * BUFFER : 0) + wave * (TURN * 16 * PIECES * 16);
 #pragma unroll 1
-        for (int i = 0; i < TR; ++i) {
-            const int first = (wr * TR + i) * 16 + lane / LANES;
+        for (int i = 0; i < TR; i += TURN) {
 #pragma unroll
             for (int k = 0; k < TR; ++k) {
-                if (k != i) continue;  // the registers of a row of tiles have to be named
+                if (TURN == 1 && k != i) continue;  // the registers of a row of tiles have to be named
 #pragma unroll
                 for (int j = 0; j < TC; ++j) {
                     const int piece = OpC::PERMUTED ? 8 * (j / 2) + 2 * q + (j & 1) : 4 * j + q;
-                    *reinterpret_cast<floatx4*>(mine + l * (PIECES * 16) + ((piece ^ (l & (PIECES - 1))) << 4)) = acc[k][j];
+                    *reinterpret_cast<floatx4*>(mine + (k % TURN * 16 + l) * (PIECES * 16) + ((piece ^ (l & (PIECES - 1))) << 4)) = acc[k][j];
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            auto take = [&](int row, floatx4 (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x[e] = *reinterpret_cast<const floatx4*>(mine + row * (PIECES * 16) + (((2 * at + e) ^ (row & (PIECES - 1))) << 4));
+            };
+            floatx4 x[2];
+            take(lane / LANES, x);
 #pragma unroll 1
-            for (int h = 0; h < TIMES; ++h) {
-                const int row = h * AT_ONCE + lane / LANES, r = first + h * AT_ONCE, valid = r < done.r_valid ? c_valid : 0;
+            for (int h = 0; h < TURN * 16; h += AT_ONCE) {
+                const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < done.r_valid ? c_valid : 0;
                 float v[8], residual[8];
                 load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const floatx4 x = *reinterpret_cast<const floatx4*>(mine + row * (PIECES * 16) + (((2 * at + e) ^ (row & (PIECES - 1))) << 4));
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) v[4 * e + n] = x[n];
-                }
+                for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
+                take(h + AT_ONCE < TURN * 16 ? row + AT_ONCE : row, x);
                 if (epi.partial) {
                     float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
                     if (valid >= 8)
@@ -1009,7 +1013,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                     finish<T>(epi, bias, residual, RAGGED == RAGGED_K ? done.group : 0, done.r0 + r, done.c0 + c, valid, v);
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written
+            if constexpr (TURN < TR) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written
         }
         if (!more) return;
     }

@@ -216,7 +216,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         const int size = LINEAR_TILE[tile], room = tile == 2 ? 1 : tile == 1 ? 2 : 4;  // blocks to a compute unit
         const double through = direct ? 1 : tile ? 2 : 1.6;  // operands through registers
         const double alone = (wide ? (tile ? 1.6 : 0.6) : tile == 2 ? 1.6 : tile == 1 ? 0.6 : 0.35) * through;  // us a stage
-        const double full = (wide ? (tile ? 2.8 : 1.6) : tile == 2 ? 1.6 : tile == 1 ? 1.0 : 0.75) * through;
+        const double full = (wide ? (tile ? 2.8 : 2.2) : tile == 2 ? 1.6 : tile == 1 ? 1.0 : 0.75) * through;
         const double around = tile == 2 ? 7 : 3.5;  // us of a block's first loads and its stores
         Plan p{};
         p.tile = tile;
@@ -225,8 +225,11 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         p.tiles_c = up(cols, size);
         const int64_t likely = (kind == DW ? p.tiles_r : up(rows, size) + (one ? 0 : l.n_groups / 2)) * p.tiles_c;  // half a tile more each
         const int of_group = (int)(kind == DW ? std::max<int64_t>(1, stages / l.n_groups) : stages);
-        for (int parts = 1; parts <= 32; parts *= 2) {
-            if (parts > 1 && (!one || stages < 4 * parts || p.tiles_r * p.tiles_c * parts > 2 * room * COMPUTE_UNITS)) break;
+        // one part, or as many as all blocks that there is room for at once (or half or a quarter of them) make of it
+        const int64_t tiles = std::max<int64_t>(1, p.tiles_r * p.tiles_c), most = one ? std::min<int64_t>(32, stages / 4) : 1;
+        for (int fill : {0, 4, 2, 1}) {
+            const int parts = fill ? (int)std::min<int64_t>(most, room * COMPUTE_UNITS / fill / tiles) : 1;
+            if (fill && parts < 2) continue;
             p.part_stages = (int)up(stages, parts);
             p.parts = (int)up(std::max(stages, 1), std::max(p.part_stages, 1));
             p.partial_bytes = parts > 1 ? (uint64_t)p.parts * rows * cols * 4 : 0;
