@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
 enum { FORWARD, DX, DW };
 
 struct Plan {
-    int few;  // if not 0: forward pass for few rows, so many times 16 of a group to a block
+    int few;  // if not 0: forward pass or input gradient for few rows, so many times 16 of a group to a block
     int tile, parts, part_stages;
     int64_t tiles_r, tiles_c;
     uint64_t partial_bytes;
@@ -205,15 +205,29 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         if (best.tiles_r * best.tiles_c <= INT32_MAX) return best;
         best = Plan{};
     }
+    const int size = dtype_size(l.dtype);
+    if (kind == DX && each <= 32 && l.in_features * size >= 16) {  // (ps_linear_few.hip says what both sides measured)
+        best.few = each <= 16 ? 1 : 2;
+        best.tiles_r = up(l.rows, 16 * best.few) + (one ? 0 : l.n_groups);
+        best.tiles_c = up(l.in_features, 256 / size);
+        // parts as many as make two blocks to a compute unit, of two steps to a wavefront at least
+        const int64_t steps = up(depth, FEW_DX_STEP / size), tiles = std::max<int64_t>(1, best.tiles_r * best.tiles_c);
+        const int64_t parts = one ? std::max<int64_t>(1, std::min(2 * COMPUTE_UNITS / tiles, steps / 16)) : 1;
+        best.part_stages = (int)up(steps, parts);
+        best.parts = (int)up(steps, best.part_stages);
+        best.partial_bytes = best.parts > 1 ? (uint64_t)best.parts * rows * cols * 4 : 0;
+        if (tiles * best.parts <= INT32_MAX) return best;
+        best = Plan{};
+    }
     // The form that should take least, by what its blocks take when one, or as many as there is room for, are on a compute
     // unit.  What that chooses, in us against the other tiles (256, 128, 64; bf16 if not said): 4096^3 256: 110, 133, 194; 8192 rows
     // 1568 -> 512 128: 53, 20, 27; 1024^3 64: 27, 20, 10; 256 rows 4096 -> 4096 128 in parts: 35, 24, 32; weight gradient of
     // 8192 rows 1568 -> 512 128 in parts: 53, 30, 38, in fp32 128 in parts: -, 92, 146.
-    const int stages = (int)up(depth, 128 / dtype_size(l.dtype));
+    const int stages = (int)up(depth, 128 / size);
     const bool wide = l.dtype == PS_F32;
     double least = 0;
     for (int tile = wide || !direct ? 1 : 2; tile >= 0; --tile) {
-        const int size = LINEAR_TILE[tile], room = tile == 2 ? 1 : tile == 1 ? 2 : 4;  // blocks to a compute unit
+        const int side = LINEAR_TILE[tile], room = tile == 2 ? 1 : tile == 1 ? 2 : 4;  // blocks to a compute unit
         const double through = direct ? 1 : tile ? 2 : 1.6;  // operands through registers
         const double alone = (wide ? (tile ? 1.6 : 0.6) : tile == 2 ? 1.6 : tile == 1 ? 0.6 : 0.35) * through;  // us a stage
         const double full = (wide ? (tile ? 2.8 : 2.2) : tile == 2 ? 1.6 : tile == 1 ? 1.0 : 0.75) * through;
@@ -221,9 +235,9 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         Plan p{};
         p.tile = tile;
         // groups that are cut up separately have at most one tile more each than all rows together
-        p.tiles_r = kind == DW ? up(rows, size) * l.n_groups : up(rows, size) + (one ? 0 : l.n_groups);
-        p.tiles_c = up(cols, size);
-        const int64_t likely = (kind == DW ? p.tiles_r : up(rows, size) + (one ? 0 : l.n_groups / 2)) * p.tiles_c;  // half a tile more each
+        p.tiles_r = kind == DW ? up(rows, side) * l.n_groups : up(rows, side) + (one ? 0 : l.n_groups);
+        p.tiles_c = up(cols, side);
+        const int64_t likely = (kind == DW ? p.tiles_r : up(rows, side) + (one ? 0 : l.n_groups / 2)) * p.tiles_c;  // half a tile more each
         const int of_group = (int)(kind == DW ? std::max<int64_t>(1, stages / l.n_groups) : stages);
         // one part, or as many as all blocks that there is room for at once (or half or a quarter of them) make of it
         const int64_t tiles = std::max<int64_t>(1, p.tiles_r * p.tiles_c), most = one ? std::min<int64_t>(32, stages / 4) : 1;
@@ -369,8 +383,10 @@ void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, 
     p.groups = groups_of(l);
     p.epi = epi;
     if (plan.parts > 1) p.epi.partial = partial;
-    if (plan.few) return launch_linear_few(p, l.dtype, plan.few, s);
-    (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
+    if (plan.few)
+        (kind == FORWARD ? launch_linear_few : launch_linear_few_dx)(p, l.dtype, plan.few, s);
+    else
+        (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
     if (plan.parts > 1) {
         const int64_t threads = up(p.cols, 8) * p.rows;
         with_type(l.dtype, [&](auto t) {

@@ -1,4 +1,4 @@
-// Forward pass for few rows (a token, a few sequences, few rows of each of many groups): bound by reading the weights
+// Forward pass and input gradient for few rows (a token, a few sequences, few rows of each of many groups): bound by reading the weights
 // once, so these go straight to registers, and all wavefronts of a block read the same 16 columns' weights, each its share
 // of k.  bf16: 64 matrices of 2048 -> 1024 and 96 rows 44 us (6.1 TB/s), one row 4096 -> 4096 8.0 us (4.2 TB/s: of a launch
 // this short two trips to memory are half).
@@ -116,6 +116,124 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
     finish<T>(p.epi, bias, residual, 0, row, col, valid, v);
 }
 
+// Input gradient for few rows: dx = dz W, bound by reading W once, whose rows lie along the result's columns.  A lane takes E
+// columns of E consecutive k straight to registers, 16 bytes of each row, and turns them there; its c-th column is
+// column E * lane + c of the block, so that each of E matrix instructions has one column of every lane.  A block: 16 E columns,
+// 16 * TR rows of a group, and a part of the contraction, of which wavefront w takes every WAVES-th step.  bf16, against the
+// tiles of ps_linear.h: one row 4096 -> 4096 14.1 -> 8.7 us, 16 rows 17.0 -> 10.8, 16 rows 16384 -> 4096 28.5 -> 26.4 (5.1 TB/s),
+// 32 groups of 12 rows 192 -> 7424 57 -> 28, 10 of one row 90 -> 4340 88 -> 14; fp32 4096 -> 4096 30 -> 17 and 18.  From 33 rows
+// on it gains nothing (four row tiles, 64 rows 4096 -> 4096 15.6 -> 16.3, 64 groups of 60 rows 512 -> 1024 18.7 -> 19.6).
+template <class T, int TR, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 4) void linear_few_dx_kernel(Product p)
+{
+    constexpr int E = Mma<T>::E, COLS = 16 * E, STEP = FEW_DX_STEP / sizeof(T), AHEAD = TR > 1 ? 1 : 2;
+    constexpr int PITCH = COLS + 4, EACH = 16 * COLS / (64 * WAVES);  // sums of a row of the block in LDS, and of a thread at the end
+    static_assert(STEP == 4 * E && EACH * 64 * WAVES == 16 * COLS && E % EACH == 0, "");
+    __shared__ float meet[WAVES][16 * PITCH];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), l = lane & 15, q = lane >> 4;
+    const int tc = blockIdx.x % p.tiles_c, rest = blockIdx.x / p.tiles_c, part = rest % p.parts, tr = rest / p.parts;
+    GroupRows rows;
+    int r0;
+    if (!find_rows(p.groups, tr, 16 * TR, rows, r0)) return;
+    const int matrix = group_matrix(p.groups, rows.g), c0 = tc * COLS;
+    // Columns past the end: the last E again (there are as many), stored again with the same value.  Rows past the end: the last one again.
+    auto first_column = [&](int of) { return min(c0 + of * E, p.cols - E); };
+    const T* const c = static_cast<const T*>(p.c) + matrix * p.c_matrix + first_column(l);
+    const T* r[TR];
+#pragma unroll
+    for (int i = 0; i < TR; ++i) r[i] = static_cast<const T*>(p.r) + (int64_t)min(r0 + 16 * i + l, rows.end - 1) * p.r_row;
+
+    floatx4 acc[TR][E];
+#pragma unroll
+    for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[i][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    struct Piece {
+        uintx4 w[E], d[TR];
+    };
+    auto load = [&](int k, Piece& x) __attribute__((always_inline)) {  // k: of the lane's first
+#pragma unroll
+        for (int e = 0; e < E; ++e) __builtin_memcpy(&x.w[e], c + (int64_t)(k + e) * p.c_row, 16);
+#pragma unroll
+        for (int i = 0; i < TR; ++i) __builtin_memcpy(&x.d[i], r[i] + k, 16);
+    };
+    auto load_last = [&](int k, Piece& x) __attribute__((always_inline)) {  // zeros past the end of the contraction
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            x.w[e] = uintx4{0, 0, 0, 0};
+            if (k + e < p.depth) __builtin_memcpy(&x.w[e], c + (int64_t)(k + e) * p.c_row, 16);
+        }
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+            x.d[i] = uintx4{0, 0, 0, 0};
+            T d[E];
+            __builtin_memcpy(d, &x.d[i], 16);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k + e < p.depth) d[e] = r[i][k + e];
+            __builtin_memcpy(&x.d[i], d, 16);
+        }
+    };
+    auto multiply = [&](const Piece& x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            uintx4 column;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 4)
+                    column[i] = x.w[i][e];
+                else
+                    column[i] = __builtin_amdgcn_perm(x.w[2 * i + 1][e / 2], x.w[2 * i][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+            }
+#pragma unroll
+            for (int i = 0; i < TR; ++i) Mma<T>::add(column, x.d[i], acc[i][e]);
+        }
+    };
+    const int all = (p.depth + STEP - 1) / STEP, from = min(part * p.part_stages, all), to = min(from + p.part_stages, all);
+    const int whole = min(to, p.depth / STEP);
+    int s = from + wave;
+    for (; s + (AHEAD - 1) * WAVES < whole; s += AHEAD * WAVES) {
+        Piece x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load((s + u * WAVES) * STEP + q * E, x[u]);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) multiply(x[u]);
+    }
+    for (; s < to; s += WAVES) {
+        Piece x;
+        if (s < whole)
+            load(s * STEP + q * E, x);
+        else
+            load_last(s * STEP + q * E, x);
+        multiply(x);
+    }
+    // Lane (q, l) has row l and E * 4 consecutive columns from 4 q E on: column e of lane 4 q + n in acc[e][n].
+#pragma unroll
+    for (int i = 0; i < TR; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<floatx4*>(&meet[wave][l * PITCH + (4 * q + n) * E + e]) = floatx4{acc[i][e][n], acc[i][e + 1][n], acc[i][e + 2][n], acc[i][e + 3][n]};
+        __syncthreads();
+        const int at = threadIdx.x * EACH, row = at / COLS, of = at % COLS, out_row = r0 + 16 * i + row;
+        float v[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) v[e] = meet[0][row * PITCH + of + e];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) v[e] += meet[w][row * PITCH + of + e];
+        if (out_row >= rows.end) continue;
+        const int col = first_column(of / E) + of % E;
+        if (p.epi.partial)
+            store_n(p.epi.partial + ((int64_t)part * p.rows + out_row) * p.cols + col, v);
+        else
+            store_n(static_cast<T*>(p.epi.out) + out_row * p.epi.out_row + col, v);
+    }
+}
+
 template <class T>
 void start_few(const Product& p, int row_tiles, hipStream_t s)
 {
@@ -129,7 +247,27 @@ void start_few(const Product& p, int row_tiles, hipStream_t s)
         hipLaunchKernelGGL((linear_few_kernel<T, 4, 8>), grid, dim3(512), 0, s, p);
 }
 
+template <class T>
+void start_few_dx(const Product& p, int row_tiles, hipStream_t s)
+{
+    const dim3 grid(p.tiles_r * p.tiles_c * p.parts);
+    if (row_tiles == 1)
+        hipLaunchKernelGGL((linear_few_dx_kernel<T, 1, 8>), grid, dim3(512), 0, s, p);
+    else
+        hipLaunchKernelGGL((linear_few_dx_kernel<T, 2, 8>), grid, dim3(512), 0, s, p);
+}
+
 }  // namespace
+
+void launch_linear_few_dx(const Product& p, int dtype, int row_tiles, hipStream_t s)
+{
+    if (dtype == PS_F32)
+        start_few_dx<float>(p, row_tiles, s);
+    else if (dtype == PS_BF16)
+        start_few_dx<bf16_t>(p, row_tiles, s);
+    else
+        start_few_dx<f16_t>(p, row_tiles, s);
+}
 
 void launch_linear_few(const Product& p, int dtype, int row_tiles, hipStream_t s)
 {
