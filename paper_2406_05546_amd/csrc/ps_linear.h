@@ -464,7 +464,8 @@ __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N]
 struct Product {
     const void *r, *c;                       // operands
     int64_t r_row, c_row, c_matrix;          // strides in elements; c_matrix between the matrices of C
-    int32_t rows, cols, depth;               // of the result (RAGGED_K: per group) and of the contraction (RAGGED_K: of all groups)
+    int32_t rows, cols, depth;               // of the result (RAGGED_K: per group) and of the contraction (RAGGED_K: of all groups), as the operands have them
+    int32_t out_rows, out_cols;              // of the result as it is written: operands may be padded
     int32_t tiles_r, tiles_c;                // tiles along the rows (RAGGED_K: of all groups together) and columns
     int32_t parts, part_stages;              // the contraction in parts of so many stages each
     Groups groups;
@@ -954,11 +955,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         // What comes to LDS for the next tile is older than the stores here, and the loads of what is added
         // wait for it too; so the bias is there before, once for the tile.
         const Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
-        const int rows = argument().rows, cols = argument().cols;
+        const int rows = argument().out_rows, cols = argument().out_cols;
         constexpr int PIECES = FINISH_PIECES, LANES = TC * 2, AT_ONCE = 64 / LANES;  // lanes of a row, rows at once
         const Tile done = tile;
         const int lane = anew(threadIdx.x) & 63, l = lane & 15, q = lane >> 4;
-        const int at = lane % LANES, c = wc * TC * 16 + 8 * at, c_valid = done.c_valid - c;  // the lane's eight columns
+        const int at = lane % LANES, c = wc * TC * 16 + 8 * at, c_valid = cols - done.c0 - c;  // the lane's eight columns
+        const int r_valid = RAGGED == RAGGED_K ? rows - done.r0 : done.r_valid;
         float bias[8];
         load_bias<T>(epi, done.matrix, done.c0 + c, c_valid, bias);
         block_barrier();  // nobody reads what comes, or these sums, take the place of
@@ -997,7 +999,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             take(lane / LANES, x);
 #pragma unroll 1
             for (int h = 0; h < TURN * 16; h += AT_ONCE) {
-                const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < done.r_valid ? c_valid : 0;
+                const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < r_valid ? c_valid : 0;
                 float v[8], residual[8];
                 load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
 #pragma unroll

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             if (n == 8)
                 store_n(dz, d);
             else
-                store_some(dz, n, d);
+                store_some(dz, (int)min(a.dz_row - col, (int64_t)8), d);  // zeros up to the end of its rows
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += d[i];
@@ -177,6 +177,32 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
     finish<T>(epi, bias, residual, 0, row, col, n, v);
 }
 
+// ---- operands of odd sizes ------------------------------------------------------------------------------------------
+
+// Copies rows of `cols` elements to rows of `cols_to` (a multiple of 16 bytes) and matrices of `rows` to `rows_to`, zeros behind: 16 bytes to a thread.
+template <class T>
+__global__ __launch_bounds__(256) void pad_kernel(const T* __restrict__ from, int64_t row, int64_t matrix, int rows, int cols, T* __restrict__ to, int rows_to, int cols_to, int64_t pieces)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int per_row = cols_to / E;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t line = i / per_row, m = line / rows_to;
+        const int r = (int)(line - m * rows_to), c = (int)(i - line * per_row) * E;
+        T v[E] = {};
+        if (r < rows) {
+            const T* p = from + m * matrix + r * row + c;
+            if (c + E <= cols) {
+                __builtin_memcpy(v, p, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (c + e < cols) v[e] = p[e];
+            }
+        }
+        __builtin_memcpy(to + line * cols_to + c, v, 16);
+    }
+}
+
 // ---- plans ---------------------------------------------------------------------------------------------------------
 
 enum { FORWARD, DX, DW };
@@ -186,6 +212,7 @@ struct Plan {
     int tile, parts, part_stages;
     int64_t tiles_r, tiles_c;
     uint64_t partial_bytes;
+    double us;  // estimated; 0 for few rows
 };
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -225,10 +252,10 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
     // 8192 rows 1568 -> 512 128 in parts: 53, 30, 38, in fp32 128 in parts: -, 92, 146.
     const int stages = (int)up(depth, 128 / size);
     const bool wide = l.dtype == PS_F32;
-    double least = 0;
     for (int tile = wide || !direct ? 1 : 2; tile >= 0; --tile) {
         const int side = LINEAR_TILE[tile], room = tile == 2 ? 1 : tile == 1 ? 2 : 4;  // blocks to a compute unit
-        const double through = direct ? 1 : tile ? 2 : 1.6;  // operands through registers
+        // operands through registers, which in 16 bits are turned element by element where they lie along the result
+        const double through = direct ? 1 : wide ? (tile ? 1.5 : 1.1) : (tile ? 2 : 1.6) * (kind == FORWARD ? 1 : 2);
         const double alone = (wide ? (tile ? 1.6 : 0.6) : tile == 2 ? 1.6 : tile == 1 ? 0.6 : 0.35) * through;  // us a stage
         const double full = (wide ? (tile ? 2.8 : 2.2) : tile == 2 ? 1.6 : tile == 1 ? 1.0 : 0.75) * through;
         const double around = tile == 2 ? 7 : 3.5;  // us of a block's first loads and its stores
@@ -250,12 +277,9 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
             const int64_t blocks = likely * p.parts, rounds = up(blocks, (int64_t)room * COMPUTE_UNITS);
             const double on_a_unit = std::min<double>(room, (double)up(blocks, COMPUTE_UNITS));
             const double stage = room > 1 ? alone + (full - alone) * (on_a_unit - 1) / (room - 1) : full;
-            double us = (double)rounds * (around + stage * std::min(of_group, std::max(p.part_stages, 1)));
-            if (parts > 1) us += 4 + (double)p.partial_bytes * 1.5 / 4e6;  // written, read and joined
-            if (!best.tiles_r || us < least) {
-                best = p;
-                least = us;
-            }
+            p.us = (double)rounds * (around + stage * std::min(of_group, std::max(p.part_stages, 1)));
+            if (parts > 1) p.us += 4 + (double)p.partial_bytes * 1.5 / 4e6;  // written, read and joined
+            if (!best.tiles_r || p.us < best.us) best = p;
         }
     }
     return best;
@@ -267,12 +291,6 @@ int slope_parts(const ps_linear& l)
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(up(4 * COMPUTE_UNITS, blocks), up(up(l.rows, l.n_groups), 16)), 65535 / std::min<int64_t>(l.n_groups, 65535)));
 }
 
-struct BackwardSpace {
-    uint64_t dz, bias, partial, total;
-    int64_t dz_row;
-    int parts;
-};
-
 uint64_t up256(uint64_t b) { return (b + 255) / 256 * 256; }
 
 bool direct_possible(const ps_linear& l, int kind)
@@ -281,13 +299,48 @@ bool direct_possible(const ps_linear& l, int kind)
     return l.in_features % e == 0 && (kind == FORWARD || l.out_features % e == 0);
 }
 
+// Where rows are no multiples of 16 bytes, operands come through registers, in 1.5 (fp32) to 4 times the time, or are copied
+// first to rows that are; then the copies come straight to LDS.  Copied if the plans differ by more than copying takes: backward of 7335 rows
+// 949 -> 4658 with GELU in bf16 1076 -> 285 us, in fp32 1370 -> 1035, forward 168 -> 124 and 576 -> 405; of 3414 rows 1665 -> 605 in bf16 121 -> 63.
+// (The kernels for few rows take any alignment.)
+struct Padded {
+    int64_t in, out;  // features, up to multiples of 16 bytes
+    uint64_t x, w, dz;  // bytes of the copies
+};
+Padded padded(const ps_linear& l)
+{
+    const int size = dtype_size(l.dtype), e = 16 / size;
+    Padded p{up(l.in_features, e) * e, up(l.out_features, e) * e, 0, 0, 0};
+    p.x = up256((uint64_t)l.rows * p.in * size);
+    p.w = up256((uint64_t)l.n_weights * p.out * p.in * size);
+    p.dz = up256((uint64_t)l.rows * p.out * size);
+    return p;
+}
+bool worth_padding(const ps_linear& l, int kind)
+{
+    if (direct_possible(l, kind)) return false;
+    const Padded p = padded(l);
+    const bool dz = l.activation == PS_ACT_NONE;  // with an activation it is in such rows already
+    const double bytes = 2. * (kind == FORWARD ? p.x + p.w : (kind == DX ? p.w : p.x) + (dz ? p.dz : 0));
+    return plan_product(l, kind, false).us > plan_product(l, kind, true).us + bytes / 4e6 + (kind == FORWARD || dz ? 10 : 5);
+}
+
+struct BackwardSpace {
+    uint64_t dz, bias, partial, x, w, total;
+    int64_t dz_row;
+    int parts;
+    bool pad_dx, pad_dw;
+};
+
 BackwardSpace backward_space(const ps_linear& l)
 {
     BackwardSpace b{};
-    const int size = dtype_size(l.dtype);
-    b.dz_row = up(l.out_features, 16 / size) * (16 / size);
+    const Padded p = padded(l);
+    b.dz_row = p.out;
     b.parts = slope_parts(l);
-    const uint64_t dz = l.activation != PS_ACT_NONE ? up256((uint64_t)l.rows * b.dz_row * size) : 0;
+    b.pad_dx = worth_padding(l, DX);
+    b.pad_dw = worth_padding(l, DW);
+    const uint64_t dz = l.activation != PS_ACT_NONE || b.pad_dx || b.pad_dw ? p.dz : 0;
     const uint64_t bias = up256((uint64_t)l.n_groups * b.parts * l.out_features * 4);
     uint64_t partial = 0;
     for (int kind : {DX, DW})
@@ -295,13 +348,25 @@ BackwardSpace backward_space(const ps_linear& l)
     b.dz = 0;
     b.bias = dz;
     b.partial = dz + bias;
-    b.total = b.partial + up256(partial);
+    b.x = b.partial + up256(partial);
+    b.w = b.x + (b.pad_dw ? p.x : 0);
+    b.total = b.w + (b.pad_dx ? p.w : 0);
     return b;
 }
 
-uint64_t forward_space(const ps_linear& l)
+struct ForwardSpace {
+    uint64_t x, w, total;
+    bool pad;
+};
+
+ForwardSpace forward_space(const ps_linear& l)
 {
-    return up256(std::max(plan_product(l, FORWARD, true).partial_bytes, plan_product(l, FORWARD, false).partial_bytes));
+    ForwardSpace f{};
+    f.pad = worth_padding(l, FORWARD);
+    f.x = up256(std::max(plan_product(l, FORWARD, true).partial_bytes, plan_product(l, FORWARD, false).partial_bytes));
+    f.w = f.x + (f.pad ? padded(l).x : 0);
+    f.total = f.w + (f.pad ? padded(l).w : 0);
+    return f;
 }
 
 // ---- checks --------------------------------------------------------------------------------------------------------
@@ -363,19 +428,36 @@ void with_type(int dtype, F f)
         f(f16_t{});
 }
 
-void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, const ps_matrix& c, Epilogue epi, float* partial, hipStream_t s)
+// A copy of [matrices][rows][cols] in rows of a multiple of 16 bytes, zeros behind rows and columns.
+ps_matrix pad(const ps_linear& l, const ps_matrix& m, int64_t matrices, int64_t rows, int64_t cols, int64_t rows_to, int64_t cols_to, void* to, hipStream_t s)
+{
+    const int64_t pieces = matrices * rows_to * cols_to * dtype_size(l.dtype) / 16;
+    if (pieces)
+        with_type(l.dtype, [&](auto t) {
+            using T = decltype(t);
+            hipLaunchKernelGGL(pad_kernel<T>, dim3((uint32_t)std::min<int64_t>(up(pieces, 256), 16 * COMPUTE_UNITS)), dim3(256), 0, s, static_cast<const T*>(m.data_dev),
+                               m.row, m.matrix, (int)rows, (int)cols, static_cast<T*>(to), (int)rows_to, (int)cols_to, pieces);
+        });
+    return ps_matrix{to, cols_to, rows_to * cols_to};
+}
+
+// copied: both operands are padded copies.
+void run_product(const ps_linear& l, int kind, bool direct, bool copied, const ps_matrix& r, const ps_matrix& c, Epilogue epi, float* partial, hipStream_t s)
 {
     const Plan plan = plan_product(l, kind, direct);
+    const int64_t in = copied ? padded(l).in : l.in_features, out = copied ? padded(l).out : l.out_features;
     Product p{};
     p.r = r.data_dev;
     p.c = c.data_dev;
     // a single row's distance to the next may be anything, but the kernels multiply with it
-    p.r_row = l.rows > 1 ? r.row : kind == FORWARD ? l.in_features : l.out_features;
-    p.c_row = (kind == DW ? l.rows : l.out_features) > 1 ? c.row : l.in_features;
+    p.r_row = l.rows > 1 ? r.row : kind == FORWARD ? in : out;
+    p.c_row = (kind == DW ? l.rows : out) > 1 ? c.row : in;
     p.c_matrix = c.matrix;
-    p.rows = (int32_t)(kind == DW ? l.out_features : l.rows);
-    p.cols = (int32_t)(kind == FORWARD ? l.out_features : l.in_features);
-    p.depth = (int32_t)(kind == FORWARD ? l.in_features : kind == DX ? l.out_features : l.rows);
+    p.out_rows = (int32_t)(kind == DW ? l.out_features : l.rows);
+    p.out_cols = (int32_t)(kind == FORWARD ? l.out_features : l.in_features);
+    p.rows = (int32_t)(kind == DW ? out : l.rows);
+    p.cols = (int32_t)(kind == FORWARD ? l.out_features : in);
+    p.depth = (int32_t)(kind == FORWARD ? in : kind == DX ? out : l.rows);
     p.tiles_r = (int32_t)plan.tiles_r;
     p.tiles_c = (int32_t)plan.tiles_c;
     p.parts = plan.parts;
@@ -388,9 +470,9 @@ void run_product(const ps_linear& l, int kind, bool direct, const ps_matrix& r, 
     else
         (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
     if (plan.parts > 1) {
-        const int64_t threads = up(p.cols, 8) * p.rows;
+        const int64_t threads = up(p.out_cols, 8) * p.out_rows;
         with_type(l.dtype, [&](auto t) {
-            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.rows, p.cols, epi);
+            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, epi);
         });
     }
 }
@@ -412,7 +494,7 @@ extern "C" ps_status ps_linear_workspace_bytes(const ps_linear* l, int32_t backw
     const ps_status st = check_layer("ps_linear_workspace_bytes", l);
     if (st != PS_OK) return st;
     if (!bytes_out) return dense_fail(PS_EINVAL, "ps_linear_workspace_bytes: no place for the result");
-    *bytes_out = backward ? backward_space(*l).total : forward_space(*l);
+    *bytes_out = backward ? backward_space(*l).total : forward_space(*l).total;
     return PS_OK;
 }
 
@@ -430,7 +512,8 @@ extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, c
     if ((st = check_matrix(call, "y", *l, y, true, l->rows, l->out_features, 1)) != PS_OK) return st;
     if ((st = check_matrix(call, "pre", *l, pre, false, l->rows, l->out_features, 1)) != PS_OK) return st;
     if (!l->rows) return PS_OK;
-    const uint64_t need = forward_space(*l);
+    const ForwardSpace space = forward_space(*l);
+    const uint64_t need = space.total;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
     if (workspace_bytes < need) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -442,7 +525,15 @@ extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, c
     if (there(pre)) e.pre = pre->data_dev, e.pre_row = pre->row;
     e.act = l->activation;
     const bool direct = direct_possible(*l, FORWARD) && aligned16(*l, *x, l->rows, 1) && aligned16(*l, *w, l->out_features, l->n_weights);
-    run_product(*l, FORWARD, direct, *x, *w, e, static_cast<float*>(workspace), s);
+    char* const base = static_cast<char*>(workspace);
+    if (space.pad) {
+        const Padded to = padded(*l);
+        const ps_matrix xp = pad(*l, *x, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s);
+        const ps_matrix wp = pad(*l, *w, l->n_weights, l->out_features, l->in_features, to.out, to.in, base + space.w, s);
+        run_product(*l, FORWARD, true, true, xp, wp, e, reinterpret_cast<float*>(base), s);
+    } else {
+        run_product(*l, FORWARD, direct, false, *x, *w, e, reinterpret_cast<float*>(base), s);
+    }
     return launched(call);
 }
 
@@ -492,12 +583,19 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
         });
     }
     float* const partial = reinterpret_cast<float*>(base + space.partial);
+    const Padded to = padded(*l);
+    const bool pad_dx = want_dx && space.pad_dx, pad_dw = want_dw && space.pad_dw;
+    ps_matrix dzp = dz;
+    if ((pad_dx || pad_dw) && !act) dzp = pad(*l, dz, 1, l->rows, l->out_features, l->rows, to.out, base + space.dz, s);
     if (want_dx && l->rows) {
         Epilogue e{};
         e.out = dx->data_dev;
         e.out_row = dx->row;
         const bool direct = direct_possible(*l, DX) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, *w, l->out_features, l->n_weights);
-        run_product(*l, DX, direct, dz, *w, e, partial, s);
+        if (pad_dx)
+            run_product(*l, DX, true, true, dzp, pad(*l, *w, l->n_weights, l->out_features, l->in_features, to.out, to.in, base + space.w, s), e, partial, s);
+        else
+            run_product(*l, DX, direct, false, dz, *w, e, partial, s);
     }
     if (want_dw) {
         Epilogue e{};
@@ -506,7 +604,10 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
         e.out_matrix = dw->matrix;
         const ps_matrix xm = x ? *x : none;
         const bool direct = direct_possible(*l, DW) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, xm, l->rows, 1);
-        run_product(*l, DW, direct, dz, xm, e, partial, s);
+        if (pad_dw)
+            run_product(*l, DW, true, true, dzp, pad(*l, xm, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s), e, partial, s);
+        else
+            run_product(*l, DW, direct, false, dz, xm, e, partial, s);
     }
     return launched(call);
 }
