@@ -424,21 +424,22 @@ __device__ __forceinline__ void load_residual(const Epilogue& e, int64_t row, in
     if (e.residual && valid > 0) load_columns<T>(e.residual, row * e.residual_row + col, valid, x);
 }
 template <class T, int N>
-__device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int group, int64_t row, int col, int valid, float (&v)[N])
+__device__ __forceinline__ void store_columns(T* p, int valid, const float (&v)[N])
+{
+    if (valid >= N)
+        store_n(p, v);
+    else
+        store_some(p, valid, v);
+}
+template <class T, int N>
+__device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int64_t row, int col, int valid, float (&v)[N])
 {
     if (valid <= 0) return;
-    auto store = [&](void* base, int64_t at) __attribute__((always_inline)) {
-        T* p = static_cast<T*>(base) + at;
-        if (valid >= N)
-            store_n(p, v);
-        else
-            store_some(p, valid, v);
-    };
     if (e.bias) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += bias[i];
     }
-    if (e.pre) store(e.pre, row * e.pre_row + col);
+    if (e.pre) store_columns(static_cast<T*>(e.pre) + row * e.pre_row + col, valid, v);
     if (e.act == PS_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = activate<PS_ACT_RELU>(v[i]);
@@ -453,7 +454,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N]
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += residual[i];
     }
-    store(e.out, group * e.out_matrix + row * e.out_row + col);
+    store_columns(static_cast<T*>(e.out) + row * e.out_row + col, valid, v);
 }
 
 #endif
@@ -570,7 +571,7 @@ template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DI
 __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 {
     constexpr int NT = 64 * WR * WC, TR = BR / WR / 16, TC = BC / WC / 16;
-    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr bool SPLIT = sizeof(T) == 4, FORWARD_PASS = R_KC && C_KC;
     constexpr int HALVES = DIRECT && TR >= 4 && TC >= 4 ? 2 : 1, HR = TR / HALVES, HC = TC / HALVES;
     using OpR = Operand<T, R_KC, false, BR, WR, HALVES, NT, DIRECT>;
     using OpC = Operand<T, C_KC, true, BC, WC, HALVES, NT, DIRECT>;
@@ -962,13 +963,13 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         const int at = lane % LANES, c = wc * TC * 16 + 8 * at, c_valid = cols - done.c0 - c;  // the lane's eight columns
         const int r_valid = RAGGED == RAGGED_K ? rows - done.r0 : done.r_valid;
         float bias[8];
-        load_bias<T>(epi, done.matrix, done.c0 + c, c_valid, bias);
+        if constexpr (FORWARD_PASS) load_bias<T>(epi, done.matrix, done.c0 + c, c_valid, bias);
         block_barrier();  // nobody reads what comes, or these sums, take the place of
         bool more = false;
         if constexpr (PERSISTENT) {
             block += gridDim.x;
             more = find_tile<BR, BC, BK, RAGGED>(argument(), tiles_r, block, tile);
-            if (epi.bias) {
+            if (FORWARD_PASS && epi.bias) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(bias[e]));
             }
@@ -1001,18 +1002,18 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             for (int h = 0; h < TURN * 16; h += AT_ONCE) {
                 const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < r_valid ? c_valid : 0;
                 float v[8], residual[8];
-                load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
+                if constexpr (FORWARD_PASS) load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
                 take(h + AT_ONCE < TURN * 16 ? row + AT_ONCE : row, x);
+                if (valid <= 0) continue;
                 if (epi.partial) {
                     float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
-                    if (valid >= 8)
-                        store_n(to, v);
-                    else if (valid > 0)
-                        store_some(to, valid, v);
+                    store_columns(to, valid, v);
+                } else if constexpr (FORWARD_PASS) {
+                    finish<T>(epi, bias, residual, done.r0 + r, done.c0 + c, valid, v);
                 } else {
-                    finish<T>(epi, bias, residual, RAGGED == RAGGED_K ? done.group : 0, done.r0 + r, done.c0 + c, valid, v);
+                    store_columns(static_cast<T*>(epi.out) + (RAGGED == RAGGED_K ? done.group : 0) * epi.out_matrix + (done.r0 + r) * epi.out_row + done.c0 + c, valid, v);
                 }
             }
             if constexpr (TURN < TR) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
     float bias[8], residual[8];
     load_bias<T>(epi, 0, col, n, bias);
     load_residual<T>(epi, row, col, n, residual);
-    finish<T>(epi, bias, residual, 0, row, col, n, v);
+    finish<T>(epi, bias, residual, row, col, n, v);
 }
 
 // ---- operands of odd sizes ------------------------------------------------------------------------------------------
