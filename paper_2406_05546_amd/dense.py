@@ -88,7 +88,7 @@ def _dtype(call: str, name: str, t) -> int:
 
 def _matrix(call: str, name: str, t, device, dtype, shape: Tuple[int, ...], matrices: bool = False) -> Tuple[int, int, int]:
     """Checks that `t` has this shape, type and device; the fields of its ps_matrix."""
-    if t.dtype is not dtype or t.device != device:
+    if t.dtype is not dtype or t.get_device() != device.index:
         _refuse(call, f"{name} is {t.dtype} on {t.device}, not {dtype} on {device}")
     if t.shape != shape:
         _refuse(call, f"{name} has the shape {tuple(t.shape)}, not {shape}")
@@ -126,6 +126,7 @@ class _Arguments(threading.local):
         self.need = ctypes.c_uint64(0)
         self.at = ctypes.addressof(self.memory)
         self.at_need = ctypes.addressof(self.need)
+        self.at_matrices = [self.at + _LAYER_BYTES + i * _MATRIX_BYTES for i in range(7)]
 
 
 _arguments = _Arguments()
@@ -168,8 +169,7 @@ def _run(call: str, layer: Tuple[int, ...], backward: int, device, matrices) -> 
         _check(call, st)
     need = a.need.value
     ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    first = a.at + _LAYER_BYTES
-    refs = [None if m is None else first + i * _MATRIX_BYTES for i, m in enumerate(matrices)]
+    refs = [at if m else None for m, at in zip(matrices, a.at_matrices)]
     st = (lib.ps_linear_backward if backward else lib.ps_linear_forward)(a.at, *refs, None if ws is None else ws.data_ptr(), need,
                                                                          torch._C._cuda_getCurrentRawStream(index))
     if st != PS_OK:
@@ -182,7 +182,7 @@ def _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, ou
     grouped, device, dtype, rows, fin, fout = offsets is not None, x.device, x.dtype, layer[2], layer[3], layer[4]
     mats = (w.shape[0],) if grouped else ()
     of_out = (rows, fout)
-    y = torch.empty(of_out, dtype=dtype, device=device) if out is None else out
+    y = x.new_empty(of_out) if out is None else out
     _run(call, layer, 0, device, [
         _matrix(call, "x", x, device, dtype, (rows, fin)), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
         None if bias is None else _matrix(call, "bias", bias, device, dtype, mats + (fout,), grouped),
@@ -211,11 +211,11 @@ def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need
     mats, of = ((w.shape[0],), (groups,)) if grouped else ((), ())
     of_in, of_out, of_w, of_b = (rows, fin), (rows, fout), of + (fout, fin), of + (fout,)
     if dx is None and need_dx:
-        dx = torch.empty(of_in, dtype=dtype, device=device)
+        dx = x.new_empty(of_in)
     if dw is None and need_dw:
-        dw = torch.empty(of_w, dtype=dtype, device=device)
+        dw = x.new_empty(of_w)
     if db is None and need_db:
-        db = torch.empty(of_b, dtype=dtype, device=device)
+        db = x.new_empty(of_b)
     _run(call, layer, 1, device, [
         _matrix(call, "dy", dy, device, dtype, of_out), _matrix(call, "x", x, device, dtype, of_in), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
         None if pre is None else _matrix(call, "pre", pre, device, dtype, of_out), None if dx is None else _matrix(call, "dx", dx, device, dtype, of_in),
