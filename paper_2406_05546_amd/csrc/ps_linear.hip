@@ -137,8 +137,7 @@ template <class T>
 __global__ __launch_bounds__(BIAS_COLS * BIAS_SHARES) void bias_sum_kernel(const float* __restrict__ partial, T* __restrict__ db, int64_t db_matrix, int cols, int parts)
 {
     __shared__ float meet[BIAS_SHARES][BIAS_COLS];
-    const int i = threadIdx.x % BIAS_COLS, share = threadIdx.x / BIAS_COLS, g = blockIdx.x / ((cols + BIAS_COLS - 1) / BIAS_COLS);
-    const int c = (blockIdx.x - g * ((cols + BIAS_COLS - 1) / BIAS_COLS)) * BIAS_COLS + i;
+    const int i = threadIdx.x % BIAS_COLS, share = threadIdx.x / BIAS_COLS, g = blockIdx.y, c = blockIdx.x * BIAS_COLS + i;
     const int each = (parts + BIAS_SHARES - 1) / BIAS_SHARES, first = share * each, last = min(first + each, parts);
     float s = 0.f;
     if (c < cols) {
@@ -217,6 +216,9 @@ struct Plan {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Blocks of 512 threads in a launch, which has less than 2^32 threads.
+constexpr int64_t FEW_BLOCKS = 1 << 23;
+
 Plan plan_product(const ps_linear& l, int kind, bool direct)
 {
     const int64_t rows = kind == DW ? l.out_features : l.rows, cols = kind == FORWARD ? l.out_features : l.in_features;
@@ -229,7 +231,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         best.parts = 1;
         best.tiles_r = up(l.rows, 16 * best.few) + (one ? 0 : l.n_groups);
         best.tiles_c = up(l.out_features, 16);
-        if (best.tiles_r * best.tiles_c <= INT32_MAX) return best;
+        if (best.tiles_r * best.tiles_c < FEW_BLOCKS) return best;
         best = Plan{};
     }
     const int size = dtype_size(l.dtype);
@@ -243,7 +245,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
         best.part_stages = (int)up(steps, parts);
         best.parts = (int)up(steps, best.part_stages);
         best.partial_bytes = best.parts > 1 ? (uint64_t)best.parts * rows * cols * 4 : 0;
-        if (tiles * best.parts <= INT32_MAX) return best;
+        if (tiles * best.parts < FEW_BLOCKS) return best;
         best = Plan{};
     }
     // The form that should take least, by what its blocks take when one, or as many as there is room for, are on a compute
@@ -578,7 +580,7 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
             using T = decltype(t);
             hipLaunchKernelGGL(slope_kernel<T>, dim3((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many), dim3(256), 0, s, a);
             if (want_db)
-                hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)(up(l->out_features, BIAS_COLS) * l->n_groups)), dim3(BIAS_COLS * BIAS_SHARES), 0, s, a.partial,
+                hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)up(l->out_features, BIAS_COLS), (uint32_t)l->n_groups), dim3(BIAS_COLS * BIAS_SHARES), 0, s, a.partial,
                                    static_cast<T*>(db->data_dev), db->matrix, (int)l->out_features, space.parts);
         });
     }

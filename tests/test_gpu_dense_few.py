@@ -2,7 +2,7 @@
 in parts, strides, and what is not finite.  Tolerances are those of test_gpu_dense."""
 import pytest
 
-from tests.test_gpu_dense import TYPES, check_backward, dense, gen, randn  # noqa: F401
+from tests.test_gpu_dense import TYPES, check_backward, check_forward, dense, gen, randn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,19 @@ def test_groups_whose_sizes_are_far_from_their_mean(dense):  # noqa: F811
             s = slice(edges[i], edges[i + 1])
             check_backward((dx[s], None, None), dy[s], x[s], w[i], "none", None)
     assert bool((dx[edges[-1]:] == 7).all())
+
+
+def test_more_groups_than_one_launch_of_the_small_blocks_holds(dense):  # noqa: F811
+    """32768 groups, most of them empty, and 4608 columns: 9.4 million blocks of 16 columns would pass 2^32 threads."""
+    import torch
+    t, g = torch.bfloat16, gen(6)
+    groups, rows, fin, fout = 32768, 40, 16, 4608
+    edges = torch.zeros(groups + 1, dtype=torch.int32)
+    edges[7:] = 9
+    edges[20000:] = rows
+    x, w, b = randn(g, t, rows, fin), randn(g, t, 2, fout, fin, scale=0.25), randn(g, t, 2, fout)
+    index = torch.zeros(groups, dtype=torch.int32)
+    index[19999] = 1
+    y = dense.ps_grouped_linear_forward(x, edges.cuda(), w, b, weight_of_group=index.cuda())
+    check_forward(y[:9], x[:9], w[0], b[0], None, "none")
+    check_forward(y[9:], x[9:], w[1], b[1], None, "none")
