@@ -50,16 +50,19 @@ __device__ __forceinline__ void store_n(T* p, const float (&v)[N])
     for (int i = 0; i < N; ++i) raw[i] = from_float<T>(v[i]);
     __builtin_memcpy(p, raw, sizeof(raw));
 }
-// The first n of them (zeros behind).
+// The first n of them (zeros behind).  The address is hidden from the compiler: next to load_n or store_n of the same elements, in the
+// other branch, it would take what both have in common out of both, and leave no wide access in either.
 template <int N, class T>
 __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[N])
 {
+    asm volatile("" : "+v"(p));
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = i < n ? to_float(p[i]) : 0.f;
 }
 template <int N, class T>
 __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N])
 {
+    asm volatile("" : "+v"(p));
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < n) p[i] = from_float<T>(v[i]);

@@ -431,7 +431,7 @@ __device__ __forceinline__ void store_columns(T* p, int valid, const float (&v)[
     else
         store_some(p, valid, v);
 }
-template <class T, int N>
+template <class T, bool RESIDUAL, int N>
 __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int64_t row, int col, int valid, float (&v)[N])
 {
     if (valid <= 0) return;
@@ -450,7 +450,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N]
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = activate<PS_ACT_SILU>(v[i]);
     }
-    if (e.residual) {
+    if (RESIDUAL) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += residual[i];
     }
@@ -996,25 +996,37 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) x[e] = *reinterpret_cast<const floatx4*>(mine + row * (PIECES * 16) + (((2 * at + e) ^ (row & (PIECES - 1))) << 4));
             };
-            floatx4 x[2];
-            take(lane / LANES, x);
+            // A loop of its own where there is a residual: behind its loads, taken or not, the compiler waits for all stores before.
+            auto finish_rows = [&](auto residual_too) __attribute__((always_inline)) {
+                constexpr bool RESIDUAL = decltype(residual_too)::value;
+                floatx4 x[2];
+                take(lane / LANES, x);
 #pragma unroll 1
-            for (int h = 0; h < TURN * 16; h += AT_ONCE) {
-                const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < r_valid ? c_valid : 0;
-                float v[8], residual[8];
-                if constexpr (FORWARD_PASS) load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
+                for (int h = 0; h < TURN * 16; h += AT_ONCE) {
+                    const int row = h + lane / LANES, r = (wr * TR + i) * 16 + row, valid = r < r_valid ? c_valid : 0;
+                    float v[8], residual[8];
+                    if constexpr (RESIDUAL) load_residual<T>(epi, done.r0 + r, done.c0 + c, valid, residual);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
-                take(h + AT_ONCE < TURN * 16 ? row + AT_ONCE : row, x);
-                if (valid <= 0) continue;
-                if (epi.partial) {
-                    float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
-                    store_columns(to, valid, v);
-                } else if constexpr (FORWARD_PASS) {
-                    finish<T>(epi, bias, residual, done.r0 + r, done.c0 + c, valid, v);
-                } else {
-                    store_columns(static_cast<T*>(epi.out) + (RAGGED == RAGGED_K ? done.group : 0) * epi.out_matrix + (done.r0 + r) * epi.out_row + done.c0 + c, valid, v);
+                    for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
+                    take(h + AT_ONCE < TURN * 16 ? row + AT_ONCE : row, x);
+                    if (valid <= 0) continue;
+                    if (epi.partial) {
+                        float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
+                        store_columns(to, valid, v);
+                    } else if constexpr (FORWARD_PASS) {
+                        finish<T, RESIDUAL>(epi, bias, residual, done.r0 + r, done.c0 + c, valid, v);
+                    } else {
+                        store_columns(static_cast<T*>(epi.out) + (RAGGED == RAGGED_K ? done.group : 0) * epi.out_matrix + (done.r0 + r) * epi.out_row + done.c0 + c, valid, v);
+                    }
                 }
+            };
+            if constexpr (FORWARD_PASS) {
+                if (epi.residual && !epi.partial)
+                    finish_rows(std::true_type{});
+                else
+                    finish_rows(std::false_type{});
+            } else {
+                finish_rows(std::false_type{});
             }
             if constexpr (TURN < TR) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows are written
         }

@@ -173,7 +173,10 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
     float bias[8], residual[8];
     load_bias<T>(epi, 0, col, n, bias);
     load_residual<T>(epi, row, col, n, residual);
-    finish<T>(epi, bias, residual, row, col, n, v);
+    if (epi.residual)
+        finish<T, true>(epi, bias, residual, row, col, n, v);
+    else
+        finish<T, false>(epi, bias, residual, row, col, n, v);
 }
 
 // ---- operands of odd sizes ------------------------------------------------------------------------------------------

@@ -113,7 +113,10 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += meet[w][wave][lane];
     float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    finish<T>(p.epi, bias, residual, row, col, valid, v);
+    if (p.epi.residual)
+        finish<T, true>(p.epi, bias, residual, row, col, valid, v);
+    else
+        finish<T, false>(p.epi, bias, residual, row, col, valid, v);
 }
 
 // Input gradient for few rows: dx = dz W, bound by reading W once, whose rows lie along the result's columns.  A lane takes E
