@@ -60,7 +60,8 @@ typedef struct {
     const int32_t* weight_of_group_dev; /* [n_groups] or NULL     */
 } ps_linear;
 
-/* Device bytes that a forward (backward = 0) or backward call with this layer needs as its workspace. */
+/* Device bytes that a forward (backward = 0) or backward call with this layer needs as its workspace: dz, partial sums,
+ * and copies of operands whose features are no multiples of 16 bytes, where these make a large product faster. */
 PS_API ps_status ps_linear_workspace_bytes(const ps_linear* layer, int32_t backward, uint64_t* bytes_out);
 
 /* z = x W^T + b, y = act(z) + r.  x [rows][in], w [out][in] per matrix, bias [out] per matrix (row stride
