@@ -62,3 +62,24 @@ def test_what_is_not_finite_stays_in_its_row_and_column(dense, dtype):  # noqa: 
     assert bool(dx[:-1, :-1].isfinite().all()) and not bool(dx[-1].isfinite().any()) and bool(dx[:, -1].isnan().all())
     assert bool(dw[:-1, :-1].isfinite().all()) and not bool(dw[-1].isfinite().any()) and not bool(dw[:, -1].isfinite().any())
     assert bool(db[:-1].isfinite().all()) and float(db[-1]) == float("-inf")
+
+
+@pytest.mark.parametrize("rows,fin,fout", [(2049, 1025, 1111), (5, 520, 4099)])
+def test_captured_into_a_graph(dense, rows, fin, fout):  # noqa: F811
+    """Copies, parts and the products of them, replayed on new values, with eager calls between the replays."""
+    import torch
+    t, g = torch.bfloat16, gen(rows)
+    x, w, dy = randn(g, t, rows, fin), randn(g, t, fout, fin, scale=fin ** -0.5), randn(g, t, rows, fout)
+    call = lambda: (dense.ps_linear_forward(x, w), *dense.ps_linear_backward(dy, x, w))  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(4):
+        for v in (x, w, dy):
+            v.copy_(randn(g, t, *v.shape, scale=fin ** -0.5))
+        want = [v.clone() for v in call()]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
