@@ -1041,7 +1041,7 @@ void launch_linear_forward(const Product& p, int dtype, bool direct, int tile, h
 void launch_linear_dx(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 void launch_linear_dw(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 
-// Forward pass for few rows, 16 * row_tiles of a group (1, 2 or 4) to a block; tiles_r counts these, tiles_c 16 columns each.
+// Forward pass for few rows, 16 * row_tiles of a group (1 to 4) to a block; tiles_r counts these, tiles_c 16 columns each.
 void launch_linear_few(const Product& p, int dtype, int row_tiles, hipStream_t s);
 // Input gradient for few rows (row_tiles 1 or 2); tiles_c counts 16 * (16 bytes) of columns each, of which there are at least 16 bytes; the
 // contraction in parts of part_stages steps of FEW_DX_STEP / (bytes of a value).

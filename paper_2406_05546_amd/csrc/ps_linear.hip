@@ -230,7 +230,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
     Plan best{};
     const int64_t each = up(l.rows, l.n_groups);
     if (kind == FORWARD && each <= 64) {
-        best.few = each <= 16 ? 1 : each <= 32 ? 2 : 4;
+        best.few = (int)std::max<int64_t>(1, up(each, 16));
         best.parts = 1;
         best.tiles_r = up(l.rows, 16 * best.few) + (one ? 0 : l.n_groups);
         best.tiles_c = up(l.out_features, 16);
