@@ -180,9 +180,11 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const Tensor* __re
     const int64_t from = n ? at : 0;  // lanes past the end read nothing
     load_typed(t.param_type, t.param, from, n, p);
     if (t.bits == 8) {
-        const int64_t block = n ? at / PS_ADAMW_BLOCK : 0;
-        decode8(t.m, from, n, t.m_scale[block], m);
-        decode8(t.v, from, n, t.v_scale[block], v);
+        // Lanes past the end hold zeros, and read no scale: those of a block's other lanes meet them for the largest magnitude, and any
+        // other block's scale may be NaN, or on its way to be written.
+        const int64_t block = at / PS_ADAMW_BLOCK;
+        decode8(t.m, from, n, n ? t.m_scale[block] : 0.f, m);
+        decode8(t.v, from, n, n ? t.v_scale[block] : 0.f, v);
     } else {
         load_part<float>(t.m, from, n, m);
         load_part<float>(t.v, from, n, v);
