@@ -152,9 +152,9 @@ __global__ __launch_bounds__(BIAS_COLS * BIAS_SHARES) void bias_sum_kernel(const
     db[g * db_matrix + c] = from_float<T>(s);
 }
 
-// Adds up the parts of a contraction, in order, and finishes the sums.
+// Adds up the parts of a contraction, in order, and finishes the sums.  (There are parts only where there is one group.)
 template <class T>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int parts, int rows, int cols, Epilogue epi)
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int parts, int rows, int cols, Groups groups, Epilogue epi)
 {
     const int per_row = (cols + 7) / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
         for (int e = 0; e < 8; ++e) v[e] = k ? v[e] + x[e] : x[e];
     }
     float bias[8], residual[8];
-    load_bias<T>(epi, 0, col, n, bias);
+    load_bias<T>(epi, group_matrix(groups, 0), col, n, bias);
     load_residual<T>(epi, row, col, n, residual);
     if (epi.residual)
         finish<T, true>(epi, bias, residual, row, col, n, v);
@@ -477,7 +477,7 @@ void run_product(const ps_linear& l, int kind, bool direct, bool copied, const p
     if (plan.parts > 1) {
         const int64_t threads = up(p.out_cols, 8) * p.out_rows;
         with_type(l.dtype, [&](auto t) {
-            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, epi);
+            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, p.groups, epi);
         });
     }
 }

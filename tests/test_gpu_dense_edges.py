@@ -1,7 +1,7 @@
 """Dense layers and AdamW on the GPU at their edges.  Tolerances are those of test_gpu_dense."""
 import pytest
 
-from tests.test_gpu_dense import dense, gen, randn  # noqa: F401
+from tests.test_gpu_dense import TYPES, check_backward, check_forward, dense, gen, randn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,36 @@ def test_adamw_what_is_not_finite_stays_in_its_block(dense, bad, dtype, rows, co
             assert torch.equal(a[first:], b[first:])
             assert a.dtype == torch.uint8 or bool(a.isfinite().all())
         assert bool(hurt[3][0].isnan() | hurt[3][0].isinf()) and bool(hurt[4][0].isnan() | hurt[4][0].isinf())
+
+
+def matrix(dense, t):  # noqa: F811
+    return dense.ps_matrix(t.data_ptr(), t.stride(-2) if t.dim() > 1 else t.numel(), t.stride(0) if t.dim() > 1 else 0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,fin,fout", [(5, 4096, 200), (128, 4096, 256), (100, 2048, 77), (300, 64, 80)])
+def test_one_group_of_all_rows_on_any_of_several_matrices(dense, dtype, rows, fin, fout):  # noqa: F811
+    """Without offsets, and with the number of the matrix: W and the bias are that matrix's, also where the contraction is cut into parts
+    (the second and third size, in dx the first too)."""
+    import ctypes
+
+    import torch
+    t, g = getattr(torch, dtype), gen(rows + fin)
+    x, w, b = randn(g, t, rows, fin), randn(g, t, 3, fout, fin, scale=fin ** -0.5), randn(g, t, 3, fout)
+    y, z = torch.empty(rows, fout, device="cuda", dtype=t), torch.empty(rows, fout, device="cuda", dtype=t)
+    dy, dx = randn(g, t, rows, fout), torch.empty(rows, fin, device="cuda", dtype=t)
+    dw, db = torch.empty(fout, fin, device="cuda", dtype=t), torch.empty(fout, device="cuda", dtype=t)
+    lib, stream = dense._library(), torch.cuda.current_stream().cuda_stream
+    for number in (2, 0):
+        index = torch.tensor([number], dtype=torch.int32, device="cuda")
+        layer = dense.ps_linear(dense._DTYPES[t], dense.ACTIVATIONS["gelu"], rows, fin, fout, 1, 3, None, index.data_ptr())
+        for backward, operands in ((0, (x, w, b, None, y, z)), (1, (dy, x, w, z, dx, dw, db))):
+            need = ctypes.c_uint64(0)
+            assert lib.ps_linear_workspace_bytes(ctypes.byref(layer), backward, ctypes.byref(need)) == 0
+            ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device="cuda")
+            args = [None if o is None else ctypes.byref(matrix(dense, o)) for o in operands]
+            call = lib.ps_linear_backward if backward else lib.ps_linear_forward
+            assert call(ctypes.byref(layer), *args, ws.data_ptr(), need.value, stream) == 0, lib.ps_dense_last_error()
+            torch.cuda.synchronize()
+        check_forward(y, x, w[number], b[number], None, "gelu", z)
+        check_backward((dx, dw, db), dy, x, w[number], "gelu", z)
