@@ -496,6 +496,10 @@ __device__ __forceinline__ bool tile_of_block(const Product& p, int tiles_r, int
     return true;
 }
 
+// A dimension of a grid has less than 2^32 threads, which are 2^24 blocks of 256: tiles beyond ROW_OF_BLOCKS go along the second one.
+constexpr int ROW_OF_BLOCKS = 1 << 23;
+static_assert(ROW_OF_BLOCKS % LINEAR_XCDS == 0, "every row of blocks begins at the first XCD");
+
 // One tile: its rows, columns and piece of the contraction.
 struct Tile {
     int r0, r_valid, c0, c_valid, k_first, depth, matrix, group, part;
@@ -592,7 +596,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
     int lane = tid & 63;
     const int wr = wave / WC, wc = wave % WC;  // of eight wavefronts, two that share a SIMD have different rows
     Tile tile;
-    int block = blockIdx.x;
+    int block = blockIdx.y * ROW_OF_BLOCKS + blockIdx.x;
     if (!find_tile<BR, BC, BK, RAGGED>(p, tiles_r, block, tile)) return;
     OpR opr;
     OpC opc;
@@ -967,7 +971,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         block_barrier();  // nobody reads what comes, or these sums, take the place of
         bool more = false;
         if constexpr (PERSISTENT) {
-            block += gridDim.x;
+            block += gridDim.x;  // (as many as compute units, in one row)
             more = find_tile<BR, BC, BK, RAGGED>(argument(), tiles_r, block, tile);
             if (FORWARD_PASS && epi.bias) {
 #pragma unroll
@@ -1056,13 +1060,15 @@ template <class T, bool R_KC, bool C_KC, bool DIRECT, int RAGGED>
 void start_linear(const Product& p, int tile, hipStream_t s)
 {
     const int total = (p.tiles_r * p.tiles_c * p.parts + LINEAR_XCDS - 1) / LINEAR_XCDS * LINEAR_XCDS;
-    const dim3 grid(total);
+    const dim3 grid(std::min(total, ROW_OF_BLOCKS), (total + ROW_OF_BLOCKS - 1) / ROW_OF_BLOCKS);  // blocks past the last tile end at once
     if (tile == 0)
         hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 64, 64, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
     else if (tile == 1 || !DIRECT || sizeof(T) == 4)
         hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 128, 128, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
-    else if constexpr (DIRECT && sizeof(T) == 2)
-        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), dim3(linear_persistent(256) ? std::min(total, COMPUTE_UNITS) : total), dim3(512), 0, s, p);
+    else if constexpr (DIRECT && sizeof(T) == 2) {
+        static_assert(linear_persistent(256), "a block for each tile would have to be counted as above");
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), dim3(std::min(total, COMPUTE_UNITS)), dim3(512), 0, s, p);
+    }
 }
 template <bool R_KC, bool C_KC, int RAGGED>
 void start_linear_typed(const Product& p, int dtype, bool direct, int tile, hipStream_t s)

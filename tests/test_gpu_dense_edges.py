@@ -67,3 +67,23 @@ def test_one_group_of_all_rows_on_any_of_several_matrices(dense, dtype, rows, fi
             torch.cuda.synchronize()
         check_forward(y, x, w[number], b[number], None, "gelu", z)
         check_backward((dx, dw, db), dy, x, w[number], "gelu", z)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_more_tiles_than_one_dimension_of_a_grid_holds(dense, dtype):  # noqa: F811
+    """4097 groups of a row each and 262,208 columns: more blocks of 16 columns than a launch has room for, and 17.05 million tiles of 64 x 64,
+    where 2^24 blocks of 256 threads make 2^32 threads."""
+    import torch
+    t, g = getattr(torch, dtype), gen(7)
+    groups, narrow, wide = 4097, 16, 262208
+    offsets = torch.arange(groups + 1, dtype=torch.int32, device="cuda")
+    index = torch.zeros(groups, dtype=torch.int32, device="cuda")
+    x, w = randn(g, t, groups, narrow), randn(g, t, wide, narrow, scale=0.25)
+    y = dense.ps_grouped_linear_forward(x, offsets, w[None], weight_of_group=index)
+    for c in range(0, wide, 16384):
+        check_forward(y[:, c:c + 16384], x, w[c:c + 16384], None, None, "none")
+    del y
+    dy, v = randn(g, t, groups, narrow), randn(g, t, narrow, wide, scale=0.25)
+    dx, _, _ = dense.ps_grouped_linear_backward(dy, torch.empty(groups, wide, device="cuda", dtype=t), offsets, v[None], weight_of_group=index, need_dw=False, need_db=False)
+    for c in range(0, wide, 16384):
+        check_backward((dx[:, c:c + 16384], None, None), dy, x[:, :1], v[:, c:c + 16384], "none", None)
