@@ -236,6 +236,9 @@ struct Operand {
     static_assert(!DIRECT || (KC ? NT / 8 % 32 == 0 && (NT / 8 % EACH == 0 || EACH % (NT / 8) == 0) : NT / PIECES % 16 == 0), "the loads' places differ by the same for every thread");
     static constexpr int SUBS = 2;                            // reads of 16 bytes of k for each of the four lane groups
     static constexpr int READS = KC ? 1 : SIZE == 2 ? 2 : 4;  // LDS instructions of one
+    // RC rows go on beside the tile's last column.  What is there enters only columns that nobody stores; but fp32 sums are all
+    // looked at (those that the split cannot hold are formed again), so there those columns are left out.
+    static constexpr bool CUT = DIRECT && !KC && SIZE == 4;
 
     const char* base;  // of the tile's first row (KC) or column (RC) and the first k of the next stage to be brought
     int64_t step;      // bytes from stage to stage
@@ -243,6 +246,7 @@ struct Operand {
     int32_t left;      // k still to be brought
     int32_t rows;      // KC: valid rows of the tile; RC: valid columns
     uint32_t own_offset;  // byte from `base` of this thread's piece in the first load of the first half; past a row's end NOWHERE
+    int32_t own_column;   // CUT: its first column, in every load of that half
     uintx4 reg[DIRECT ? 1 : LOADS];
 
     static __device__ __forceinline__ int kc_swap(int row)
@@ -280,6 +284,7 @@ struct Operand {
         int line, element;
         place(0, 0, t, line, element);
         own_offset = line * pitch + element * SIZE;
+        if (CUT) own_column = element;
         end_of_row(t);
     }
     static constexpr uint32_t NOWHERE = 0xfffffff0u;  // beyond what any descriptor allows, and so read as zero
@@ -305,7 +310,9 @@ struct Operand {
         place(half, i, 0, line, element);
         const int moved = line * pitch + element * SIZE;  // of thread 0, which is at 0 in the first load of the first half
         const uint64_t from = reinterpret_cast<uint64_t>(base) + (uint32_t)moved;
-        load_to_lds(uintx4{(uint32_t)scalar((int)from), (uint32_t)scalar((int)(from >> 32)) & 0xffffu, (uint32_t)scalar(max(bytes - moved, 0)), 0x00020000u}, own_offset,
+        uint32_t offset = own_offset;
+        if (CUT && own_column + half * EACH >= rows) offset = NOWHERE;  // (columns are multiples of a piece)
+        load_to_lds(uintx4{(uint32_t)scalar((int)from), (uint32_t)scalar((int)(from >> 32)) & 0xffffu, (uint32_t)scalar(max(bytes - moved, 0)), 0x00020000u}, offset,
                     tile + i * NT * 16);
     }
     // All of it

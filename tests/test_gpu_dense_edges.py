@@ -87,3 +87,20 @@ def test_more_tiles_than_one_dimension_of_a_grid_holds(dense, dtype):  # noqa: F
     dx, _, _ = dense.ps_grouped_linear_backward(dy, torch.empty(groups, wide, device="cuda", dtype=t), offsets, v[None], weight_of_group=index, need_dw=False, need_db=False)
     for c in range(0, wide, 16384):
         check_backward((dx[:, c:c + 16384], None, None), dy, x[:, :1], v[:, c:c + 16384], "none", None)
+
+
+@pytest.mark.parametrize("beside", [float("nan"), 1e38])
+@pytest.mark.parametrize("rows,fin,fout", [(300, 100, 72), (1030, 136, 260), (1030, 135, 263)])
+def test_what_lies_beside_an_operand_changes_nothing(dense, beside, rows, fin, fout):  # noqa: F811
+    """fp32 operands that are views of wider rows: their products have the same bytes whatever the columns beside them hold."""
+    import torch
+    g = gen(rows + fin)
+    values = [randn(g, torch.float32, rows, fin), randn(g, torch.float32, fout, fin), randn(g, torch.float32, rows, fout)]
+    runs = []
+    for fill in (0.0, beside):
+        wide = [torch.full((v.shape[0], v.shape[1] + 300), fill, device="cuda") for v in values]
+        x, w, dy = [b[:, 60:60 + v.shape[1]].copy_(v) for b, v in zip(wide, values)]
+        runs.append((dense.ps_linear_forward(x, w), *dense.ps_linear_backward(dy, x, w)))
+    check_forward(runs[1][0], values[0], values[1], None, None, "none")
+    check_backward(runs[1][1:], values[2], values[0], values[1], "none", None)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
