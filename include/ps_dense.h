@@ -67,7 +67,8 @@ PS_API ps_status ps_linear_workspace_bytes(const ps_linear* layer, int32_t backw
 /* z = x W^T + b, y = act(z) + r.  x [rows][in], w [out][in] per matrix, bias [out] per matrix (row stride
  * not used), residual, y and pre [rows][out]; bias, residual and pre may be NULL.  pre receives z, which
  * the backward pass of an activation reads.  y may be the residual itself; no other output may overlap
- * an input or another output.  Sums are held in 32 bits, y and pre are rounded once. */
+ * an input or another output.  Sums are held in 32 bits, y and pre are rounded once.  (fp32 operands below
+ * 2^-134, which hold 15 bits or fewer, may count as 0 in a sum that they change by less than 2^-80.) */
 PS_API ps_status ps_linear_forward(const ps_linear* layer, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias,
                                    const ps_matrix* residual, const ps_matrix* y, const ps_matrix* pre,
                                    void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);

@@ -670,8 +670,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Splitting takes
             // 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
             // instructions for each of the products that they enter.  4096^3: 685-750 us, six bf16 products at 1.1-1.2 PFLOP/s, of the
-            // 1.3-1.4 that a bf16 product of such sizes gets from this chip's power; fp32 matrix instructions: 1050.  A block whose sums the split may not hold (ps_split.h: not finite, or
-            // not zero and below 2^-80) forms them all again with fp32 matrix instructions.
+            // 1.3-1.4 that a bf16 product of such sizes gets from this chip's power; fp32 matrix instructions: 1050.  A block whose sums the split may not hold forms them all again with
+            // fp32 matrix instructions: sums that are not finite, and those that are small next to what operands may have lost.  Parts are multiples
+            // of 2^-133 (ps_split.h), so each product is off by at most 2^-133 of the largest operand that the wavefront meets (`top`), and a
+            // sum of `depth` products that is 2^-109 depth top or more by 2^-24 of it; a sum of 0, where all of it may be lost, stands
+            // if that is below 2^-80.  The largest takes four instructions beside the 44 (4096^3 651-673 -> 677-704 us).
+            float top = 0.f;
             auto pass = [&](auto form) __attribute__((always_inline)) {
                 constexpr bool exact = decltype(form)::value;
                 auto products = [&](const char* r, const char* c) __attribute__((always_inline)) {
@@ -687,10 +691,13 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
                             for (int h = 0; h < HALVES * HALVES; ++h) multiply(h / HALVES, h % HALVES, sub, h % HALVES);
                         }
                     } else {
-                        auto parts = [](const uintx4& x, const uintx4& y) __attribute__((always_inline)) {
+                        auto parts = [&](const uintx4& x, const uintx4& y) __attribute__((always_inline)) {
                             float v[8];
 #pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? x[e] : y[e - 4]);
+#pragma unroll
+                            for (int e = 0; e < 8; e += 2) top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, fabsf(v[e])), fabsf(v[e + 1]));
+                            asm volatile("" : "+v"(top));  // now: left to the stage's end it would keep all operands in registers
                             return split8(v);
                         };
                         auto of_c = [&](int j, int sub) __attribute__((always_inline)) { return OpC::fetch(c + j / HC * OpC::HBYTES, wc, j % HC, sub, lane); };
@@ -794,6 +801,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             };
             clear(small);
             pass(std::false_type{});
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, off, 64));
+            const float reach = top * (float)tile.depth, least = fmaxf(SPLIT_TINY, reach * 0x1p-109f);  // (NaN only where sums are)
+            const bool zero_too = reach >= 0x1p53f;
             bool lost = false;
 #pragma unroll
             for (int i = 0; i < TR; ++i)
@@ -803,7 +814,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float m = fabsf(acc[i][j][e]);
-                        lost |= !(m < INFINITY) || (m < SPLIT_TINY && m > 0.f);
+                        lost |= !(m < INFINITY) || (m < least && (m > 0.f || zero_too));
                     }
                 }
             if (__syncthreads_or(lost)) {

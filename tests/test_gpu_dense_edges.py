@@ -104,3 +104,28 @@ def test_what_lies_beside_an_operand_changes_nothing(dense, beside, rows, fin, f
     check_forward(runs[1][0], values[0], values[1], None, None, "none")
     check_backward(runs[1][1:], values[2], values[0], values[1], "none", None)
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+# magnitudes of the two operands of a product; the third: every second row of the first is as large as makes ordinary products, 1 at most
+EXTREMES = [(1.2e-37, 1e30, False), (1e30, 1.2e-37, False), (3e-37, 1e35, True), (1e-41, 1e37, False), (1e-42, 3e37, True), (1e-15, 1e-15, False), (1e-12, 3e-18, True)]
+
+
+@pytest.mark.parametrize("rows,fin,fout", [(40, 64, 96), (200, 64, 96), (333, 200, 135), (700, 1025, 260)])
+@pytest.mark.parametrize("a,b,mixed", EXTREMES)
+def test_fp32_operands_of_extreme_sizes(dense, a, b, mixed, rows, fin, fout):  # noqa: F811
+    """Products of ordinary size, of fp32 operands that the split into three bf16 parts does not hold in all their bits, or at all, and sums that
+    are tiny: as exact as any others.  (Inputs and what is expected are made on the CPU, which keeps subnormal numbers.)"""
+    import torch
+    g = torch.Generator()
+    g.manual_seed(rows + fin)
+    def values(n, k, size, some=False):  # noqa: E306
+        v = torch.randn(n, k, generator=g) * size
+        if some:
+            v[::2] = torch.randn(v[::2].shape, generator=g) * min(1.0, 1 / b)
+        return v.cuda()
+    x, w = values(rows, fin, a, mixed), values(fout, fin, b)
+    y = dense.ps_linear_forward(x, w)
+    check_forward(y.cpu(), x.cpu(), w.cpu(), None, None, "none")
+    dy, v, u = values(rows, fout, a, mixed), values(fout, fin, b), values(rows, fin, b)
+    dx, dw, _ = dense.ps_linear_backward(dy, u, v, need_db=False)
+    check_backward((dx.cpu(), dw.cpu(), None), dy.cpu(), u.cpu(), v.cpu(), "none", None)
