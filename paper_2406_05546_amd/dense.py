@@ -239,7 +239,8 @@ def ps_grouped_linear_backward(dy, x, offsets, w, activation: str = "none", pre=
 
 @dataclass
 class AdamW:
-    """Handle of one table of tensors, and what it refers to: the weights, gradients and states stay alive with it."""
+    """Handle of one table of tensors, and what it refers to: the weights, gradients and states stay alive with it.  Steps may run on any
+    stream (the caller orders them); a handle that is dropped may leave steps behind that still run."""
     handle: ctypes.c_void_p
     device: object
     state_bits: int
@@ -252,6 +253,7 @@ class AdamW:
     copies: List[object]
     workspace: object = None
     rows: int = 1                    # gradient rows that every tensor has
+    streams: set = field(default_factory=set)  # those on which the allocator knows all of these to be used
     options: ps_adamw_options = field(default_factory=ps_adamw_options)
     closed: bool = field(default=False)
 
@@ -317,12 +319,13 @@ def ps_adamw_create(params: Sequence, grads: Sequence, state_bits: int = 32, wei
     size = ctypes.c_uint64(0)
     handle = ctypes.c_void_p()
     with torch.cuda.device(device):
+        stream = torch.cuda.current_stream(device).cuda_stream
         _check(call, lib.ps_adamw_workspace_bytes(table, n, ctypes.byref(size)))
         ws = torch.empty(size.value, dtype=torch.uint8, device=device)
         _check(call, lib.ps_adamw_create(ctypes.byref(handle), table, n, ctypes.c_void_p(ws.data_ptr()), size.value,
-                                         ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
+                                         ctypes.c_void_p(stream)))
     return AdamW(handle, device, state_bits, params, grads, states["m"], states["v"], states["m_scale"], states["v_scale"], copies, ws,
-                 min(t.grad_rows for t in table))
+                 min(t.grad_rows for t in table), {stream})
 
 
 def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
@@ -335,9 +338,17 @@ def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: f
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return ps_adamw_step(opt, step, lr, beta1, beta2, eps, grad_scale, n_rows)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if stream not in opt.streams:
+        # what the handle keeps may be freed with it while this step runs: not for use on its own stream before that
+        current = torch.cuda.current_stream(index)
+        for t in (opt.workspace, *opt.params, *opt.grads, *opt.m, *opt.v, *opt.m_scale, *opt.v_scale, *opt.copies):
+            if t is not None:
+                t.record_stream(current)
+        opt.streams.add(stream)
     o = opt.options
     o.lr, o.beta1, o.beta2, o.eps, o.grad_scale, o.step, o.n_rows = lr, beta1, beta2, eps, grad_scale, step, opt.rows if n_rows is None else n_rows
-    st = _library().ps_adamw_step(opt.handle, ctypes.byref(o), torch._C._cuda_getCurrentRawStream(index))
+    st = _library().ps_adamw_step(opt.handle, ctypes.byref(o), stream)
     if st != PS_OK:
         _check(call, st)
 

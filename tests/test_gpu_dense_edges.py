@@ -129,3 +129,25 @@ def test_fp32_operands_of_extreme_sizes(dense, a, b, mixed, rows, fin, fout):  #
     dy, v, u = values(rows, fout, a, mixed), values(fout, fin, b), values(rows, fin, b)
     dx, dw, _ = dense.ps_linear_backward(dy, u, v, need_db=False)
     check_backward((dx.cpu(), dw.cpu(), None), dy.cpu(), u.cpu(), v.cpu(), "none", None)
+
+
+def test_a_handle_dropped_while_a_step_runs_on_another_stream(dense):  # noqa: F811
+    """Its table and states are not given out again on the stream where they were made before that step is done."""
+    import torch
+    n = 3_000_017
+    start, grad = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    want, got = start.clone(), start.clone()
+    dense.ps_adamw_step(dense.ps_adamw_create([want], [grad], state_bits=8), 1, 0.1)
+    opt = dense.ps_adamw_create([got], [grad], state_bits=8)
+    own = [opt.workspace, opt.m[0], opt.v[0], opt.m_scale[0], opt.v_scale[0]]
+    places, sizes = {t.data_ptr() for t in own}, [t.numel() * t.element_size() for t in own]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)  # a tenth of a second: a step that waits for its turn
+        dense.ps_adamw_step(opt, 1, 0.1)
+    del opt, own
+    others = [torch.full((b,), 255, dtype=torch.uint8, device="cuda") for b in sizes]
+    assert not places & {t.data_ptr() for t in others}
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
