@@ -124,6 +124,7 @@ class _Arguments(threading.local):
     def __init__(self):
         self.memory = ctypes.create_string_buffer(_LAYER_BYTES + 7 * _MATRIX_BYTES)
         self.need = ctypes.c_uint64(0)
+        self.options = ps_adamw_options()
         self.at = ctypes.addressof(self.memory)
         self.at_need = ctypes.addressof(self.need)
         self.at_matrices = [self.at + _LAYER_BYTES + i * _MATRIX_BYTES for i in range(7)]
@@ -254,7 +255,6 @@ class AdamW:
     workspace: object = None
     rows: int = 1                    # gradient rows that every tensor has
     streams: set = field(default_factory=set)  # those on which the allocator knows all of these to be used
-    options: ps_adamw_options = field(default_factory=ps_adamw_options)
     closed: bool = field(default=False)
 
     def __del__(self):
@@ -346,7 +346,7 @@ def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: f
             if t is not None:
                 t.record_stream(current)
         opt.streams.add(stream)
-    o = opt.options
+    o = _arguments.options
     o.lr, o.beta1, o.beta2, o.eps, o.grad_scale, o.step, o.n_rows = lr, beta1, beta2, eps, grad_scale, step, opt.rows if n_rows is None else n_rows
     st = _library().ps_adamw_step(opt.handle, ctypes.byref(o), stream)
     if st != PS_OK:

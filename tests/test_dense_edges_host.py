@@ -51,3 +51,28 @@ def test_a_step_on_another_stream_is_known_to_the_allocator(stand_in):
     for stand_in.now in (9, 9, 7, 11):
         dense.ps_adamw_step(opt, 1, 0.1)
     assert all(t.streams == ["stream 9", "stream 11"] for t in kept)
+
+
+def test_two_threads_step_one_table_each_with_its_own_options(stand_in):
+    """Each call reads what its thread asked for, although the other thread calls in between."""
+    both, seen = threading.Barrier(2, timeout=20), {}
+
+    class Waits(Library):
+        def ps_adamw_step(self, handle, options, stream):
+            both.wait()  # both calls have written their options
+            seen[threading.get_ident()] = (options._obj.lr, options._obj.step, options._obj.n_rows)
+            both.wait()
+            return 0
+    stand_in.library = Waits()
+    opt, _ = table(7)
+    opt.rows, asked = 5, {}
+
+    def step(lr, number, rows):
+        asked[threading.get_ident()] = (lr, number, 5 if rows is None else rows)
+        dense.ps_adamw_step(opt, number, lr, n_rows=rows)
+    threads = [threading.Thread(target=step, args=a) for a in ((0.25, 3, 2), (0.5, 4, None))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert seen == asked and len(seen) == 2
