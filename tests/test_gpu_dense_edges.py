@@ -151,3 +151,33 @@ def test_a_handle_dropped_while_a_step_runs_on_another_stream(dense):  # noqa: F
     assert not places & {t.data_ptr() for t in others}
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_groups_than_are_counted_beforehand(dense, dtype):  # noqa: F811
+    """1300 groups, beyond the 1024 whose tiles the kernels count, a third of them empty and one of them large: forward and all gradients."""
+    import torch
+    t, g = getattr(torch, dtype), gen(9)
+    sizes = [(0, 3, 5)[i % 3] if i != 700 else 2000 for i in range(1300)]
+    edges = [0]
+    for n in sizes:
+        edges.append(edges[-1] + n)
+    rows, fin, fout = edges[-1], 40, 24
+    offsets = torch.tensor(edges, dtype=torch.int32, device="cuda")
+    index = torch.tensor([i % 3 for i in range(len(sizes))], dtype=torch.int32, device="cuda")
+    x, w, b, dy = randn(g, t, rows, fin), randn(g, t, 3, fout, fin, scale=fin ** -0.5), randn(g, t, 3, fout), randn(g, t, rows, fout)
+    z = torch.empty(rows, fout, device="cuda", dtype=t)
+    y = dense.ps_grouped_linear_forward(x, offsets, w, b, None, "silu", index, pre=z)
+    dx, dw, db = dense.ps_grouped_linear_backward(dy, x, offsets, w, "silu", z, index)
+    group = torch.repeat_interleave(torch.arange(len(sizes), device="cuda"), torch.tensor(sizes, device="cuda"))
+    for k in range(3):
+        r = (group % 3 == k).nonzero().squeeze(1)
+        if len(r):
+            check_forward(y[r], x[r], w[k], b[k], None, "silu", z[r])
+            check_backward((dx[r], None, None), dy[r], x[r], w[k], "silu", z[r])
+    for i in (0, 1, 2, 3, 699, 700, 701, 1023, 1024, 1025, 1297, 1298, 1299):
+        s = slice(edges[i], edges[i + 1])
+        if sizes[i]:
+            check_backward((None, dw[i], db[i]), dy[s], x[s], w[i % 3], "silu", z[s])
+    empty = torch.tensor(sizes, device="cuda") == 0
+    assert bool((dw[empty] == 0).all()) and bool((db[empty] == 0).all()) and bool((dw[~empty] != 0).flatten(1).any(1).all())

@@ -109,3 +109,37 @@ def test_a_buffer_of_one_gradient(mlp):
     loss = server.work(torch.ones(4, 8).cuda(), torch.tensor([0, 1, 2, 0]).cuda(), offsets, version)
     assert loss.shape == (1,) and server.apply(1e-3) == 1
     server.close()
+
+
+def test_an_outage_leaves_the_weights_alone_and_piles_gradients_up(mlp, monkeypatch):
+    """Rounds 3 to 5 without the server: the buffer grows by a gradient for each worker, master weights, published weights and versions keep
+    their bytes, and the first round after takes all that piled up in one step."""
+    import torch
+    log, servers = [], []
+
+    class Watched(mlp.MlpServer):
+        def __init__(self, *a, **k):
+            super().__init__(*a, **k)
+            servers.append(self)
+
+        def work(self, *a):
+            before = [t.clone() for t in (self.master, self.fresh, self.versions)]
+            loss = super().work(*a)
+            assert all(torch.equal(t, b) for t, b in zip((self.master, self.fresh, self.versions), before))
+            log.append(("work", self.pending, before))
+            return loss
+
+        def apply(self, lr, mean=True):
+            n = super().apply(lr, mean)
+            log.append(("apply", n, self.steps))
+            return n
+    monkeypatch.setattr(mlp, "MlpServer", Watched)
+    workers, down = 6, range(3, 6)
+    mlp.train(rounds=8, down=down, workers=workers, batch=8, widths=(32, 48, 5))
+    rounds = [e for e in log if e[0] == "work"]
+    assert [e[1] for e in rounds] == [workers * n for n in (1, 1, 1, 1, 2, 3, 4, 1)]
+    assert [e[1:] for e in log if e[0] == "apply"] == [(workers, 1), (workers, 2), (workers, 3), (4 * workers, 4), (workers, 5)]
+    for r in range(8):
+        same = [torch.equal(a, b) for a, b in zip(rounds[r][2], rounds[r - 1][2])] if r else [False]
+        assert all(same) if r in range(4, 7) else not any(same[:2])
+    assert len(servers) == 1
