@@ -222,6 +222,28 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Blocks of 512 threads in a launch, which has less than 2^32 threads.
 constexpr int64_t FEW_BLOCKS = 1 << 23;
 
+// Whether the forward pass takes the kernel for few rows, `each` in a group.  Each of its blocks, 16 columns, reads all rows of its
+// group over the whole contraction; tiles read them once for 64 columns or more, and cut the contraction of one group into parts.  So it
+// is the faster one up to about so many values for each compute unit.  us, this kernel against tiles (bf16 if not said):
+//   one group      4096 -> 4096   16 rows 11.5, 16.9   24 14.8, 15.6   32 16.4, 15.9   64 24.0, 16.9   fp32 24 27.5, 28.6   48 37.3, 33.0
+//                  1024 -> 16384   1 8.4, 14.9   24 14.3, 15.2   32 16.3, 15.4   64 24.2, 15.5   4096 -> 16384   4 27.6, 30.0   16 36.7, 31.3
+//                  1024 -> 1024   64 7.3, 10.6   2048 -> 512   48 9.8, 9.9   64 11.6, 9.9   512 -> 8192   64 9.1, 9.2
+//   deep, narrow   16384 -> 512    1 23.3, 19.3   fp32 8192 -> 512   1 35.6, 21.3   8192 -> 2048   1 38.5, 33.7
+//   odd rows       1111 -> 2777   48 12.9, 13.6   64 15.6, 13.7   4097 -> 4099   1 20.2, 18.7   4 29.3, 19.4   (32 bits:   12 29.2, 36.8)
+//   groups         64 of 2048 -> 1024   8 rows each 61, 70   16 74, 69   64 172, 71   all 4096 rows in one 152, 28   fp32 8 136, 148
+//                  16 of them   32 30.5, 29.3   48 37.5, 29.6   2 of 4096 -> 4096   64 45, 51   64 of 512 -> 512   4 11.8, 12.0   16 15.1, 12.4
+//                  fp32 63 of 960 -> 4352   2 224, 296
+bool few_rows(const ps_linear& l, int64_t each)
+{
+    if (each > 64) return false;
+    if (l.offsets_dev) return each <= 4 || l.rows * l.out_features <= 1 << 19;
+    const int size = dtype_size(l.dtype);
+    const int64_t values = l.in_features * std::max<int64_t>(l.out_features, 4096) / 4096;  // of one row, to a compute unit
+    if (l.out_features < 4096 && l.in_features * size > 16384) return false;
+    if (size == 2 && l.in_features % 8) return (each + 16) * values <= 73728;
+    return each * values <= 98304;
+}
+
 Plan plan_product(const ps_linear& l, int kind, bool direct)
 {
     const int64_t rows = kind == DW ? l.out_features : l.rows, cols = kind == FORWARD ? l.out_features : l.in_features;
@@ -229,7 +251,7 @@ Plan plan_product(const ps_linear& l, int kind, bool direct)
     const bool one = !l.offsets_dev;
     Plan best{};
     const int64_t each = up(l.rows, l.n_groups);
-    if (kind == FORWARD && each <= 64) {
+    if (kind == FORWARD && few_rows(l, each)) {
         best.few = (int)std::max<int64_t>(1, up(each, 16));
         best.parts = 1;
         best.tiles_r = up(l.rows, 16 * best.few) + (one ? 0 : l.n_groups);

@@ -181,3 +181,27 @@ def test_more_groups_than_are_counted_beforehand(dense, dtype):  # noqa: F811
             check_backward((None, dw[i], db[i]), dy[s], x[s], w[i % 3], "silu", z[s])
     empty = torch.tensor(sizes, device="cuda") == 0
     assert bool((dw[empty] == 0).all()) and bool((db[empty] == 0).all()) and bool((dw[~empty] != 0).flatten(1).any(1).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_forward_on_both_sides_of_the_limits_for_few_rows(dense, dtype):  # noqa: F811
+    """One group: rows times features, narrow results of deep contractions, rows that are no multiples of 16 bytes; groups: rows times columns, evenly
+    spread or all in one group."""
+    import torch
+    t, g = getattr(torch, dtype), gen(11)
+    for rows, fin, fout in ((24, 4096, 200), (25, 4096, 200), (64, 1536, 72), (64, 1544, 72), (2, 4096, 64), (2, 4104, 64), (2, 8200, 64), (2, 8200, 4096), (6, 4096, 16400),
+                            (50, 1111, 96), (51, 1111, 96), (1, 4097, 300), (3, 4097, 300)):
+        x, w, b, r = randn(g, t, rows, fin), randn(g, t, fout, fin, scale=fin ** -0.5), randn(g, t, fout), randn(g, t, rows, fout)
+        z = torch.empty(rows, fout, device="cuda", dtype=t)
+        check_forward(dense.ps_linear_forward(x, w, b, r, "gelu", pre=z), x, w, b, r, "gelu", z)
+    groups, fin, fout = 16, 72, 2056
+    w, b = randn(g, t, groups, fout, fin, scale=fin ** -0.5), randn(g, t, groups, fout)
+    for each in (4, 5, 15, 16, 40):
+        for sizes in ([each] * groups, [0] * 7 + [each * groups] + [0] * 8):
+            edges = [sum(sizes[:i]) for i in range(groups + 1)]
+            x = randn(g, t, edges[-1], fin)
+            y = dense.ps_grouped_linear_forward(x, torch.tensor(edges, dtype=torch.int32, device="cuda"), w, b, None, "relu")
+            for i in range(groups):
+                if sizes[i]:
+                    s = slice(edges[i], edges[i + 1])
+                    check_forward(y[s], x[s], w[i], b[i], None, "relu")
