@@ -15,7 +15,8 @@
  * (a hipStream_t, NULL for the default stream) of the current device and is asynchronous, and the
  * caller orders it against work on other streams.  No call depends on what an earlier one left in a
  * workspace, and two calls may overlap if their workspaces and outputs differ.  Every call but
- * ps_adamw_create can be captured into a graph.  Results do not depend on timing: nothing is summed
+ * ps_adamw_create can be captured into a graph (a captured step repeats its number, rates and scale on every
+ * replay, and needs its handle's workspace as long).  Results do not depend on timing: nothing is summed
  * by atomics.  ps_dense_last_error() gives a message for the calling thread's last failing call.
  */
 #ifndef PS_DENSE_H

@@ -10,8 +10,9 @@
 // (v_mfma_f32_16x16x32_bf16 / _f16, v_mfma_f32_16x16x4_f32) with C as the instruction's first operand, so that a lane
 // gets consecutive columns of one row of the result.
 //
-// Bound by the matrix cores (and the chip's power) where rows are many: bf16 8192^3 1380-1410 TFLOP/s in all three kinds, the
-// library's product of two row-major matrices 1320, of their transposed forms 1150 and 1020; by memory where they are few.
+// Bound by the matrix cores (and the chip's power) where rows are many: bf16 8192^3 1340-1410 TFLOP/s in all three kinds, the
+// library's product of rows with rows 1330-1570 (the first and the third ten one after the other), of its two transposed forms
+// 1170-1360 and 1040-1180; by memory where they are few.
 #pragma once
 #include "ps_dense.h"
 #include "ps_split.h"
@@ -120,9 +121,10 @@ __device__ __forceinline__ bool find_rows(const Groups& gs, int tile, int size, 
 // ---------------------------------------------------------------------------------------------------------------
 // Activations
 
-// The normal distribution at z: the smaller of Phi(z) and 1 - Phi(z), to 5e-7 of it however small, and exp(-z^2 / 2).  With
-// t = 1 / (1 + c |z|), exp(z^2 / 2) (1 - Phi(|z|)) is t times a polynomial in t, fitted to 9.2e-8 of the value for |z| up to 13.1
-// (beyond, both are below the smallest number).  The library's erfc takes five times as long, and with it the
+// The normal distribution at z: the smaller of Phi(z) and 1 - Phi(z), and exp(-z^2 / 2).  With
+// t = 1 / (1 + c |z|), exp(z^2 / 2) (1 - Phi(|z|)) is t times a polynomial in t, which with the coefficients as they stand is off by
+// at most 2.0e-7 of the value for |z| up to 13.1 (beyond, both are below the smallest number).  The tail is measured to 5.4e-7 of it for |z| up
+// to 2 and, as the exponent's rounding makes z^2 2^-24 of it, to 1.6e-6 at 5, 5.3e-6 at 10 and 7.7e-6 at 13.  The library's erfc takes five times as long, and with it the
 // 256 x 256 tiles of a GELU layer spent a fifth of their time here.
 struct NormalTail {
     float tail, bell;
@@ -203,7 +205,8 @@ struct Mma<float> {
 // ---------------------------------------------------------------------------------------------------------------
 // 16 bytes for every lane from memory straight to LDS, one behind the other from `to` on (the same for all lanes).  Written as
 // it is and not by its builtin, because the compiler has every transposing LDS read wait for all such loads that it knows of;
-// it has no result that could be overwritten, and whoever reads what it brings waits for vmcnt himself.
+// it has no result that could be overwritten, and whoever reads what it brings waits for vmcnt himself.  (m0 cannot be named
+// as changed: it is reserved, and the compiler sets it before each use of its own, of which there are none here.)
 __device__ __forceinline__ void load_to_lds(uintx4 descriptor, uint32_t offset, int to)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(descriptor), "s"(to) : "memory");
@@ -669,7 +672,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
             // fp32 products on the bf16 matrix instructions, operands split in three (ps_split.h), which are read as they are and split
             // by every wavefront that uses them: a column once a stage, a row's parts where they are used.  Splitting takes
             // 44 instructions, 176 cycles, for eight k of 16 rows, next to 96 cycles of matrix
-            // instructions for each of the products that they enter.  4096^3: 685-750 us, six bf16 products at 1.1-1.2 PFLOP/s, of the
+            // instructions for each of the products that they enter.  4096^3: 677-735 us, six bf16 products at 1.1-1.2 PFLOP/s, of the
             // 1.3-1.4 that a bf16 product of such sizes gets from this chip's power; fp32 matrix instructions: 1050.  A block whose sums the split may not hold forms them all again with
             // fp32 matrix instructions: sums that are not finite, and those that are small next to what operands may have lost.  Parts are multiples
             // of 2^-133 (ps_split.h), so each product is off by at most 2^-133 of the largest operand that the wavefront meets (`top`), and a

@@ -1,7 +1,7 @@
 // Forward pass and input gradient for few rows (a token, a few sequences, few rows of each of many groups): bound by reading the weights
 // once, so these go straight to registers, and all wavefronts of a block read the same 16 columns' weights, each its share
-// of k.  bf16: 64 matrices of 2048 -> 1024 and 96 rows 44 us (6.1 TB/s), one row 4096 -> 4096 8.0 us (4.2 TB/s: of a launch
-// this short two trips to memory are half).
+// of k.  bf16: 64 matrices of 2048 -> 1024 and 96 rows 44 us (6.1 TB/s), one row 4096 -> 4096 7.8 us (4.3 TB/s: in a launch
+// this short the trips to memory that wait for each other, bias, residual and the first weights, are a good part).
 #include "ps_linear.h"
 
 namespace ps {
@@ -29,7 +29,8 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(Product p)
 #pragma unroll
     for (int i = 0; i < TR; ++i) r[i] = static_cast<const T*>(p.r) + (int64_t)min(r0 + 16 * i + l, rows.end - 1) * p.r_row;
 
-    // lane (q, l) of wavefront w finishes row l of row tile w, columns 4q .. 4q + 3; what is added to them is asked for first
+    // lane (q, l) of wavefront w finishes row l of row tile w, columns 4q .. 4q + 3.  What is added to them is read first, and
+    // waited for: it is converted in the branch that loads it.
     const int row = r0 + 16 * wave + l, col = c0 + 4 * q, valid = wave < TR && row < rows.end ? p.cols - col : 0;
     float bias[4], residual[4];
     load_bias<T>(p.epi, matrix, col, valid, bias);

@@ -1,7 +1,7 @@
 """ctypes binding of the dense-layer and optimizer operators of libps_hotpath.so (include/ps_dense.h): same names,
 argument checks and marshalling only.  Tensors are torch cuda tensors; work runs on torch's current stream of their device, and results
 and workspaces come from torch's allocator on that stream.  There is no fallback: a missing library or a refused call
-raises an exception."""
+raises an exception.  Nothing is recorded for autograd, also where tensors require gradients: the backward passes are calls of their own."""
 from __future__ import annotations
 
 import ctypes
@@ -330,7 +330,8 @@ def ps_adamw_create(params: Sequence, grads: Sequence, state_bits: int = 32, wei
 
 def ps_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
                   n_rows: Optional[int] = None) -> None:
-    """Step number `step` (from 1) with the sum of the first n_rows gradient rows (all that every tensor has, if not given)."""
+    """Step number `step` (from 1) with the sum of the first n_rows gradient rows (all that every tensor has, if not given).  Captured into a graph,
+    every replay repeats this step's number and rates, and the handle has to be kept for as long."""
     call = "ps_adamw_step"
     if opt.closed:
         _refuse(call, "the table was destroyed")
