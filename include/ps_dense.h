@@ -6,6 +6,8 @@
  *                 many (workers), each group on a weight matrix of its own or on the version it last
  *                 pulled; every group's gradients land where the caller wants them, for instance in its
  *                 row of the server's gradient buffer.
+ *   ps_checkpoint_*  activations kept in 8 bits for the backward pass: codes and a scale for every 32 columns
+ *                 of a row; ps_linear_*_checkpoint write the pre-activations so, and read them and the inputs.
  *   ps_adamw_*    one AdamW step over many tensors in one launch, the gradient being the sum of the
  *                 buffered rows, states in 32 bits or in 8.
  *
@@ -81,6 +83,40 @@ PS_API ps_status ps_linear_forward(const ps_linear* layer, const ps_matrix* x, c
 PS_API ps_status ps_linear_backward(const ps_linear* layer, const ps_matrix* dy, const ps_matrix* x, const ps_matrix* w,
                                     const ps_matrix* pre, const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db,
                                     void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
+
+/* Activations [rows][cols] in 8 bits.  Columns 32 b .. 32 b + 31 of a row are a block: value = code * scale, codes e4m3 (one byte
+ * each, as float8_e4m3fn) at codes_dev[r * row + c], scales powers of two (one byte s each for 2^(s - 127), as float8_e8m0fnu,
+ * 1 .. 254) at scales_dev[r * scale_row + b]; strides in bytes, any alignment.  Encoding takes the smallest scale from 2^-126
+ * on with which the block's largest finite magnitude is at most 448 and rounds to the nearest code, ties to even; but what
+ * is not 0 becomes the least code of its sign at the lowest (so a ReLU passes its gradient where it did), and what is not
+ * finite becomes NaN, the block's other values staying what they are. */
+typedef struct {
+    void *codes_dev, *scales_dev;
+    int64_t row, scale_row;
+} ps_checkpoint;
+
+#define PS_CHECKPOINT_BLOCK 32
+
+/* to = codes of x, and x = act(values of from); x [rows][cols] of dtype.  Nothing may overlap. */
+PS_API ps_status ps_checkpoint_encode(int32_t dtype, int64_t rows, int64_t cols, const ps_matrix* x, const ps_checkpoint* to, void* hip_stream);
+PS_API ps_status ps_checkpoint_decode(int32_t dtype, int64_t rows, int64_t cols, const ps_checkpoint* from, int32_t activation,
+                                      const ps_matrix* x, void* hip_stream);
+
+/* The layer's forward pass with z, rounded to the layer's type, kept in 8 bits. */
+PS_API ps_status ps_linear_forward_checkpoint(const ps_linear* layer, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias,
+                                              const ps_matrix* residual, const ps_matrix* y, const ps_checkpoint* pre, void* workspace_dev,
+                                              uint64_t workspace_bytes, void* hip_stream);
+
+/* The layer's backward pass with its input and its pre-activations as they are (x, pre) or, where x8 or pre8 is there, from 8
+ * bits.  What is read of x8 is x_activation of its values, rounded to the layer's type: PS_ACT_NONE where the input was kept, the activation
+ * of the layer before where that layer's pre-activations were. */
+PS_API ps_status ps_linear_backward_checkpoint(const ps_linear* layer, const ps_matrix* dy, const ps_matrix* x, const ps_checkpoint* x8,
+                                               int32_t x_activation, const ps_matrix* w, const ps_matrix* pre, const ps_checkpoint* pre8,
+                                               const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db, void* workspace_dev,
+                                               uint64_t workspace_bytes, void* hip_stream);
+
+/* Device bytes that these two need; x_in_8_bits: whether the backward call has an x8 to make dw from. */
+PS_API ps_status ps_linear_checkpoint_workspace_bytes(const ps_linear* layer, int32_t backward, int32_t x_in_8_bits, uint64_t* bytes_out);
 
 /* One tensor of an AdamW step.  The gradient of element i is the sum over the buffered rows k, in order,
  * of grad[k * grad_row + i].  States: 32 bits: m and v are float [numel].  8 bits: m and v hold e4m3

@@ -1,0 +1,102 @@
+// Activations kept in 8 bits (include/ps_dense.h): e4m3 codes, 32 columns of a row sharing a power of two as their scale.
+//
+// Powers of two cost no precision, only up to one binade of range, and what a code stands for is a value of every type here
+// (bf16 always, fp16 in its range) without another rounding.  A lane holds eight consecutive columns, so a block is four lanes.
+#pragma once
+#include "ps_dense.h"
+
+namespace ps {
+
+constexpr int CHECKPOINT_LANES = PS_CHECKPOINT_BLOCK / 8;
+
+#if defined(__HIPCC__)
+
+// The largest over the four lanes of a quad, all of which take part.
+__device__ __forceinline__ uint32_t largest_of_quad(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));  // lanes 1, 0, 3, 2
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));  // lanes 2, 3, 0, 1
+}
+
+// The codes of a lane's eight values and the block's scale (2^(scale - 127)).  Columns that are not there are 0.
+__device__ __forceinline__ uint32_t checkpoint_encode(const float (&v)[8], uint32_t (&code)[2])
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
+        top = max(top, a < 0x7f800000u ? a : 0u);
+    }
+    top = largest_of_quad(top);
+    // The exponent of the largest less 8, one more where it is above 1.75 times its power of two: at most 448 = 1.75 * 2^8 remains.
+    const int scale = max((int)((top + 0x1fffffu) >> 23) - 8, 1);
+    const float inverse = __uint_as_float((uint32_t)(254 - scale) << 23);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // what is not 0 is not held as 0: at least 2^-9, the least code; what is not finite as NaN
+        x[i] = v[i] * inverse;
+        const float least = copysignf(fmaxf(fabsf(x[i]), 0x1p-9f), v[i]);
+        x[i] = v[i] == 0.f ? v[i] : (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u ? least : __uint_as_float(0x7fc00000u);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int c = 0;
+        c = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 0], x[4 * i + 1], c, false);
+        c = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], c, true);
+        code[i] = (uint32_t)c;
+    }
+    return (uint32_t)scale;
+}
+
+__device__ __forceinline__ void checkpoint_decode(const uint32_t (&code)[2], uint32_t scale, float (&v)[8])
+{
+    const float s = __uint_as_float(scale << 23);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[4 * i + 0] = __builtin_amdgcn_cvt_f32_fp8((int)code[i], 0) * s;
+        v[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)code[i], 1) * s;
+        v[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)code[i], 2) * s;
+        v[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)code[i], 3) * s;
+    }
+}
+
+// `n` codes (8: all) from or to memory of any alignment
+__device__ __forceinline__ void load_codes(const uint8_t* p, int n, uint32_t (&code)[2])
+{
+    if (n >= 8) {
+        __builtin_memcpy(code, p, 8);
+        return;
+    }
+    asm volatile("" : "+v"(p));
+    code[0] = code[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < n) code[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, const uint32_t (&code)[2])
+{
+    if (n >= 8) {
+        __builtin_memcpy(p, code, 8);
+        return;
+    }
+    asm volatile("" : "+v"(p));
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < n) p[i] = (uint8_t)(code[i / 4] >> (8 * (i % 4)));
+}
+
+// Eight columns from `col` (a multiple of 8) of a row, of which `valid` exist: their codes, and once for a block its scale.  Every lane of a
+// quad calls this.
+__device__ __forceinline__ void checkpoint_store(uint8_t* codes, uint8_t* scales, int col, int valid, const float (&v)[8])
+{
+    uint32_t code[2];
+    const uint32_t scale = checkpoint_encode(v, code);
+    if (valid <= 0) return;
+    store_codes(codes + col, valid, code);
+    if (col % PS_CHECKPOINT_BLOCK == 0) scales[col / PS_CHECKPOINT_BLOCK] = (uint8_t)scale;
+}
+
+#endif
+
+}  // namespace ps

@@ -16,23 +16,6 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
 
-// The group that has row r, or -1: the last one that begins at r or before, if it ends behind it.
-__device__ __forceinline__ int group_of_row(const Groups& gs, int64_t r)
-{
-    if (!gs.offsets) return 0;
-    int lo = 0, hi = gs.n;  // groups before lo begin at r or before, those from hi on behind it
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (min(max(gs.offsets[mid], 0), gs.rows) <= r)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    if (lo == 0) return -1;
-    const GroupRows rows = group_rows(gs, lo - 1);
-    return r >= rows.begin && r < rows.end ? lo - 1 : -1;
-}
-
 struct LookupArgs {
     const void *table, *tokens;
     void* out;

@@ -14,6 +14,7 @@
 // library's product of rows with rows 1330-1570 (the first and the third ten one after the other), of its two transposed forms
 // 1170-1360 and 1040-1180; by memory where they are few.
 #pragma once
+#include "ps_checkpoint.h"
 #include "ps_dense.h"
 #include "ps_split.h"
 
@@ -88,6 +89,23 @@ __device__ __forceinline__ int count_tiles(const Groups& gs, int size, int bound
         total += __builtin_amdgcn_readlane(tiles_upto(gs, g0, size, r, own), 63);
     }
     return min(total, bound);
+}
+
+// The group that has row r, or -1: the last one that begins at r or before, if it ends behind it.
+__device__ __forceinline__ int group_of_row(const Groups& gs, int64_t r)
+{
+    if (!gs.offsets) return 0;
+    int lo = 0, hi = gs.n;  // groups before lo begin at r or before, those from hi on behind it
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (min(max(gs.offsets[mid], 0), gs.rows) <= r)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    if (lo == 0) return -1;
+    const GroupRows rows = group_rows(gs, lo - 1);
+    return r >= rows.begin && r < rows.end ? lo - 1 : -1;
 }
 
 // The group and the first row of the `tile`-th piece of `size` rows when the groups are cut up one after the other; false
@@ -408,6 +426,8 @@ struct Epilogue {
     int64_t out_row, residual_row, pre_row, bias_matrix, out_matrix;  // elements
     int32_t act;
     float* partial;  // if not null the sums go there instead, one result for each part of the contraction: [part][rows][cols]
+    uint8_t *codes, *scales;  // KEPT: pre in 8 bits
+    int64_t codes_row, scales_row;
 };
 
 #if defined(__HIPCC__)
@@ -440,6 +460,15 @@ __device__ __forceinline__ void store_columns(T* p, int valid, const float (&v)[
         store_n(p, v);
     else
         store_some(p, valid, v);
+}
+// sum + bias, rounded to T, in 8 bits; of a quad of lanes every one calls this, whatever `valid` is.
+template <class T>
+__device__ __forceinline__ void keep(const Epilogue& e, const float (&bias)[8], int64_t row, int col, int valid, const float (&v)[8])
+{
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = i < valid ? to_float(from_float<T>(e.bias ? v[i] + bias[i] : v[i])) : 0.f;
+    checkpoint_store(e.codes + row * e.codes_row, e.scales + row * e.scales_row, col, valid, z);
 }
 template <class T, bool RESIDUAL, int N>
 __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int64_t row, int col, int valid, float (&v)[N])
@@ -581,7 +610,8 @@ __device__ __forceinline__ void block_barrier_after_reads()
     block_barrier();
 }
 
-template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DIRECT, int RAGGED>
+// KEPT: the forward pass keeps its pre-activations in 8 bits.
+template <class T, bool R_KC, bool C_KC, int BR, int BC, int WR, int WC, bool DIRECT, int RAGGED, bool KEPT>
 __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 {
     constexpr int NT = 64 * WR * WC, TR = BR / WR / 16, TC = BC / WC / 16;
@@ -1034,6 +1064,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
                     take(h + AT_ONCE < TURN * 16 ? row + AT_ONCE : row, x);
+                    if constexpr (KEPT) {
+                        if (r < r_valid && !epi.partial) keep<T>(epi, bias, done.r0 + r, done.c0 + c, c_valid, v);
+                    }
                     if (valid <= 0) continue;
                     if (epi.partial) {
                         float* to = epi.partial + ((int64_t)done.part * rows + (done.r0 + r)) * cols + done.c0 + c;
@@ -1063,6 +1096,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
 
 // Launchers, one file each (kinds of operands): forward, input gradient, weight gradient.
 void launch_linear_forward(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
+void launch_linear_forward_kept(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 void launch_linear_dx(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 void launch_linear_dw(const Product& p, int dtype, bool direct, int tile, hipStream_t s);
 
@@ -1077,29 +1111,29 @@ constexpr int FEW_DX_STEP = 64;
 constexpr int LINEAR_TILE[3] = {64, 128, 256};
 
 #if defined(__HIPCC__)
-template <class T, bool R_KC, bool C_KC, bool DIRECT, int RAGGED>
+template <class T, bool R_KC, bool C_KC, bool DIRECT, int RAGGED, bool KEPT>
 void start_linear(const Product& p, int tile, hipStream_t s)
 {
     const int total = (p.tiles_r * p.tiles_c * p.parts + LINEAR_XCDS - 1) / LINEAR_XCDS * LINEAR_XCDS;
     const dim3 grid(std::min(total, ROW_OF_BLOCKS), (total + ROW_OF_BLOCKS - 1) / ROW_OF_BLOCKS);  // blocks past the last tile end at once
     if (tile == 0)
-        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 64, 64, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 64, 64, 2, 2, DIRECT, RAGGED, KEPT>), grid, dim3(256), 0, s, p);
     else if (tile == 1 || !DIRECT || sizeof(T) == 4)
-        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 128, 128, 2, 2, DIRECT, RAGGED>), grid, dim3(256), 0, s, p);
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 128, 128, 2, 2, DIRECT, RAGGED, KEPT>), grid, dim3(256), 0, s, p);
     else if constexpr (DIRECT && sizeof(T) == 2) {
         static_assert(linear_persistent(256), "a block for each tile would have to be counted as above");
-        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED>), dim3(std::min(total, COMPUTE_UNITS)), dim3(512), 0, s, p);
+        hipLaunchKernelGGL((linear_kernel<T, R_KC, C_KC, 256, 256, 2, 4, DIRECT, RAGGED, KEPT>), dim3(std::min(total, COMPUTE_UNITS)), dim3(512), 0, s, p);
     }
 }
-template <bool R_KC, bool C_KC, int RAGGED>
+template <bool R_KC, bool C_KC, int RAGGED, bool KEPT = false>
 void start_linear_typed(const Product& p, int dtype, bool direct, int tile, hipStream_t s)
 {
     if (dtype == PS_F32)
-        direct ? start_linear<float, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<float, R_KC, C_KC, false, RAGGED>(p, tile, s);
+        direct ? start_linear<float, R_KC, C_KC, true, RAGGED, KEPT>(p, tile, s) : start_linear<float, R_KC, C_KC, false, RAGGED, KEPT>(p, tile, s);
     else if (dtype == PS_BF16)
-        direct ? start_linear<bf16_t, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<bf16_t, R_KC, C_KC, false, RAGGED>(p, tile, s);
+        direct ? start_linear<bf16_t, R_KC, C_KC, true, RAGGED, KEPT>(p, tile, s) : start_linear<bf16_t, R_KC, C_KC, false, RAGGED, KEPT>(p, tile, s);
     else
-        direct ? start_linear<f16_t, R_KC, C_KC, true, RAGGED>(p, tile, s) : start_linear<f16_t, R_KC, C_KC, false, RAGGED>(p, tile, s);
+        direct ? start_linear<f16_t, R_KC, C_KC, true, RAGGED, KEPT>(p, tile, s) : start_linear<f16_t, R_KC, C_KC, false, RAGGED, KEPT>(p, tile, s);
 }
 #endif
 

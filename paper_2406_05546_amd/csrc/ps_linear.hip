@@ -1,5 +1,6 @@
 // Entry points of the dense layers (include/ps_dense.h): checks, choice of tiles, workspaces, and the kernels around the
 // products of ps_linear.h.
+#include "ps_checkpoint_calls.h"
 #include "ps_linear.h"
 
 #include <cstdarg>
@@ -25,9 +26,10 @@ namespace {
 // ---- dz = dy act'(z), and the sums over rows that are the bias's gradient ------------------------------------------
 
 struct SlopeArgs {
-    const void *dy, *pre;  // pre null: no activation
+    const void *dy, *pre;  // pre null: no activation (CODES: pre's codes)
+    const uint8_t* scales; // CODES: their scales
     void* dz;              // null: only the sums
-    int64_t dy_row, pre_row, dz_row;
+    int64_t dy_row, pre_row, dz_row, scale_row;
     int32_t act, cols, parts;
     float* partial;  // [group][part][cols], or null: no sums
     Groups groups;
@@ -39,7 +41,7 @@ struct SlopeArgs {
 // 114 -> 88-104 us, 3.9-4.6 TB/s; 8192 x 512 13.8 -> 9.6).
 constexpr int SLOPE_COLS = 512;
 
-template <class T>
+template <class T, bool CODES>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
 {
     constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
@@ -52,17 +54,27 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     const int col = blockIdx.x * SLOPE_COLS + lane * 8, n = min(8, a.cols - col);
     float sum[8] = {};
     struct Row {
-        T dy[8], pre[8];
+        T dy[8], pre[CODES ? 1 : 8];
+        uint32_t code[2];
+        uint8_t scale;
     };
     auto take = [&](int64_t r, Row& x) __attribute__((always_inline)) {
         __builtin_memcpy(x.dy, static_cast<const T*>(a.dy) + r * a.dy_row + col, sizeof(x.dy));
-        if (a.pre) __builtin_memcpy(x.pre, static_cast<const T*>(a.pre) + r * a.pre_row + col, sizeof(x.pre));
+        if constexpr (CODES) {
+            __builtin_memcpy(x.code, static_cast<const uint8_t*>(a.pre) + r * a.pre_row + col, 8);
+            x.scale = a.scales[r * a.scale_row + col / PS_CHECKPOINT_BLOCK];
+        } else if (a.pre) __builtin_memcpy(x.pre, static_cast<const T*>(a.pre) + r * a.pre_row + col, sizeof(x.pre));
     };
     auto give = [&](int64_t r, const Row& x) __attribute__((always_inline)) {
         float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = to_float(x.dy[i]);
-        if (a.pre) {
+        if constexpr (CODES) {
+            float z[8];
+            checkpoint_decode(x.code, x.scale, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] *= activation_slope(z[i], a.act);
+        } else if (a.pre) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] *= activation_slope(to_float(x.pre[i]), a.act);
         }
@@ -107,7 +119,12 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             for (int i = 0; i < 7; ++i) {
                 if (i >= n) continue;
                 x.dy[i] = static_cast<const T*>(a.dy)[r * a.dy_row + col + i];
-                if (a.pre) x.pre[i] = static_cast<const T*>(a.pre)[r * a.pre_row + col + i];
+                if constexpr (!CODES)
+                    if (a.pre) x.pre[i] = static_cast<const T*>(a.pre)[r * a.pre_row + col + i];
+            }
+            if constexpr (CODES) {
+                load_codes(static_cast<const uint8_t*>(a.pre) + r * a.pre_row + col, n, x.code);
+                x.scale = a.scales[r * a.scale_row + col / PS_CHECKPOINT_BLOCK];
             }
             give(r, x);
         }
@@ -152,16 +169,19 @@ __global__ __launch_bounds__(BIAS_COLS * BIAS_SHARES) void bias_sum_kernel(const
     db[g * db_matrix + c] = from_float<T>(s);
 }
 
+// Threads for a row, eight columns each; whole blocks of them where it is kept in 8 bits.
+__host__ __device__ inline int join_pieces(int cols, const void* codes) { return codes ? (cols + PS_CHECKPOINT_BLOCK - 1) / PS_CHECKPOINT_BLOCK * CHECKPOINT_LANES : (cols + 7) / 8; }
+
 // Adds up the parts of a contraction, in order, and finishes the sums.  (There are parts only where there is one group.)
 template <class T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int parts, int rows, int cols, Groups groups, Epilogue epi)
 {
-    const int per_row = (cols + 7) / 8;
+    const int per_row = join_pieces(cols, epi.codes);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
     if (row >= rows) return;
     const int col = (int)(i % per_row) * 8, n = min(8, cols - col);
     float v[8], x[8];
-    for (int k = 0; k < parts; ++k) {
+    for (int k = 0; k < parts && n > 0; ++k) {
         const float* p = partial + ((int64_t)k * rows + row) * cols + col;
         if (n == 8)
             load_n(p, x);
@@ -173,6 +193,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
     float bias[8], residual[8];
     load_bias<T>(epi, group_matrix(groups, 0), col, n, bias);
     load_residual<T>(epi, row, col, n, residual);
+    if (epi.codes) keep<T>(epi, bias, row, col, n, v);
     if (epi.residual)
         finish<T, true>(epi, bias, residual, row, col, n, v);
     else
@@ -352,6 +373,7 @@ bool worth_padding(const ps_linear& l, int kind)
     return plan_product(l, kind, false).us > plan_product(l, kind, true).us + bytes / 4e6 + (kind == FORWARD || dz ? 10 : 5);
 }
 
+// x8: x comes in 8 bits and is brought to rows as padded copies have them first.
 struct BackwardSpace {
     uint64_t dz, bias, partial, x, w, total;
     int64_t dz_row;
@@ -359,7 +381,7 @@ struct BackwardSpace {
     bool pad_dx, pad_dw;
 };
 
-BackwardSpace backward_space(const ps_linear& l)
+BackwardSpace backward_space(const ps_linear& l, bool x8)
 {
     BackwardSpace b{};
     const Padded p = padded(l);
@@ -376,23 +398,26 @@ BackwardSpace backward_space(const ps_linear& l)
     b.bias = dz;
     b.partial = dz + bias;
     b.x = b.partial + up256(partial);
-    b.w = b.x + (b.pad_dw ? p.x : 0);
+    b.w = b.x + (b.pad_dw || x8 ? p.x : 0);
     b.total = b.w + (b.pad_dx ? p.w : 0);
     return b;
 }
 
+// kept: pre in 8 bits, which the kernel for few rows leaves in the layer's type first.
 struct ForwardSpace {
-    uint64_t x, w, total;
-    bool pad;
+    uint64_t x, w, pre, total;
+    bool pad, encode;
 };
 
-ForwardSpace forward_space(const ps_linear& l)
+ForwardSpace forward_space(const ps_linear& l, bool kept)
 {
     ForwardSpace f{};
     f.pad = worth_padding(l, FORWARD);
     f.x = up256(std::max(plan_product(l, FORWARD, true).partial_bytes, plan_product(l, FORWARD, false).partial_bytes));
     f.w = f.x + (f.pad ? padded(l).x : 0);
-    f.total = f.w + (f.pad ? padded(l).w : 0);
+    f.pre = f.w + (f.pad ? padded(l).w : 0);
+    f.encode = kept && plan_product(l, FORWARD, true).few;  // (which does not go by how operands come)
+    f.total = f.pre + (f.encode ? up256((uint64_t)l.rows * l.out_features * dtype_size(l.dtype)) : 0);
     return f;
 }
 
@@ -495,9 +520,9 @@ void run_product(const ps_linear& l, int kind, bool direct, bool copied, const p
     if (plan.few)
         (kind == FORWARD ? launch_linear_few : launch_linear_few_dx)(p, l.dtype, plan.few, s);
     else
-        (kind == FORWARD ? launch_linear_forward : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
+        (kind == FORWARD ? (epi.codes ? launch_linear_forward_kept : launch_linear_forward) : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
     if (plan.parts > 1) {
-        const int64_t threads = up(p.out_cols, 8) * p.out_rows;
+        const int64_t threads = (int64_t)join_pieces(p.out_cols, epi.codes) * p.out_rows;
         with_type(l.dtype, [&](auto t) {
             hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, p.groups, epi);
         });
@@ -510,26 +535,10 @@ ps_status launched(const char* call)
     return e == hipSuccess ? PS_OK : dense_fail(PS_EDEVICE, "%s: %s", call, hipGetErrorString(e));
 }
 
-}  // namespace
-}  // namespace ps
-
-extern "C" const char* ps_dense_last_error(void) { return ps::dense_error; }
-
-extern "C" ps_status ps_linear_workspace_bytes(const ps_linear* l, int32_t backward, uint64_t* bytes_out)
+// pre or pre8 (or neither)
+ps_status forward(const char* call, const ps_linear* l, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias, const ps_matrix* residual, const ps_matrix* y,
+                  const ps_matrix* pre, const ps_checkpoint* pre8, void* workspace, uint64_t workspace_bytes, void* hip_stream)
 {
-    using namespace ps;
-    const ps_status st = check_layer("ps_linear_workspace_bytes", l);
-    if (st != PS_OK) return st;
-    if (!bytes_out) return dense_fail(PS_EINVAL, "ps_linear_workspace_bytes: no place for the result");
-    *bytes_out = backward ? backward_space(*l).total : forward_space(*l).total;
-    return PS_OK;
-}
-
-extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias, const ps_matrix* residual,
-                                       const ps_matrix* y, const ps_matrix* pre, void* workspace, uint64_t workspace_bytes, void* hip_stream)
-{
-    using namespace ps;
-    static const char call[] = "ps_linear_forward";
     ps_status st = check_layer(call, l);
     if (st != PS_OK) return st;
     if ((st = check_matrix(call, "x", *l, x, true, l->rows, l->in_features, 1)) != PS_OK) return st;
@@ -538,8 +547,9 @@ extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, c
     if ((st = check_matrix(call, "residual", *l, residual, false, l->rows, l->out_features, 1)) != PS_OK) return st;
     if ((st = check_matrix(call, "y", *l, y, true, l->rows, l->out_features, 1)) != PS_OK) return st;
     if ((st = check_matrix(call, "pre", *l, pre, false, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if (pre8 && (st = check_checkpoint(call, "pre", pre8, l->rows, l->out_features)) != PS_OK) return st;
     if (!l->rows) return PS_OK;
-    const ForwardSpace space = forward_space(*l);
+    const ForwardSpace space = forward_space(*l, pre8 != nullptr);
     const uint64_t need = space.total;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
     if (workspace_bytes < need) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
@@ -551,8 +561,15 @@ extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, c
     if (there(residual)) e.residual = residual->data_dev, e.residual_row = residual->row;
     if (there(pre)) e.pre = pre->data_dev, e.pre_row = pre->row;
     e.act = l->activation;
+    if (pre8 && !space.encode) {
+        e.codes = static_cast<uint8_t*>(pre8->codes_dev);
+        e.scales = static_cast<uint8_t*>(pre8->scales_dev);
+        e.codes_row = pre8->row;
+        e.scales_row = pre8->scale_row;
+    }
     const bool direct = direct_possible(*l, FORWARD) && aligned16(*l, *x, l->rows, 1) && aligned16(*l, *w, l->out_features, l->n_weights);
     char* const base = static_cast<char*>(workspace);
+    if (space.encode) e.pre = base + space.pre, e.pre_row = l->out_features;
     if (space.pad) {
         const Padded to = padded(*l);
         const ps_matrix xp = pad(*l, *x, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s);
@@ -561,27 +578,28 @@ extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, c
     } else {
         run_product(*l, FORWARD, direct, false, *x, *w, e, reinterpret_cast<float*>(base), s);
     }
+    if (space.encode) launch_checkpoint_encode(l->dtype, groups_of(*l), l->rows, l->out_features, ps_matrix{e.pre, e.pre_row, 0}, *pre8, s);
     return launched(call);
 }
 
-extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy, const ps_matrix* x, const ps_matrix* w, const ps_matrix* pre,
-                                        const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db, void* workspace, uint64_t workspace_bytes,
-                                        void* hip_stream)
+// x8 or pre8 in the place of x or pre
+ps_status backward(const char* call, const ps_linear* l, const ps_matrix* dy, const ps_matrix* x, const ps_checkpoint* x8, int32_t x_activation, const ps_matrix* w,
+                   const ps_matrix* pre, const ps_checkpoint* pre8, const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db, void* workspace,
+                   uint64_t workspace_bytes, void* hip_stream)
 {
-    using namespace ps;
-    static const char call[] = "ps_linear_backward";
     ps_status st = check_layer(call, l);
     if (st != PS_OK) return st;
     const bool act = l->activation != PS_ACT_NONE, want_dx = there(dx), want_dw = there(dw), want_db = there(db);
     if ((st = check_matrix(call, "dy", *l, dy, true, l->rows, l->out_features, 1)) != PS_OK) return st;
-    if ((st = check_matrix(call, "x", *l, x, want_dw, l->rows, l->in_features, 1)) != PS_OK) return st;
+    if (x8 ? (st = check_checkpoint(call, "x", x8, l->rows, l->in_features)) != PS_OK : (st = check_matrix(call, "x", *l, x, want_dw, l->rows, l->in_features, 1)) != PS_OK) return st;
+    if (x8 && (x_activation < PS_ACT_NONE || x_activation > PS_ACT_SILU)) return dense_fail(PS_EINVAL, "%s: unknown activation of x", call);
     if ((st = check_matrix(call, "w", *l, w, want_dx, l->out_features, l->in_features, l->n_weights)) != PS_OK) return st;
-    if ((st = check_matrix(call, "pre", *l, pre, act, l->rows, l->out_features, 1)) != PS_OK) return st;
+    if (pre8 ? (st = check_checkpoint(call, "pre", pre8, l->rows, l->out_features)) != PS_OK : (st = check_matrix(call, "pre", *l, pre, act, l->rows, l->out_features, 1)) != PS_OK) return st;
     if ((st = check_matrix(call, "dx", *l, dx, false, l->rows, l->in_features, 1)) != PS_OK) return st;
     if ((st = check_matrix(call, "dw", *l, dw, false, l->out_features, l->in_features, l->n_groups)) != PS_OK) return st;
     if ((st = check_matrix(call, "db", *l, db, false, 1, l->out_features, l->n_groups)) != PS_OK) return st;
     if (!want_dx && !want_dw && !want_db) return PS_OK;
-    const BackwardSpace space = backward_space(*l);
+    const BackwardSpace space = backward_space(*l, x8 && want_dw);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
     if (workspace_bytes < space.total) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -593,7 +611,15 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
         SlopeArgs a{};
         a.dy = dy ? dy->data_dev : nullptr;
         a.dy_row = dy ? dy->row : 0;
-        if (act && there(pre)) a.pre = pre->data_dev, a.pre_row = pre->row;
+        if (act && pre8) {
+            a.pre = pre8->codes_dev;
+            a.pre_row = pre8->row;
+            a.scales = static_cast<const uint8_t*>(pre8->scales_dev);
+            a.scale_row = pre8->scale_row;
+        } else if (act && there(pre)) {
+            a.pre = pre->data_dev;
+            a.pre_row = pre->row;
+        }
         if (act && (want_dx || want_dw)) a.dz = dz.data_dev, a.dz_row = dz.row;
         a.act = l->activation;
         a.cols = (int32_t)l->out_features;
@@ -603,7 +629,11 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
         const int64_t many = (int64_t)l->n_groups * space.parts;
         with_type(l->dtype, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL(slope_kernel<T>, dim3((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many), dim3(256), 0, s, a);
+            const dim3 grid((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many);
+            if (a.scales)
+                hipLaunchKernelGGL((slope_kernel<T, true>), grid, dim3(256), 0, s, a);
+            else
+                hipLaunchKernelGGL((slope_kernel<T, false>), grid, dim3(256), 0, s, a);
             if (want_db)
                 hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)up(l->out_features, BIAS_COLS), (uint32_t)l->n_groups), dim3(BIAS_COLS * BIAS_SHARES), 0, s, a.partial,
                                    static_cast<T*>(db->data_dev), db->matrix, (int)l->out_features, space.parts);
@@ -629,12 +659,69 @@ extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy,
         e.out = dw->data_dev;
         e.out_row = dw->row;
         e.out_matrix = dw->matrix;
-        const ps_matrix xm = x ? *x : none;
+        ps_matrix xm = x ? *x : none;
+        if (x8) {
+            xm = ps_matrix{base + space.x, to.in, 0};
+            if (l->rows) launch_checkpoint_decode(l->dtype, l->rows, l->in_features, *x8, x_activation, xm, to.in, s);
+        }
         const bool direct = direct_possible(*l, DW) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, xm, l->rows, 1);
         if (pad_dw)
-            run_product(*l, DW, true, true, dzp, pad(*l, xm, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s), e, partial, s);
+            run_product(*l, DW, true, true, dzp, x8 ? xm : pad(*l, xm, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s), e, partial, s);
         else
             run_product(*l, DW, direct, false, dz, xm, e, partial, s);
     }
     return launched(call);
+}
+
+}  // namespace
+}  // namespace ps
+
+extern "C" const char* ps_dense_last_error(void) { return ps::dense_error; }
+
+extern "C" ps_status ps_linear_workspace_bytes(const ps_linear* l, int32_t backward, uint64_t* bytes_out)
+{
+    using namespace ps;
+    const ps_status st = check_layer("ps_linear_workspace_bytes", l);
+    if (st != PS_OK) return st;
+    if (!bytes_out) return dense_fail(PS_EINVAL, "ps_linear_workspace_bytes: no place for the result");
+    *bytes_out = backward ? backward_space(*l, false).total : forward_space(*l, false).total;
+    return PS_OK;
+}
+
+extern "C" ps_status ps_linear_checkpoint_workspace_bytes(const ps_linear* l, int32_t backward, int32_t x_in_8_bits, uint64_t* bytes_out)
+{
+    using namespace ps;
+    const ps_status st = check_layer("ps_linear_checkpoint_workspace_bytes", l);
+    if (st != PS_OK) return st;
+    if (!bytes_out) return dense_fail(PS_EINVAL, "ps_linear_checkpoint_workspace_bytes: no place for the result");
+    *bytes_out = backward ? backward_space(*l, x_in_8_bits != 0).total : forward_space(*l, true).total;
+    return PS_OK;
+}
+
+extern "C" ps_status ps_linear_forward(const ps_linear* l, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias, const ps_matrix* residual,
+                                       const ps_matrix* y, const ps_matrix* pre, void* workspace, uint64_t workspace_bytes, void* hip_stream)
+{
+    return ps::forward("ps_linear_forward", l, x, w, bias, residual, y, pre, nullptr, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" ps_status ps_linear_forward_checkpoint(const ps_linear* l, const ps_matrix* x, const ps_matrix* w, const ps_matrix* bias, const ps_matrix* residual,
+                                                  const ps_matrix* y, const ps_checkpoint* pre, void* workspace, uint64_t workspace_bytes, void* hip_stream)
+{
+    static const char call[] = "ps_linear_forward_checkpoint";
+    if (!pre) return ps::dense_fail(PS_EINVAL, "%s: pre is missing", call);
+    return ps::forward(call, l, x, w, bias, residual, y, nullptr, pre, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" ps_status ps_linear_backward(const ps_linear* l, const ps_matrix* dy, const ps_matrix* x, const ps_matrix* w, const ps_matrix* pre,
+                                        const ps_matrix* dx, const ps_matrix* dw, const ps_matrix* db, void* workspace, uint64_t workspace_bytes,
+                                        void* hip_stream)
+{
+    return ps::backward("ps_linear_backward", l, dy, x, nullptr, PS_ACT_NONE, w, pre, nullptr, dx, dw, db, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" ps_status ps_linear_backward_checkpoint(const ps_linear* l, const ps_matrix* dy, const ps_matrix* x, const ps_checkpoint* x8, int32_t x_activation,
+                                                   const ps_matrix* w, const ps_matrix* pre, const ps_checkpoint* pre8, const ps_matrix* dx, const ps_matrix* dw,
+                                                   const ps_matrix* db, void* workspace, uint64_t workspace_bytes, void* hip_stream)
+{
+    return ps::backward("ps_linear_backward_checkpoint", l, dy, x, x8, x_activation, w, pre, pre8, dx, dw, db, workspace, workspace_bytes, hip_stream);
 }

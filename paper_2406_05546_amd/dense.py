@@ -17,8 +17,10 @@ from .binding import PS_EINVAL, PS_OK, PsError, load_library
 PS_F32, PS_BF16, PS_F16 = range(3)
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 ADAMW_BLOCK = 256
+CHECKPOINT_BLOCK = 32
 
-EXPORTS = ["ps_linear_workspace_bytes", "ps_linear_forward", "ps_linear_backward", "ps_adamw_workspace_bytes", "ps_adamw_create",
+EXPORTS = ["ps_linear_workspace_bytes", "ps_linear_forward", "ps_linear_backward", "ps_checkpoint_encode", "ps_checkpoint_decode",
+           "ps_linear_checkpoint_workspace_bytes", "ps_linear_forward_checkpoint", "ps_linear_backward_checkpoint", "ps_adamw_workspace_bytes", "ps_adamw_create",
            "ps_adamw_destroy", "ps_adamw_step", "ps_dense_last_error"]
 
 
@@ -30,6 +32,10 @@ class ps_linear(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("rows", ctypes.c_int64), ("in_features", ctypes.c_int64),
                 ("out_features", ctypes.c_int64), ("n_groups", ctypes.c_int32), ("n_weights", ctypes.c_int32),
                 ("offsets_dev", ctypes.c_void_p), ("weight_of_group_dev", ctypes.c_void_p)]
+
+
+class ps_checkpoint(ctypes.Structure):
+    _fields_ = [("codes_dev", ctypes.c_void_p), ("scales_dev", ctypes.c_void_p), ("row", ctypes.c_int64), ("scale_row", ctypes.c_int64)]
 
 
 class ps_adamw_tensor(ctypes.Structure):
@@ -56,6 +62,11 @@ def _library() -> ctypes.CDLL:
                 "ps_linear_workspace_bytes": [vp, i32, vp],
                 "ps_linear_forward": 8 * [vp] + [u64, vp],
                 "ps_linear_backward": 9 * [vp] + [u64, vp],
+                "ps_checkpoint_encode": [i32, ctypes.c_int64, ctypes.c_int64, vp, vp, vp],
+                "ps_checkpoint_decode": [i32, ctypes.c_int64, ctypes.c_int64, vp, i32, vp, vp],
+                "ps_linear_checkpoint_workspace_bytes": [vp, i32, i32, vp],
+                "ps_linear_forward_checkpoint": 8 * [vp] + [u64, vp],
+                "ps_linear_backward_checkpoint": 4 * [vp] + [i32] + 7 * [vp] + [u64, vp],
                 "ps_adamw_workspace_bytes": [p(ps_adamw_tensor), i32, p(u64)],
                 "ps_adamw_create": [p(vp), p(ps_adamw_tensor), i32, vp, u64, vp],
                 "ps_adamw_destroy": [vp],
@@ -115,33 +126,151 @@ def _ints(call: str, name: str, t, device, n: Optional[int] = None) -> int:
 # most of the time of a small layer).
 _LAYER, _MATRIX = "<iiqqqiiQQ", "Qqq"
 _LAYER_BYTES, _MATRIX_BYTES = struct.calcsize(_LAYER), struct.calcsize("<" + _MATRIX)
-assert _LAYER_BYTES == ctypes.sizeof(ps_linear) and _MATRIX_BYTES == ctypes.sizeof(ps_matrix)
+_CHECKPOINT = "QQqq"
+_CHECKPOINT_BYTES = struct.calcsize("<" + _CHECKPOINT)
+assert _LAYER_BYTES == ctypes.sizeof(ps_linear) and _MATRIX_BYTES == ctypes.sizeof(ps_matrix) and _CHECKPOINT_BYTES == ctypes.sizeof(ps_checkpoint)
 _PACK = {n: struct.Struct(_LAYER + n * _MATRIX).pack_into for n in (6, 7)}
+_PACK_CHECKPOINT = struct.Struct("<" + _CHECKPOINT).pack_into
 _ABSENT = (0, 0, 0)
 
 
 class _Arguments(threading.local):
     def __init__(self):
-        self.memory = ctypes.create_string_buffer(_LAYER_BYTES + 7 * _MATRIX_BYTES)
+        self.memory = ctypes.create_string_buffer(_LAYER_BYTES + 7 * _MATRIX_BYTES + 2 * _CHECKPOINT_BYTES)
         self.need = ctypes.c_uint64(0)
         self.options = ps_adamw_options()
         self.at = ctypes.addressof(self.memory)
         self.at_need = ctypes.addressof(self.need)
         self.at_matrices = [self.at + _LAYER_BYTES + i * _MATRIX_BYTES for i in range(7)]
+        self.of_checkpoints = [_LAYER_BYTES + 7 * _MATRIX_BYTES + i * _CHECKPOINT_BYTES for i in range(2)]
 
 
 _arguments = _Arguments()
 
 
-def _layer(call: str, x, w, activation: str, offsets, weight_of_group) -> Tuple[int, ...]:
-    """The fields of the call's ps_linear."""
+@dataclass
+class Checkpoint:
+    """Activations [rows, cols] in 8 bits, as ps_checkpoint_encode gives them: e4m3 codes, and for every 32 columns of a row a power of two
+    that scales them.  Rows are contiguous."""
+    codes: torch.Tensor   # [rows, cols] float8_e4m3fn (or uint8)
+    scales: torch.Tensor  # [rows, ceil(cols / 32)] float8_e8m0fnu (or uint8)
+
+    @property
+    def shape(self) -> torch.Size:
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+_CODES, _SCALES = (torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8)
+
+
+def _kept(call: str, name: str, c: Checkpoint, device, shape) -> Tuple[int, int, int, int]:
+    """Checks that `c` has this shape and device; the fields of its ps_checkpoint."""
+    codes, scales = c.codes, c.scales
+    blocks = -(-shape[1] // CHECKPOINT_BLOCK)
+    if codes.dtype not in _CODES or scales.dtype not in _SCALES or codes.device != device or scales.device != device:
+        _refuse(call, f"{name} has {codes.dtype} codes on {codes.device} and {scales.dtype} scales on {scales.device}, not e4m3 and e8m0 ones on {device}")
+    if codes.shape != shape or scales.shape != (shape[0], blocks):
+        _refuse(call, f"{name} has codes {tuple(codes.shape)} and scales {tuple(scales.shape)}, not {tuple(shape)} and {(shape[0], blocks)}")
+    row, scale_row = codes.stride(), scales.stride()
+    if codes.numel() and (shape[1] > 1 and row[1] != 1 or blocks > 1 and scale_row[1] != 1):
+        _refuse(call, f"{name}'s rows are not contiguous")
+    several = shape[0] > 1
+    return codes.data_ptr(), scales.data_ptr(), row[0] if several else shape[1], scale_row[0] if several else blocks
+
+
+def _run_checkpoint(call: str, layer: Tuple[int, ...], backward: int, device, matrices, x8, x_act: int, pre8) -> None:
+    """`_run` for calls with a checkpoint: x8 or pre8 are the fields of one in the place of x (then None in `matrices`) or pre, or None."""
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run_checkpoint(call, layer, backward, device, matrices, x8, x_act, pre8)
+    lib, a = _library(), _arguments
+    fields = list(layer)
+    for m in matrices:
+        fields += m or _ABSENT
+    _PACK[len(matrices)](a.memory, 0, *fields)
+    kept = []
+    for of, c in zip(a.of_checkpoints, (x8, pre8)):
+        if c:
+            _PACK_CHECKPOINT(a.memory, of, *c)
+        kept.append(a.at + of if c else None)
+    st = lib.ps_linear_checkpoint_workspace_bytes(a.at, backward, 1 if x8 and matrices[5] else 0, a.at_need)
+    if st != PS_OK:
+        _check(call, st)
+    need = a.need.value
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    at, stream = None if ws is None else ws.data_ptr(), torch._C._cuda_getCurrentRawStream(index)
+    refs = [at if m else None for m, at in zip(matrices, a.at_matrices)]
+    if backward:
+        dy, x, w, pre, dx, dw, db = refs
+        st = lib.ps_linear_backward_checkpoint(a.at, dy, x, kept[0], x_act, w, pre, kept[1], dx, dw, db, at, need, stream)
+    else:
+        st = lib.ps_linear_forward_checkpoint(a.at, *refs[:5], kept[1], at, need, stream)
+    if st != PS_OK:
+        _check(call, st)
+
+
+def ps_checkpoint_empty(rows: int, cols: int, device) -> Checkpoint:
+    """Room for activations [rows, cols], its contents whatever they are."""
+    return Checkpoint(torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=device),
+                      torch.empty(rows, -(-cols // CHECKPOINT_BLOCK), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def _code_call(call: str, dtype: int, x, c: Checkpoint, encode: bool, act: int) -> None:
+    device, shape = x.device, tuple(x.shape)
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _code_call(call, dtype, x, c, encode, act)
+    a = _arguments
+    struct.pack_into("<" + _MATRIX, a.memory, _LAYER_BYTES, *_matrix(call, "x", x, device, x.dtype, shape))
+    _PACK_CHECKPOINT(a.memory, a.of_checkpoints[0], *_kept(call, "the checkpoint", c, device, shape))
+    lib, at, kept, stream = _library(), a.at_matrices[0], a.at + a.of_checkpoints[0], torch._C._cuda_getCurrentRawStream(index)
+    st = lib.ps_checkpoint_encode(dtype, *shape, at, kept, stream) if encode else lib.ps_checkpoint_decode(dtype, *shape, kept, act, at, stream)
+    if st != PS_OK:
+        _check(call, st)
+
+
+def ps_checkpoint_encode(x, out: Optional[Checkpoint] = None) -> Checkpoint:
+    """x [rows, cols] (float32, bfloat16 or float16, contiguous rows) in 8 bits: half a step of 2^-4 of a value off at most, for values from
+    2^-15 of their block's largest on.  What is not 0 is not held as 0; what is not finite is held as NaN."""
+    call = "ps_checkpoint_encode"
+    dtype = _dtype(call, "x", x)
+    if x.dim() != 2 or x.device.type != "cuda":
+        _refuse(call, "x is [rows, cols] on a GPU")
+    c = ps_checkpoint_empty(*x.shape, x.device) if out is None else out
+    _code_call(call, dtype, x, c, True, 0)
+    return c
+
+
+def ps_checkpoint_decode(c: Checkpoint, dtype=torch.bfloat16, activation: str = "none", out=None):
+    """The activation of the values that a checkpoint holds, in `dtype` (or out's)."""
+    call = "ps_checkpoint_decode"
+    if c.codes.dim() != 2 or c.codes.device.type != "cuda":
+        _refuse(call, "the checkpoint is [rows, cols] on a GPU")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        _refuse(call, f"unknown activation {activation!r}")
+    x = torch.empty(c.shape, dtype=dtype, device=c.device) if out is None else out
+    if x.shape != c.shape or x.device != c.device:
+        _refuse(call, f"out has the shape {tuple(x.shape)} on {x.device}, not {tuple(c.shape)} on {c.device}")
+    _code_call(call, _dtype(call, "out", x), x, c, False, act)
+    return x
+
+
+def _layer(call: str, x, w, activation: str, offsets, weight_of_group, dtype_of=None) -> Tuple[int, ...]:
+    """The fields of the call's ps_linear.  x may be a checkpoint of the type of `dtype_of`."""
     grouped = offsets is not None
     act = ACTIVATIONS.get(activation)
     if act is None:
         _refuse(call, f"unknown activation {activation!r}")
-    if x.dim() != 2 or w.dim() != (3 if grouped else 2):
+    if len(x.shape) != 2 or w.dim() != (3 if grouped else 2):
         _refuse(call, "x is [rows, in] and w " + ("[matrices, out, in]" if grouped else "[out, in]"))
-    dtype, device = _dtype(call, "x", x), x.device
+    dtype, device = _dtype(call, "x", x) if dtype_of is None else _dtype(call, "dy", dtype_of), x.device
     if device.type != "cuda":
         _refuse(call, f"x is on {device}, not on a GPU")
     rows, fin = x.shape
@@ -179,23 +308,30 @@ def _run(call: str, layer: Tuple[int, ...], backward: int, device, matrices) -> 
 
 def _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out):
     call = "ps_linear_forward"
+    if type(x) is Checkpoint:
+        _refuse(call, "x is a checkpoint, which the backward pass reads")
     layer = _layer(call, x, w, activation, offsets, weight_of_group)
     grouped, device, dtype, rows, fin, fout = offsets is not None, x.device, x.dtype, layer[2], layer[3], layer[4]
     mats = (w.shape[0],) if grouped else ()
     of_out = (rows, fout)
     y = x.new_empty(of_out) if out is None else out
-    _run(call, layer, 0, device, [
+    kept = type(pre) is Checkpoint
+    matrices = [
         _matrix(call, "x", x, device, dtype, (rows, fin)), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
         None if bias is None else _matrix(call, "bias", bias, device, dtype, mats + (fout,), grouped),
         None if residual is None else _matrix(call, "residual", residual, device, dtype, of_out), _matrix(call, "out", y, device, dtype, of_out),
-        None if pre is None else _matrix(call, "pre", pre, device, dtype, of_out)])
+        None if pre is None or kept else _matrix(call, "pre", pre, device, dtype, of_out)]
+    if kept:
+        _run_checkpoint("ps_linear_forward_checkpoint", layer, 0, device, matrices, None, 0, _kept(call, "pre", pre, device, of_out))
+    else:
+        _run(call, layer, 0, device, matrices)
     return y
 
 
 def ps_linear_forward(x, w, bias=None, residual=None, activation: str = "none", pre=None, out=None):
     """act(x w^T + bias) + residual.  x [rows, in], w [out, in], bias [out], residual [rows, out], all of one type
     (float32, bfloat16, float16) with contiguous rows; activation "none", "relu", "gelu" or "silu".  pre [rows, out]
-    receives the value before the activation, which the backward pass reads.  out may be the residual.  Returns out."""
+    receives the value before the activation, which the backward pass reads; given a Checkpoint, in 8 bits.  out may be the residual.  Returns out."""
     return _forward(x, None, w, bias, residual, activation, None, pre, out)
 
 
@@ -205,37 +341,47 @@ def ps_grouped_linear_forward(x, offsets, w, bias=None, residual=None, activatio
     return _forward(x, offsets, w, bias, residual, activation, weight_of_group, pre, out)
 
 
-def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db):
+def _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db, x_activation):
     call = "ps_linear_backward"
-    layer = _layer(call, x, w, activation, offsets, weight_of_group)
-    grouped, device, dtype, rows, fin, fout, groups = offsets is not None, x.device, x.dtype, layer[2], layer[3], layer[4], layer[5]
+    x_kept, pre_kept = type(x) is Checkpoint, type(pre) is Checkpoint
+    layer = _layer(call, x, w, activation, offsets, weight_of_group, dy if x_kept else None)
+    grouped, device, dtype, rows, fin, fout, groups = offsets is not None, x.device, (dy if x_kept else x).dtype, layer[2], layer[3], layer[4], layer[5]
+    x_act = ACTIVATIONS.get(x_activation)
+    if x_act is None or (x_act and not x_kept):
+        _refuse(call, f"unknown activation {x_activation!r} of x" if x_act is None else "the activation of x goes with an x in 8 bits")
     mats, of = ((w.shape[0],), (groups,)) if grouped else ((), ())
     of_in, of_out, of_w, of_b = (rows, fin), (rows, fout), of + (fout, fin), of + (fout,)
     if dx is None and need_dx:
-        dx = x.new_empty(of_in)
+        dx = dy.new_empty(of_in)
     if dw is None and need_dw:
-        dw = x.new_empty(of_w)
+        dw = dy.new_empty(of_w)
     if db is None and need_db:
-        db = x.new_empty(of_b)
-    _run(call, layer, 1, device, [
-        _matrix(call, "dy", dy, device, dtype, of_out), _matrix(call, "x", x, device, dtype, of_in), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
-        None if pre is None else _matrix(call, "pre", pre, device, dtype, of_out), None if dx is None else _matrix(call, "dx", dx, device, dtype, of_in),
-        None if dw is None else _matrix(call, "dw", dw, device, dtype, of_w, grouped), None if db is None else _matrix(call, "db", db, device, dtype, of_b, grouped)])
+        db = dy.new_empty(of_b)
+    matrices = [
+        _matrix(call, "dy", dy, device, dtype, of_out), None if x_kept else _matrix(call, "x", x, device, dtype, of_in), _matrix(call, "w", w, device, dtype, mats + (fout, fin), grouped),
+        None if pre is None or pre_kept else _matrix(call, "pre", pre, device, dtype, of_out), None if dx is None else _matrix(call, "dx", dx, device, dtype, of_in),
+        None if dw is None else _matrix(call, "dw", dw, device, dtype, of_w, grouped), None if db is None else _matrix(call, "db", db, device, dtype, of_b, grouped)]
+    if x_kept or pre_kept:
+        _run_checkpoint("ps_linear_backward_checkpoint", layer, 1, device, matrices, _kept(call, "x", x, device, of_in) if x_kept else None, x_act,
+                        _kept(call, "pre", pre, device, of_out) if pre_kept else None)
+    else:
+        _run(call, layer, 1, device, matrices)
     return dx, dw, db
 
 
 def ps_linear_backward(dy, x, w, activation: str = "none", pre=None, need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
-                       dx=None, dw=None, db=None):
+                       dx=None, dw=None, db=None, x_activation: str = "none"):
     """Gradients (dx, dw, db) of ps_linear_forward for dy [rows, out]; pre as the forward pass wrote it, not needed without
-    an activation.  What is not needed is None; dx, dw and db may be given tensors.  The residual's gradient is dy."""
-    return _backward(dy, x, None, w, activation, pre, None, need_dx, need_dw, need_db, dx, dw, db)
+    an activation.  What is not needed is None; dx, dw and db may be given tensors.  The residual's gradient is dy.
+    pre and x may be Checkpoints; an x so held is x_activation of its values (that of the layer before, where its pre-activations were kept)."""
+    return _backward(dy, x, None, w, activation, pre, None, need_dx, need_dw, need_db, dx, dw, db, x_activation)
 
 
 def ps_grouped_linear_backward(dy, x, offsets, w, activation: str = "none", pre=None, weight_of_group=None, need_dx: bool = True,
-                               need_dw: bool = True, need_db: bool = True, dx=None, dw=None, db=None):
+                               need_dw: bool = True, need_db: bool = True, dx=None, dw=None, db=None, x_activation: str = "none"):
     """The same for rows in groups: dw [groups, out, in] and db [groups, out] are every group's own (of a worker, say, whatever
     matrix it used), zeros for a group without rows.  dw and db may be views into wider rows, for instance of a gradient buffer."""
-    return _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db)
+    return _backward(dy, x, offsets, w, activation, pre, weight_of_group, need_dx, need_dw, need_db, dx, dw, db, x_activation)
 
 
 @dataclass
