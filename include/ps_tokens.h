@@ -53,7 +53,7 @@ typedef struct {
 PS_API ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens* tokens, const ps_matrix* table, const ps_matrix* out,
                                       void* hip_stream);
 
-/* dtable[g][v] = scale * sum of dy[r] over the rows r of group g with token v, [n_groups][vocab][dim], summed in 32 bits, 32
+/* dtable[g][v] = scale * sum of dy[r] over the rows r of group g with token v, [n_groups][vocab][dim], summed in 32 bits, 16
  * rows after each other and these sums after each other (so a group's gradient has the same bits whatever else is in the
  * call), and rounded once; tokens that no row has get 0.  n_tables and table_of_group_dev are not looked at.  dtable
  * may not overlap dy or the tokens. */
@@ -78,8 +78,10 @@ typedef struct {
  * A logit of -infinity has probability 0.  A row of nothing else has -infinity, -infinity and 0 in norm, -infinity as log
  * probability, and no alternatives.  A row with a NaN or +infinity has NaN in what is a number (the largest excepted; NaN is no
  * alternative).  logp, top_logp and top_tokens may be NULL (the last two for top = 0 only), tokens without logp. */
+PS_API ps_status ps_logprob_workspace_bytes(const ps_logprob* l, uint64_t* bytes_out);
 PS_API ps_status ps_logprob_forward(const ps_logprob* l, const ps_tokens* tokens, const ps_matrix* logits, float* logp_dev, float* norm_dev,
-                                    float* top_logp_dev, int32_t* top_tokens_dev, void* hip_stream);
+                                    float* top_logp_dev, int32_t* top_tokens_dev, void* workspace_dev, uint64_t workspace_bytes,
+                                    void* hip_stream);
 
 /* dlogits [rows][vocab], rounded once, from the gradients of logp and of the entropy (either may be NULL: zeros), the logits
  * and what the forward pass wrote to norm.  dlogits may be the logits themselves, and no part of them else.  A row of nothing

@@ -10,81 +10,96 @@ struct CodeArgs {
     void* x;
     uint8_t *codes, *scales;
     int64_t x_row, row, scale_row, rows;
-    int32_t cols, cols_to, per_row, act;  // per_row: pieces of eight columns
+    int32_t cols, cols_to, pieces, each, act;  // pieces of eight columns of a row; rows of a block
     Groups groups;
 };
 
-// A thread takes eight columns of a row, four times; neighbours in a block take neighbouring pieces.  Bound by memory.
+// A block takes `each` rows (up to 64), a thread pieces of eight columns of them.  Bound by memory: CODE_AHEAD pieces are asked for together,
+// without a branch between them, at which the compiler would wait; a row's last piece, where it is partial, is read again.
 constexpr int CODE_AHEAD = 4;
+
+struct Piece {
+    int64_t row;
+    int col, n;  // n: columns that exist
+};
+__device__ __forceinline__ Piece piece_of(const CodeArgs& a, int64_t first, int item)
+{
+    const int line = (int)((uint32_t)item / (uint32_t)a.pieces), col = (int)((uint32_t)item % (uint32_t)a.pieces) * 8;
+    return {first + line, col, min(8, a.cols - col)};
+}
 
 template <class T>
 __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
 {
-    const int64_t total = a.rows * a.per_row;
-    for (int64_t first = (int64_t)blockIdx.x * (256 * CODE_AHEAD); first < total; first += (int64_t)gridDim.x * (256 * CODE_AHEAD)) {
-        const int64_t row0 = first / a.per_row;
-        const uint32_t rem = (uint32_t)(first - row0 * a.per_row);
-        float v[CODE_AHEAD][8];
-        int64_t row[CODE_AHEAD];
-        int col[CODE_AHEAD], n[CODE_AHEAD];
-#pragma unroll
-        for (int i = 0; i < CODE_AHEAD; ++i) {
-            const uint32_t at = rem + i * 256 + threadIdx.x;
-            row[i] = row0 + at / (uint32_t)a.per_row;
-            col[i] = (int)(at % (uint32_t)a.per_row) * 8;
-            n[i] = row[i] < a.rows && group_of_row(a.groups, row[i]) >= 0 ? min(8, a.cols - col[i]) : 0;
-            const T* from = static_cast<const T*>(a.x) + row[i] * a.x_row + col[i];
-            if (n[i] == 8)
-                load_n(from, v[i]);
-            else
-                load_some(from, n[i], v[i]);
+    __shared__ int inside[64];  // whether a row is in a group
+    for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
+        const int items = (int)min((int64_t)a.each, a.rows - first) * a.pieces;
+        if (a.groups.offsets) {
+            if (threadIdx.x < 64) inside[threadIdx.x] = groups_of_rows(a.groups, first) >= 0;
+            __syncthreads();
         }
+        for (int at = threadIdx.x; at - (int)threadIdx.x < items; at += 256 * CODE_AHEAD) {
+            T raw[CODE_AHEAD][8];
+            Piece p[CODE_AHEAD];
 #pragma unroll
-        for (int i = 0; i < CODE_AHEAD; ++i) checkpoint_store(a.codes + row[i] * a.row, a.scales + row[i] * a.scale_row, col[i], n[i], v[i]);
+            for (int i = 0; i < CODE_AHEAD; ++i) {
+                p[i] = piece_of(a, first, min(at + i * 256, items - 1));
+                if (a.cols >= 8) __builtin_memcpy(raw[i], static_cast<const T*>(a.x) + p[i].row * a.x_row + min(p[i].col, a.cols - 8), sizeof(raw[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < CODE_AHEAD; ++i) {
+                float v[8];
+                if (p[i].n < 8) {
+                    load_some(static_cast<const T*>(a.x) + p[i].row * a.x_row + p[i].col, p[i].n, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = to_float(raw[i][e]);
+                }
+                // (all four lanes of a block are there or none is: pieces are whole blocks)
+                const bool there = at + i * 256 < items && (!a.groups.offsets || inside[p[i].row - first]);
+                checkpoint_store(a.codes + p[i].row * a.row, a.scales + p[i].row * a.scale_row, p[i].col, there ? p[i].n : 0, v);
+            }
+        }
+        if (a.groups.offsets) __syncthreads();  // inside is written again
     }
 }
 
 template <class T>
 __global__ __launch_bounds__(256) void decode_kernel(CodeArgs a)
 {
-    const int64_t total = a.rows * a.per_row;
-    for (int64_t first = (int64_t)blockIdx.x * (256 * CODE_AHEAD); first < total; first += (int64_t)gridDim.x * (256 * CODE_AHEAD)) {
-        const int64_t row0 = first / a.per_row;
-        const uint32_t rem = (uint32_t)(first - row0 * a.per_row);
-        uint32_t code[CODE_AHEAD][2], scale[CODE_AHEAD];
-        int64_t row[CODE_AHEAD];
-        int col[CODE_AHEAD], n[CODE_AHEAD];
+    for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
+        const int items = (int)min((int64_t)a.each, a.rows - first) * a.pieces;
+        for (int at = threadIdx.x; at < items; at += 256 * CODE_AHEAD) {
+            uint32_t code[CODE_AHEAD][2];
+            uint8_t scale[CODE_AHEAD];
+            Piece p[CODE_AHEAD];
 #pragma unroll
-        for (int i = 0; i < CODE_AHEAD; ++i) {
-            const uint32_t at = rem + i * 256 + threadIdx.x;
-            row[i] = row0 + at / (uint32_t)a.per_row;
-            col[i] = (int)(at % (uint32_t)a.per_row) * 8;
-            n[i] = row[i] < a.rows ? min(8, a.cols - col[i]) : 0;
-            scale[i] = 0;
-            if (n[i] > 0) scale[i] = a.scales[row[i] * a.scale_row + col[i] / PS_CHECKPOINT_BLOCK];
-            load_codes(a.codes + row[i] * a.row + col[i], n[i], code[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < CODE_AHEAD; ++i) {
-            if (row[i] >= a.rows) continue;
-            float v[8];
-            checkpoint_decode(code[i], scale[i], v);
-            if (a.act == PS_ACT_RELU) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_RELU>(v[e]);
-            } else if (a.act == PS_ACT_GELU) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_GELU>(v[e]);
-            } else if (a.act == PS_ACT_SILU) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_SILU>(v[e]);
+            for (int i = 0; i < CODE_AHEAD; ++i) {
+                p[i] = piece_of(a, first, min(at + i * 256, items - 1));
+                if (a.cols >= 8) __builtin_memcpy(code[i], a.codes + p[i].row * a.row + min(p[i].col, a.cols - 8), 8);
+                scale[i] = a.scales[p[i].row * a.scale_row + min(p[i].col, a.cols - 1) / PS_CHECKPOINT_BLOCK];
             }
-            T* to = static_cast<T*>(a.x) + row[i] * a.x_row + col[i];
-            const int m = min(8, a.cols_to - col[i]);
-            if (m == 8)
-                store_n(to, v);
-            else
-                store_some(to, m, v);
+#pragma unroll
+            for (int i = 0; i < CODE_AHEAD; ++i) {
+                if (at + i * 256 >= items) continue;
+                float v[8];
+                if (p[i].n < 8) {
+                    load_codes(a.codes + p[i].row * a.row + p[i].col, p[i].n, code[i]);
+                    if (p[i].n <= 0) scale[i] = 127;  // behind the columns: 0 whatever is there
+                }
+                checkpoint_decode(code[i], scale[i], v);
+                if (a.act == PS_ACT_RELU) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_RELU>(v[e]);
+                } else if (a.act == PS_ACT_GELU) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_GELU>(v[e]);
+                } else if (a.act == PS_ACT_SILU) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_SILU>(v[e]);
+                }
+                store_columns(static_cast<T*>(a.x) + p[i].row * a.x_row + p[i].col, min(8, a.cols_to - p[i].col), v);
+            }
         }
     }
 }
@@ -111,12 +126,17 @@ CodeArgs code_args(const Groups& groups, int64_t rows, int64_t cols, const ps_ma
     a.scale_row = c.scale_row;
     a.rows = rows;
     a.cols = a.cols_to = (int32_t)cols;
-    a.per_row = (int32_t)up(cols, PS_CHECKPOINT_BLOCK) * CHECKPOINT_LANES;
+    a.pieces = (int32_t)up(cols, PS_CHECKPOINT_BLOCK) * CHECKPOINT_LANES;
     a.groups = groups;
     return a;
 }
 
-dim3 code_grid(const CodeArgs& a) { return dim3((uint32_t)std::min<int64_t>(up(a.rows * a.per_row, 256 * CODE_AHEAD), 1 << 20)); }
+// Rows of 2048 pieces together, or fewer where that leaves less than eight blocks to a compute unit.
+dim3 code_grid(CodeArgs& a)
+{
+    a.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2048 / a.pieces), a.rows / (8 * COMPUTE_UNITS)));
+    return dim3((uint32_t)std::min<int64_t>(up(a.rows, a.each), 1 << 22));
+}
 
 ps_status check_matrix_of_codes(const char* call, int32_t dtype, int64_t rows, int64_t cols, const ps_matrix* x, const ps_checkpoint* c)
 {
@@ -147,17 +167,19 @@ ps_status check_checkpoint(const char* call, const char* name, const ps_checkpoi
 
 void launch_checkpoint_encode(int dtype, const Groups& groups, int64_t rows, int64_t cols, const ps_matrix& x, const ps_checkpoint& to, hipStream_t s)
 {
-    const CodeArgs a = code_args(groups, rows, cols, x, to);
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(encode_kernel<decltype(t)>, code_grid(a), dim3(256), 0, s, a); });
+    CodeArgs a = code_args(groups, rows, cols, x, to);
+    const dim3 grid = code_grid(a);
+    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(encode_kernel<decltype(t)>, grid, dim3(256), 0, s, a); });
 }
 
 void launch_checkpoint_decode(int dtype, int64_t rows, int64_t cols, const ps_checkpoint& from, int activation, const ps_matrix& x, int64_t cols_to, hipStream_t s)
 {
     CodeArgs a = code_args(Groups{}, rows, cols, x, from);
     a.cols_to = (int32_t)cols_to;
-    a.per_row = (int32_t)up(cols_to, 8);
+    a.pieces = (int32_t)up(cols_to, 8);
     a.act = activation;
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(decode_kernel<decltype(t)>, code_grid(a), dim3(256), 0, s, a); });
+    const dim3 grid = code_grid(a);
+    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(decode_kernel<decltype(t)>, grid, dim3(256), 0, s, a); });
 }
 
 }  // namespace ps

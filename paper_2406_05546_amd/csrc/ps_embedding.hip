@@ -1,8 +1,8 @@
 // Rows of a table for given tokens, and the gradient of the table (include/ps_tokens.h).
 //
 // The gradient is summed over sorted tokens: rows are put in the order of (group, token), those of equal ones staying in the order
-// that they have (a stable radix sort, 8 bits at a time), and so the rows of one sum lie one behind the other.  No atomics: the
-// same order every time.
+// that they have, and so the rows of one sum lie one behind the other.  No atomics: the same order every time.  The table is cleared
+// as a whole beside the sorting, and the tokens that are there are written over it.
 #include "../../include/ps_tokens.h"
 #include "ps_linear.h"
 #include "ps_tokens.h"
@@ -20,77 +20,60 @@ struct LookupArgs {
     const void *table, *tokens;
     void* out;
     int64_t table_row, table_matrix, out_row, token_stride, vocab;
-    int32_t rows, dim, pieces;
+    int32_t rows, dim, pieces, each;  // pieces of a row; rows of a block
     float scale;
     Groups groups;
 };
 
-// A thread takes 16 bytes of a row, four times; neighbours in a block take neighbouring pieces of the same row or the next one.  Bound
-// by memory: the four are asked for together.
+// A block takes `each` rows (up to 64).  Its first wavefront finds where they come from, one row to a lane; then every thread takes
+// pieces of E columns, LOOKUP_AHEAD of them asked for together.  A row's last piece ends with the row, and so covers columns of the one
+// before again: no piece is partial (E is 1 for rows shorter than 16 bytes).
 constexpr int LOOKUP_AHEAD = 4;
+constexpr int64_t NO_GROUP = -1, NO_TOKEN = -2;
 
-template <class T, class TOKEN>
+template <class T, class TOKEN, int E>
 __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a)
 {
-    constexpr int E = 16 / sizeof(T);
-    const int64_t total = (int64_t)a.rows * a.pieces;
-    for (int64_t first = (int64_t)blockIdx.x * (256 * LOOKUP_AHEAD); first < total; first += (int64_t)gridDim.x * (256 * LOOKUP_AHEAD)) {
-        const int64_t row0 = first / a.pieces;
-        const uint32_t rem = (uint32_t)(first - row0 * a.pieces);
-        int64_t row[LOOKUP_AHEAD], token[LOOKUP_AHEAD];
-        int col[LOOKUP_AHEAD], matrix[LOOKUP_AHEAD];
-        T raw[LOOKUP_AHEAD][E];
+    __shared__ int64_t source[64];
+    for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
+        const int each = (int)min((int64_t)a.each, a.rows - first);
+        if (threadIdx.x < 64) {
+            const int64_t r = min(first + threadIdx.x, (int64_t)a.rows - 1);
+            const int64_t token = static_cast<const TOKEN*>(a.tokens)[r * a.token_stride];
+            const int g = groups_of_rows(a.groups, first);
+            int64_t from = NO_GROUP;
+            if (g >= 0) from = token >= 0 && token < a.vocab ? group_matrix(a.groups, g) * a.table_matrix + token * a.table_row : NO_TOKEN;
+            source[threadIdx.x] = from;
+        }
+        __syncthreads();
+        const int items = each * a.pieces;
+        for (int at = threadIdx.x; at < items; at += 256 * LOOKUP_AHEAD) {
+            T raw[LOOKUP_AHEAD][E];
+            int64_t from[LOOKUP_AHEAD];
+            int line[LOOKUP_AHEAD], col[LOOKUP_AHEAD];
 #pragma unroll
-        for (int i = 0; i < LOOKUP_AHEAD; ++i) {
-            const uint32_t at = rem + i * 256 + threadIdx.x;
-            row[i] = row0 + at / (uint32_t)a.pieces;
-            col[i] = (int)(at % (uint32_t)a.pieces) * E;
-            matrix[i] = -1;
-            if (row[i] < a.rows) {
-                token[i] = static_cast<const TOKEN*>(a.tokens)[row[i] * a.token_stride];
-                const int g = group_of_row(a.groups, row[i]);
-                if (g >= 0) matrix[i] = group_matrix(a.groups, g);
+            for (int i = 0; i < LOOKUP_AHEAD; ++i) {
+                const uint32_t item = min(at + i * 256, items - 1);
+                line[i] = (int)(item / (uint32_t)a.pieces);
+                col[i] = min((int)(item % (uint32_t)a.pieces) * E, a.dim - E);
+                from[i] = source[line[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < LOOKUP_AHEAD; ++i) __builtin_memcpy(raw[i], static_cast<const T*>(a.table) + max(from[i], (int64_t)0) + col[i], sizeof(raw[i]));
+#pragma unroll
+            for (int i = 0; i < LOOKUP_AHEAD; ++i) {
+                if (at + i * 256 >= items || from[i] == NO_GROUP) continue;
+                float v[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = from[i] == NO_TOKEN ? 0.f : to_float(raw[i][e]) * a.scale;
+                store_n(static_cast<T*>(a.out) + (first + line[i]) * a.out_row + col[i], v);
             }
         }
-#pragma unroll
-        for (int i = 0; i < LOOKUP_AHEAD; ++i) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) raw[i][e] = T{};
-            if (matrix[i] < 0 || token[i] < 0 || token[i] >= a.vocab) continue;
-            const T* from = static_cast<const T*>(a.table) + matrix[i] * a.table_matrix + token[i] * a.table_row + col[i];
-            if (col[i] + E <= a.dim) {
-                __builtin_memcpy(raw[i], from, 16);
-            } else {
-                asm volatile("" : "+v"(from));
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col[i] + e < a.dim) raw[i][e] = from[e];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < LOOKUP_AHEAD; ++i) {
-            if (matrix[i] < 0) continue;
-            float v[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = to_float(raw[i][e]) * a.scale;
-            if (token[i] < 0 || token[i] >= a.vocab) {  // also where the scale times 0 is not 0
-#pragma unroll
-                for (int e = 0; e < E; ++e) v[e] = 0.f;
-            }
-            T* to = static_cast<T*>(a.out) + row[i] * a.out_row + col[i];
-            if (col[i] + E <= a.dim)
-                store_n(to, v);
-            else
-                store_some(to, a.dim - col[i], v);
-        }
+        __syncthreads();  // source is written again
     }
 }
 
 // ---- sorting -----------------------------------------------------------------------------------------------------------
-
-// A tile of keys is ranked by a block: every wavefront has 64 at a time, finds with eight ballots which of them have the same
-// digit, and counts them in a column of its own, so that equal digits stay in order.
-constexpr int DIGITS = 256, TILE_WAVES = 16, TILE_EACH = 8, SORT_TILE = TILE_WAVES * 64 * TILE_EACH;
 
 struct SortArgs {
     const void* tokens;
@@ -100,14 +83,118 @@ struct SortArgs {
     Groups groups;
 };
 
+// The key of row `first` + lane, for a whole wavefront; `behind` for rows past the last.
 template <class TOKEN>
-__device__ __forceinline__ uint32_t key_of_row(const SortArgs& a, int r)
+__device__ __forceinline__ uint32_t key_of_row(const SortArgs& a, int64_t first, uint32_t behind)
 {
-    const int64_t t = static_cast<const TOKEN*>(a.tokens)[r * a.token_stride];
-    if (t < 0 || t >= a.vocab) return a.none;
-    const int g = group_of_row(a.groups, r);
-    return g < 0 ? a.none : (uint32_t)(g * a.vocab + t);
+    if (first >= a.rows) return behind;
+    const int64_t r = first + (threadIdx.x & 63);
+    const int64_t t = static_cast<const TOKEN*>(a.tokens)[min(r, (int64_t)a.rows - 1) * a.token_stride];
+    const int g = groups_of_rows(a.groups, first);
+    if (r >= a.rows) return behind;
+    return g < 0 || t < 0 || t >= a.vocab ? a.none : (uint32_t)(g * a.vocab + t);
 }
+
+// What is cleared: lines of contiguous bytes, in blocks of CLEAR_BYTES or whole lines.
+constexpr int CLEAR_BYTES = 65536;
+struct ClearArgs {
+    char* base;
+    int64_t lines, per_matrix, line_stride, matrix_stride, line_bytes;  // line l: matrix l / per_matrix, row l % per_matrix
+    int32_t size, blocks_per_line, lines_per_block;                     // size of an element; one of the two others is 1
+    uint32_t blocks;
+};
+
+__device__ __forceinline__ void clear_line(char* to, int64_t first, int64_t end, int size, int t, int threads)
+{
+    for (int64_t at = first + (int64_t)t * 16; at < end; at += (int64_t)threads * 16) {
+        if (at + 16 <= end) {
+            const uintx4 zero = {0, 0, 0, 0};
+            __builtin_memcpy(to + at, &zero, 16);
+        } else if (size == 4) {
+            for (int64_t i = at; i < end; i += 4) *reinterpret_cast<uint32_t*>(to + i) = 0;
+        } else {
+            for (int64_t i = at; i < end; i += 2) *reinterpret_cast<uint16_t*>(to + i) = 0;
+        }
+    }
+}
+__device__ __forceinline__ void clear_block(const ClearArgs& a, uint32_t block)
+{
+    auto line_at = [&](int64_t l) { return a.base + l / a.per_matrix * a.matrix_stride + l % a.per_matrix * a.line_stride; };
+    if (a.lines_per_block == 1) {
+        const int64_t first = (int64_t)(block % a.blocks_per_line) * CLEAR_BYTES;
+        clear_line(line_at(block / a.blocks_per_line), first, min(first + CLEAR_BYTES, a.line_bytes), a.size, threadIdx.x, blockDim.x);
+        return;
+    }
+    // short lines: so many threads to a line as it has pieces
+    const int pieces = (int)((a.line_bytes + 15) / 16), threads = blockDim.x / pieces * pieces, at = threadIdx.x / pieces, step = blockDim.x / pieces;
+    const int64_t first = (int64_t)block * a.lines_per_block, end = min(first + a.lines_per_block, a.lines);
+    if (step == 0) {
+        for (int64_t l = first; l < end; ++l) clear_line(line_at(l), 0, a.line_bytes, a.size, threadIdx.x, blockDim.x);
+    } else if ((int)threadIdx.x < threads) {
+        for (int64_t l = first + at; l < end; l += step) clear_line(line_at(l), 0, a.line_bytes, a.size, threadIdx.x % pieces, pieces);
+    }
+}
+
+// Up to RANK_MOST rows: a row's place is the number of keys below its own, and of equal ones before it, which is counted.  Wavefronts compare
+// the keys of their RANK_ROWS rows with RANK_KEYS others, 32-bit comparisons of which the chip does 1.9e13 in a second (16384 rows:
+// 14 us); next to them the table is cleared, which is bound by memory and takes longer for all but small ones.
+constexpr int RANK_ROWS = 256, RANK_KEYS = 1024, RANK_MOST = 16384;
+
+template <class TOKEN>
+__global__ __launch_bounds__(RANK_ROWS) void rank_and_clear_kernel(SortArgs a, uint32_t rank_blocks, int parts, uint32_t* __restrict__ keys, uint16_t* __restrict__ counts, ClearArgs clear)
+{
+    if (blockIdx.x >= rank_blocks) {
+        clear_block(clear, blockIdx.x - rank_blocks);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) uint32_t others[RANK_KEYS];
+    const int part = blockIdx.x % parts, r = blockIdx.x / parts * RANK_ROWS + threadIdx.x, first = part * RANK_KEYS;
+    uint32_t there[RANK_KEYS / RANK_ROWS];
+#pragma unroll
+    for (int i = 0; i < RANK_KEYS / RANK_ROWS; ++i) {
+        there[i] = key_of_row<TOKEN>(a, scalar(first + i * RANK_ROWS + (threadIdx.x & ~63)), ~0u);  // (above every key)
+    }
+#pragma unroll
+    for (int i = 0; i < RANK_KEYS / RANK_ROWS; ++i) others[i * RANK_ROWS + threadIdx.x] = there[i];
+    const int wave_first = scalar(r & ~63);
+    const uint32_t key = key_of_row<TOKEN>(a, wave_first, a.none);
+    __syncthreads();
+    // keys of 64 rows before the wavefront's own count where they are equal, too; those of rows behind only where they are below
+    uint32_t n = 0;
+    auto count = [&](int from, int to, uint32_t below) __attribute__((always_inline)) {
+        for (int k = from; k < to; k += 16) {
+            uintx4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uintx4*>(&others[k + 4 * i]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n += x[i / 4][i % 4] < below;
+        }
+    };
+    const int before = min(max(wave_first - first, 0), RANK_KEYS), behind = min(max(wave_first + 64 - first, 0), RANK_KEYS);
+    count(0, before, key + 1);
+    for (int k = before; k < behind; ++k) n += others[k] < key || (others[k] == key && first + k < r);
+    count(behind, RANK_KEYS, key);
+    if (r >= a.rows) return;
+    if (part == 0) keys[r] = key;
+    counts[(int64_t)part * a.rows + r] = (uint16_t)n;
+}
+
+__global__ __launch_bounds__(64) void rank_place_kernel(int rows, int parts, const uint32_t* __restrict__ keys, const uint16_t* __restrict__ counts, uint32_t* __restrict__ keys_to,
+                                                        uint32_t* __restrict__ order_to)
+{
+    const int r = blockIdx.x * 64 + threadIdx.x;
+    if (r >= rows) return;
+    uint32_t n = 0;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) n += counts[(int64_t)p * rows + r];
+    keys_to[n] = keys[r];
+    order_to[n] = (uint32_t)r;
+}
+
+// More rows: a stable radix sort of their keys, 8 bits at a time.  A tile of keys is ranked by a block: every wavefront has 64 at a time,
+// finds with eight ballots which of them have the same digit, and counts them in a column of its own, so that equal digits stay in order.
+constexpr int DIGITS = 256, TILE_WAVES = 4, TILE_EACH = 4, SORT_TILE = TILE_WAVES * 64 * TILE_EACH;
+static_assert(TILE_WAVES * 64 == DIGITS, "a thread for each digit");
 
 struct TileCounts {
     uint32_t at[TILE_WAVES][DIGITS];  // first counts, then where each wavefront's keys of a digit go
@@ -139,7 +226,7 @@ __device__ __forceinline__ void rank_keys(TileCounts& c, const uint32_t (&key)[T
     }
 }
 
-// Sum of v over the block's threads before this one, of DIGITS threads that call this.
+// Sum of v over the block's threads before this one.
 __device__ __forceinline__ uint32_t sum_before(TileCounts& c, uint32_t v)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -149,7 +236,7 @@ __device__ __forceinline__ uint32_t sum_before(TileCounts& c, uint32_t v)
         const uint32_t other = __shfl_up(upto, d, 64);
         if (lane >= d) upto += other;
     }
-    if (threadIdx.x < DIGITS && lane == 63) c.wave_sum[wave] = upto;
+    if (lane == 63) c.wave_sum[wave] = upto;
     __syncthreads();
     uint32_t s = upto - v;
     for (int w = 0; w < DIGITS / 64; ++w)
@@ -157,91 +244,46 @@ __device__ __forceinline__ uint32_t sum_before(TileCounts& c, uint32_t v)
     return s;
 }
 
-// All of it in one block: up to SORT_TILE rows.
-template <class TOKEN>
-__global__ __launch_bounds__(TILE_WAVES * 64) void sort_one_kernel(SortArgs a, int passes, uint32_t* __restrict__ keys, uint32_t* __restrict__ order)
-{
-    __shared__ TileCounts counts;
-    __shared__ uint32_t key_at[SORT_TILE];
-    __shared__ uint16_t row_at[SORT_TILE];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * 64 * TILE_EACH + lane;
-    uint32_t key[TILE_EACH], rank[TILE_EACH];
-    uint16_t row[TILE_EACH];
-#pragma unroll
-    for (int i = 0; i < TILE_EACH; ++i) {
-        const int r = first + i * 64;
-        row[i] = (uint16_t)r;
-        key[i] = r < a.rows ? key_of_row<TOKEN>(a, r) : ~0u;  // behind all others, and the last among equal digits
-    }
-    for (int pass = 0; pass < passes; ++pass) {
-        rank_keys(counts, key, 8 * pass, rank);
-        __syncthreads();
-        uint32_t total = 0;
-        if (threadIdx.x < DIGITS)
-            for (int w = 0; w < TILE_WAVES; ++w) total += counts.at[w][threadIdx.x];
-        uint32_t to = sum_before(counts, total);
-        if (threadIdx.x < DIGITS)
-            for (int w = 0; w < TILE_WAVES; ++w) {
-                const uint32_t n = counts.at[w][threadIdx.x];
-                counts.at[w][threadIdx.x] = to;
-                to += n;
-            }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < TILE_EACH; ++i) {
-            const uint32_t p = counts.at[wave][key[i] >> (8 * pass) & (DIGITS - 1)] + rank[i];
-            key_at[p] = key[i];
-            row_at[p] = row[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < TILE_EACH; ++i) {
-            key[i] = key_at[first + i * 64];
-            row[i] = row_at[first + i * 64];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < TILE_EACH; ++i) {
-        if (first + i * 64 >= a.rows) continue;
-        keys[first + i * 64] = key[i];
-        order[first + i * 64] = row[i];
-    }
-}
-
-// One pass over more tiles.  keys and order null: the first pass, whose keys are made from the tokens.
+// keys null: the first pass, whose keys are made from the tokens.
 template <class TOKEN>
 __device__ __forceinline__ void tile_keys(const SortArgs& a, const uint32_t* keys, int tile, uint32_t (&key)[TILE_EACH])
 {
-    const int64_t first = (int64_t)tile * SORT_TILE + (threadIdx.x >> 6) * 64 * TILE_EACH + (threadIdx.x & 63);
+    const int64_t first = (int64_t)tile * SORT_TILE + scalar(threadIdx.x >> 6) * 64 * TILE_EACH;
 #pragma unroll
     for (int i = 0; i < TILE_EACH; ++i) {
-        const int64_t r = first + i * 64;
-        key[i] = r >= a.rows ? ~0u : keys ? keys[r] : key_of_row<TOKEN>(a, (int)r);
+        const int64_t r = first + i * 64 + (threadIdx.x & 63);
+        if (keys)
+            key[i] = r < a.rows ? keys[r] : ~0u;  // behind all others, and the last among equal digits
+        else
+            key[i] = key_of_row<TOKEN>(a, first + i * 64, ~0u);
     }
 }
 
-// Counts of every digit: [digit][tile]
+// Counts of every digit: [digit][tile].  In the first pass the table is cleared beside it.
 template <class TOKEN>
-__global__ __launch_bounds__(TILE_WAVES * 64) void sort_count_kernel(SortArgs a, int shift, const uint32_t* __restrict__ keys, uint32_t* __restrict__ counts, int tiles)
+__global__ __launch_bounds__(DIGITS) void sort_count_kernel(SortArgs a, int shift, const uint32_t* __restrict__ keys, uint32_t* __restrict__ counts, int tiles, ClearArgs clear)
 {
     __shared__ TileCounts c;
+    if ((int)blockIdx.x >= tiles) {
+        clear_block(clear, blockIdx.x - tiles);
+        return;
+    }
     uint32_t key[TILE_EACH], rank[TILE_EACH];
     tile_keys<TOKEN>(a, keys, blockIdx.x, key);
     rank_keys(c, key, shift, rank);
     __syncthreads();
-    if (threadIdx.x >= DIGITS) return;
     uint32_t total = 0;
     for (int w = 0; w < TILE_WAVES; ++w) total += c.at[w][threadIdx.x];
     counts[(int64_t)threadIdx.x * tiles + blockIdx.x] = total;
 }
 
 // A block for each digit: its counts to sums over the tiles before, their total to counts[DIGITS * tiles + digit].
-__global__ __launch_bounds__(256) void sort_scan_kernel(uint32_t* __restrict__ counts, int tiles)
+__global__ __launch_bounds__(DIGITS) void sort_scan_kernel(uint32_t* __restrict__ counts, int tiles)
 {
     __shared__ TileCounts c;
     uint32_t* mine = counts + (int64_t)blockIdx.x * tiles;
     uint32_t before = 0;
-    for (int t0 = 0; t0 < tiles; t0 += 256) {
+    for (int t0 = 0; t0 < tiles; t0 += DIGITS) {
         const int t = t0 + threadIdx.x;
         const uint32_t n = t < tiles ? mine[t] : 0;
         const uint32_t s = sum_before(c, n);
@@ -253,24 +295,19 @@ __global__ __launch_bounds__(256) void sort_scan_kernel(uint32_t* __restrict__ c
 }
 
 template <class TOKEN>
-__global__ __launch_bounds__(TILE_WAVES * 64) void sort_place_kernel(SortArgs a, int shift, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ order,
-                                                                     const uint32_t* __restrict__ counts, int tiles, uint32_t* __restrict__ keys_to,
-                                                                     uint32_t* __restrict__ order_to)
+__global__ __launch_bounds__(DIGITS) void sort_place_kernel(SortArgs a, int shift, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ order,
+                                                            const uint32_t* __restrict__ counts, int tiles, uint32_t* __restrict__ keys_to, uint32_t* __restrict__ order_to)
 {
     __shared__ TileCounts c;
     uint32_t key[TILE_EACH], rank[TILE_EACH];
     tile_keys<TOKEN>(a, keys, blockIdx.x, key);
     rank_keys(c, key, shift, rank);
     __syncthreads();
-    const uint32_t of_digit = threadIdx.x < DIGITS ? counts[(int64_t)DIGITS * tiles + threadIdx.x] : 0;
-    uint32_t to = sum_before(c, of_digit);
-    if (threadIdx.x < DIGITS) {
-        to += counts[(int64_t)threadIdx.x * tiles + blockIdx.x];
-        for (int w = 0; w < TILE_WAVES; ++w) {
-            const uint32_t n = c.at[w][threadIdx.x];
-            c.at[w][threadIdx.x] = to;
-            to += n;
-        }
+    uint32_t to = sum_before(c, counts[(int64_t)DIGITS * tiles + threadIdx.x]) + counts[(int64_t)threadIdx.x * tiles + blockIdx.x];
+    for (int w = 0; w < TILE_WAVES; ++w) {
+        const uint32_t n = c.at[w][threadIdx.x];
+        c.at[w][threadIdx.x] = to;
+        to += n;
     }
     __syncthreads();
     const int wave = threadIdx.x >> 6;
@@ -291,7 +328,7 @@ __global__ __launch_bounds__(TILE_WAVES * 64) void sort_place_kernel(SortArgs a,
 // the gradient, those of a longer run go to `partial`, of which each PIECE places in the order have two rows: for the piece, not the
 // first of its run, that begins in them, and for the first piece of a run longer than that.  (There cannot be more: two pieces
 // of a run begin PIECE places apart.)
-constexpr int PIECE = 32, SUM_AHEAD = 8;
+constexpr int PIECE = 16, SUM_AHEAD = 8;
 
 struct SumArgs {
     const void* dy;
@@ -325,14 +362,16 @@ __device__ __forceinline__ T* row_of_key(const SumArgs& a, uint32_t key)
     return static_cast<T*>(a.dtable) + (int64_t)g * a.table_matrix + (int64_t)v * a.table_row;
 }
 
-// Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.
-template <class T>
+// Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.  A lane
+// whose columns would go past the row's end takes the last E of the row, which others have too (E is 1 for rows shorter than 16 bytes).  Bound by
+// memory: SUM_AHEAD rows are asked for while as many are added up, without a branch between them, at which the compiler would wait.
+template <class T, int E>
 __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
 {
-    constexpr int E = 16 / sizeof(T);
     const int lane = threadIdx.x & 63;
     const int64_t w = (int64_t)blockIdx.x * 4 + scalar(threadIdx.x >> 6);
-    const int chunk = (int)(w / a.col_blocks), col = (int)(w % a.col_blocks) * 64 * E + lane * E, n = min(E, a.dim - col);
+    const int chunk = (int)(w / a.col_blocks), own = (int)(w % a.col_blocks) * 64 * E + lane * E, col = min(own, a.dim - E);
+    const bool there = own < a.dim;
     if (chunk >= a.chunks) return;
     const int p0 = chunk * PIECE, p = p0 + lane;
     const uint32_t key = p < a.rows ? a.keys[p] : ~0u;
@@ -349,107 +388,107 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
         if (!upto) run = first;
     }
     const unsigned long long pieces = __ballot((lane - run) % PIECE == 0) & exist;
-    unsigned long long todo = pieces & ((1ull << PIECE) - 1);
+    const unsigned long long todo = pieces & ((1ull << PIECE) - 1);
     if (!todo) return;
     // places from the first piece's beginning to where a piece that begins behind the chunk, or nothing, follows
     const int from = __builtin_ctzll(todo);
     const unsigned long long behind = pieces >> PIECE << PIECE | ~exist;  // (rows that exist come first)
-    const int to = behind ? __builtin_ctzll(behind) : 64;
+    const int to = __builtin_ctzll(behind);                               // (at most 2 * PIECE - 1)
+    // the last places of pieces; those that are not all of their run
+    const unsigned long long ends = (pieces | ~exist) >> 1;
+    const unsigned long long goes_on = exist >> 1 & ~(begins >> 1), starts_run = begins & pieces;
     float sum[E] = {};
-    for (int at = from; at < to; at += SUM_AHEAD) {
-        float x[SUM_AHEAD][E];
-        T raw[SUM_AHEAD][E];
+    T now[SUM_AHEAD][E], then[SUM_AHEAD][E];
+    auto take = [&](int at, T (&raw)[SUM_AHEAD][E]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < SUM_AHEAD; ++u) {
-            if (at + u >= to || n <= 0) continue;
-            const T* src = static_cast<const T*>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(row, at + u) * a.dy_row + col;
-            if (n == E) {
-                __builtin_memcpy(raw[u], src, 16);
-            } else {
-                asm volatile("" : "+v"(src));
-#pragma unroll
-                for (int e = 0; e < E; ++e) raw[u][e] = e < n ? src[e] : T{};
-            }
+            const int64_t r = (uint32_t)__builtin_amdgcn_readlane(row, min(at + u, to - 1));
+            __builtin_memcpy(raw[u], static_cast<const T*>(a.dy) + r * a.dy_row + col, sizeof(raw[u]));
         }
+    };
+    take(from, now);
+    for (int at = from; at < to; at += SUM_AHEAD) {
+        if (at + SUM_AHEAD < to) take(at + SUM_AHEAD, then);
 #pragma unroll
         for (int u = 0; u < SUM_AHEAD; ++u) {
-            if (at + u >= to) continue;
             const int place = at + u;
+            if (place >= to) continue;
             const bool first = pieces >> place & 1;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                x[u][e] = n > 0 ? to_float(raw[u][e]) : 0.f;
-                sum[e] = first ? x[u][e] : sum[e] + x[u][e];
+                const float x = to_float(now[u][e]);
+                sum[e] = first ? x : sum[e] + x;
             }
-            // the piece's end: the next place is another piece's first, or none
-            if (place + 1 < 64 && !((pieces | ~exist) >> (place + 1) & 1)) continue;
-            const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(key, place);
-            const unsigned long long starts = pieces & (~0ull >> (63 - place));
-            const int start = 63 - __builtin_clzll(starts), run_at = __builtin_amdgcn_readlane(run, start);
-            const bool goes_on = place + 1 < 64 && (exist >> (place + 1) & 1) && !(begins >> (place + 1) & 1);
-            if (run_at == start && !goes_on) {
+            if (!(ends >> place & 1) || !there) continue;
+            const int start = 63 - __builtin_clzll(pieces & (~0ull >> (63 - place)));
+            const bool whole_start = starts_run >> start & 1;
+            if (whole_start && !(goes_on >> place & 1)) {
                 float v[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[e] = sum[e] * a.scale;
-                if (n > 0) store_columns(row_of_key<T>(a, k) + col, n, v);
-            } else if (n > 0) {
-                store_columns(a.partial + (2 * (int64_t)chunk + (run_at == start)) * a.dim + col, n, sum);
+                store_n(row_of_key<T>(a, (uint32_t)__builtin_amdgcn_readlane(key, place)) + col, v);
+            } else {
+                store_n(a.partial + (2 * (int64_t)chunk + whole_start) * a.dim + col, sum);
             }
         }
+#pragma unroll
+        for (int u = 0; u < SUM_AHEAD; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) now[u][e] = then[u][e];
     }
 }
 
-// Adds up the pieces of longer runs, and clears the rows of tokens that are nowhere.  Wavefronts [chunk][columns] of the
-// first `join` blocks: the run longer than PIECE that begins in the chunk; of the others, 64 rows of the tables each.
-template <class T>
-__global__ __launch_bounds__(256) void join_and_clear_kernel(SumArgs a, uint32_t join)
+// Adds up the pieces of longer runs.  A block for a chunk and 64 * E columns: the run longer than PIECE that begins in the chunk, if there is
+// one, a quarter of its pieces to each wavefront, one behind the other, and these four sums in order.
+template <class T, int E>
+__global__ __launch_bounds__(256) void join_runs_kernel(SumArgs a)
 {
-    constexpr int E = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63;
-    if (blockIdx.x >= join) {
-        const uint32_t first = ((blockIdx.x - join) * 4 + scalar(threadIdx.x >> 6)) * 64, key = first + lane;
-        if (first >= a.none) return;
-        int lo = 0, hi = a.rows;
-        while (lo < hi) {
-            const int mid = (int)(((uint32_t)lo + (uint32_t)hi) >> 1);
-            if (a.keys[mid] < key)
-                lo = mid + 1;
-            else
-                hi = mid;
+    __shared__ float meet[3][64][E + 1];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
+    const int64_t total = (int64_t)a.chunks * a.col_blocks;
+    for (int64_t block = blockIdx.x; block < total; block += gridDim.x) {
+        const int chunk = (int)(block / a.col_blocks), own = (int)(block % a.col_blocks) * 64 * E + lane * E, col = min(own, a.dim - E);
+        const int p0 = chunk * PIECE, p = p0 + lane;
+        const uint32_t key = p < a.rows ? a.keys[p] : ~0u, before = p0 ? a.keys[p0 - 1] : ~0u;
+        const uint32_t previous = __shfl_up(key, 1, 64), later = __shfl_down(key, PIECE, 64);
+        const bool differs = lane ? key != previous : p0 == 0 || key != before;
+        const unsigned long long longer = __ballot(lane < PIECE && differs && p + PIECE < a.rows && key < a.none && key == later);
+        if (!longer) continue;  // (the same in all wavefronts)
+        const int at = __builtin_ctzll(longer);
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(key, at);
+        // its pieces: those whose first place has the key, counted 64 at a time
+        int pieces = 0;
+        for (bool more = true; more; pieces += 64) {
+            const int64_t q = p0 + at + (int64_t)(pieces + lane) * PIECE;
+            const unsigned long long same = __ballot(q < a.rows && a.keys[min(q, (int64_t)a.rows - 1)] == k);
+            more = same == ~0ull;
+            if (!more) pieces += __popcll(same) - 64;
         }
-        const bool absent = key < a.none && (lo >= a.rows || a.keys[lo] != key);
-        const float zero[E] = {};
-        for (unsigned long long todo = __ballot(absent); todo; todo &= todo - 1) {
-            T* to = row_of_key<T>(a, first + __builtin_ctzll(todo));
-            for (int col = lane * E; col < a.dim; col += 64 * E) store_columns(to + col, a.dim - col, zero);
+        const int each = (pieces + 3) / 4, first = min(wave * each, pieces), end = min(first + each, pieces);
+        float sum[E] = {};
+#pragma unroll 8
+        for (int i = first; i < end; ++i) {
+            float x[E];
+            load_n(a.partial + (2 * (int64_t)(chunk + i) + (i == 0)) * a.dim + col, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += x[e];
         }
-        return;
-    }
-    const int64_t w = (int64_t)blockIdx.x * 4 + scalar(threadIdx.x >> 6);
-    const int chunk = (int)(w / a.col_blocks), col = (int)(w % a.col_blocks) * 64 * E + lane * E, n = min(E, a.dim - col);
-    if (chunk >= a.chunks) return;
-    // the run that begins in the chunk and still goes on PIECE places behind
-    const int p0 = chunk * PIECE, p = p0 + lane;
-    const uint32_t key = p < a.rows ? a.keys[p] : ~0u, before = p0 ? a.keys[p0 - 1] : ~0u;
-    const uint32_t previous = __shfl_up(key, 1, 64), later = __shfl_down(key, PIECE, 64);
-    const bool differs = lane ? key != previous : p0 == 0 || key != before;
-    const unsigned long long longer = __ballot(lane < PIECE && differs && p + PIECE < a.rows && key < a.none && key == later);
-    if (!longer) return;
-    const int at = __builtin_ctzll(longer);
-    const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(key, at);
-    const int last_piece = (a.rows - 1 - (p0 + at)) / PIECE;
-    float sum[E] = {}, x[E];
-    for (int i = 0; i <= last_piece; ++i) {
-        if (i > 1 && a.keys[p0 + at + i * PIECE] != k) break;
-        const float* from = a.partial + (2 * (int64_t)(chunk + i) + (i == 0)) * a.dim + col;
-        if (n <= 0) continue;
-        load_columns<float>(from, 0, n, x);
+        if (wave) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += x[e];
-    }
+            for (int e = 0; e < E; ++e) meet[wave - 1][lane][e] = sum[e];
+        }
+        __syncthreads();
+        if (wave == 0 && own < a.dim) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] *= a.scale;
-    if (n > 0) store_columns(row_of_key<T>(a, k) + col, n, sum);
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] += meet[w][lane][e];
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] *= a.scale;
+            store_n(row_of_key<T>(a, k) + col, sum);
+        }
+        __syncthreads();  // what met is written again
+    }
 }
 
 // ---- entry points --------------------------------------------------------------------------------------------------------
@@ -476,7 +515,7 @@ ps_status check_embedding(const char* call, const ps_embedding* e, bool forward)
 
 struct GradientSpace {
     uint64_t keys[2], order[2], counts, partial, total;
-    int passes, tiles, chunks;
+    int passes, tiles, chunks, parts;
 };
 
 GradientSpace gradient_space(const ps_embedding& e)
@@ -484,22 +523,52 @@ GradientSpace gradient_space(const ps_embedding& e)
     GradientSpace g{};
     const uint64_t none = (uint64_t)e.n_groups * e.vocab;
     while (none >> (8 * g.passes)) ++g.passes;
-    g.tiles = (int)up(e.rows, SORT_TILE);
     g.chunks = (int)up(e.rows, PIECE);
+    if (e.rows <= RANK_MOST)
+        g.parts = (int)up(e.rows, RANK_KEYS);
+    else
+        g.tiles = (int)up(e.rows, SORT_TILE);
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
         const uint64_t here = at;
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    for (int i = 0; i < (g.tiles > 1 ? 2 : 1); ++i) {
+    for (int i = 0; i < 2; ++i) {
         g.keys[i] = take((uint64_t)e.rows * 4);
         g.order[i] = take((uint64_t)e.rows * 4);
     }
-    g.counts = take(g.tiles > 1 ? (uint64_t)DIGITS * (g.tiles + 1) * 4 : 0);
+    g.counts = take(g.tiles ? (uint64_t)DIGITS * (g.tiles + 1) * 4 : (uint64_t)g.parts * e.rows * 2);
     g.partial = take((uint64_t)2 * g.chunks * e.dim * 4);
     g.total = at;
     return g;
+}
+
+// Rows that lie one behind the other are one line.
+ClearArgs clear_args(const ps_embedding& e, const ps_matrix& m)
+{
+    const int size = dtype_size(e.dtype);
+    ClearArgs c{};
+    c.base = static_cast<char*>(m.data_dev);
+    c.size = size;
+    c.lines = e.n_groups * e.vocab;
+    c.per_matrix = e.vocab;
+    c.line_stride = m.row * size;
+    c.matrix_stride = m.matrix * size;
+    c.line_bytes = e.dim * size;
+    if (e.vocab == 1 || m.row == e.dim) {
+        c.lines = e.n_groups;
+        c.per_matrix = 1;
+        c.line_bytes *= e.vocab;
+        if (e.n_groups == 1 || m.matrix * size == c.line_bytes) {
+            c.lines = 1;
+            c.line_bytes *= e.n_groups;
+        }
+    }
+    c.blocks_per_line = (int32_t)up(c.line_bytes, CLEAR_BYTES);
+    c.lines_per_block = c.blocks_per_line > 1 ? 1 : (int32_t)(CLEAR_BYTES / c.line_bytes);
+    c.blocks = (uint32_t)(c.lines_per_block > 1 ? up(c.lines, c.lines_per_block) : c.lines * c.blocks_per_line);
+    return c;
 }
 
 template <class F>
@@ -568,12 +637,20 @@ extern "C" ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens
     a.vocab = e->vocab;
     a.rows = (int32_t)e->rows;
     a.dim = (int32_t)e->dim;
-    a.pieces = (int32_t)up(e->dim * dtype_size(e->dtype), 16);
+    const int wide = 16 / dtype_size(e->dtype);
+    a.pieces = (int32_t)(e->dim < wide ? e->dim : up(e->dim, wide));
+    // rows of 32 KB together, or fewer where that leaves less than four blocks to a compute unit
+    a.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2048 / a.pieces), e->rows / (4 * COMPUTE_UNITS)));
     a.scale = (float)e->scale;
     a.groups = groups_of(*e);
-    const int64_t blocks = std::min<int64_t>(up(e->rows * a.pieces, 256 * LOOKUP_AHEAD), 1 << 20);
+    const int64_t blocks = std::min<int64_t>(up(e->rows, a.each), 1 << 22);
     with_types(e->dtype, tokens->bytes, [&](auto t, auto token) {
-        hipLaunchKernelGGL((lookup_kernel<decltype(t), decltype(token)>), dim3((uint32_t)blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+        using T = decltype(t);
+        const dim3 grid((uint32_t)blocks), block(256);
+        if (e->dim < wide)
+            hipLaunchKernelGGL((lookup_kernel<T, decltype(token), 1>), grid, block, 0, static_cast<hipStream_t>(hip_stream), a);
+        else
+            hipLaunchKernelGGL((lookup_kernel<T, decltype(token), 16 / sizeof(T)>), grid, block, 0, static_cast<hipStream_t>(hip_stream), a);
     });
     return tokens_launched(call);
 }
@@ -606,49 +683,60 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
     const uint32_t none = (uint32_t)(e->n_groups * e->vocab);
     const uint32_t* keys = nullptr;
     const uint32_t* order = nullptr;
-    if (e->rows) {
-        SortArgs a{tokens->data_dev, tokens->stride, e->vocab, (int32_t)e->rows, none, groups_of(*e)};
-        auto word = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(base + at); };
-        with_types(PS_F32, tokens->bytes, [&](auto, auto token) {
-            using TOKEN = decltype(token);
-            if (space.tiles == 1) {
-                hipLaunchKernelGGL(sort_one_kernel<TOKEN>, dim3(1), dim3(TILE_WAVES * 64), 0, s, a, space.passes, word(space.keys[0]), word(space.order[0]));
-                keys = word(space.keys[0]);
-                order = word(space.order[0]);
-                return;
-            }
-            for (int pass = 0; pass < space.passes; ++pass) {
-                uint32_t *keys_to = word(space.keys[pass & 1]), *order_to = word(space.order[pass & 1]);
-                const dim3 grid((uint32_t)space.tiles), block(TILE_WAVES * 64);
-                hipLaunchKernelGGL(sort_count_kernel<TOKEN>, grid, block, 0, s, a, 8 * pass, keys, word(space.counts), space.tiles);
-                hipLaunchKernelGGL(sort_scan_kernel, dim3(DIGITS), dim3(256), 0, s, word(space.counts), space.tiles);
-                hipLaunchKernelGGL(sort_place_kernel<TOKEN>, grid, block, 0, s, a, 8 * pass, keys, order, word(space.counts), space.tiles, keys_to, order_to);
-                keys = keys_to;
-                order = order_to;
-            }
-        });
-    }
-    SumArgs a{};
-    a.dy = dy ? dy->data_dev : nullptr;
-    a.dy_row = dy ? dy->row : 0;
-    a.dtable = dtable->data_dev;
-    a.table_row = dtable->row;
-    a.table_matrix = dtable->matrix;
-    a.keys = keys;
-    a.order = order;
-    a.partial = reinterpret_cast<float*>(base + space.partial);
-    a.vocab = e->vocab;
-    a.rows = (int32_t)e->rows;
-    a.dim = (int32_t)e->dim;
-    a.chunks = space.chunks;
-    a.col_blocks = (int32_t)up(e->dim * dtype_size(e->dtype), 1024);
-    a.none = none;
-    a.scale = (float)e->scale;
-    const uint32_t sums = (uint32_t)up((int64_t)a.chunks * a.col_blocks, 4), clear = (uint32_t)up(none, 256);  // (below 2^24: dy fits the memory)
+    SortArgs a{tokens ? tokens->data_dev : nullptr, tokens ? tokens->stride : 0, e->vocab, (int32_t)e->rows, none, groups_of(*e)};
+    const ClearArgs clear = clear_args(*e, *dtable);
+    auto word = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(base + at); };
+    with_types(PS_F32, tokens && tokens->data_dev ? tokens->bytes : 4, [&](auto, auto token) {
+        using TOKEN = decltype(token);
+        if (!space.tiles) {
+            const uint32_t ranks = (uint32_t)(up(e->rows, RANK_ROWS) * space.parts);
+            hipLaunchKernelGGL(rank_and_clear_kernel<TOKEN>, dim3(ranks + clear.blocks), dim3(RANK_ROWS), 0, s, a, ranks, space.parts, word(space.keys[1]),
+                               reinterpret_cast<uint16_t*>(base + space.counts), clear);
+            keys = word(space.keys[0]);
+            order = word(space.order[0]);
+            if (e->rows)
+                hipLaunchKernelGGL(rank_place_kernel, dim3((uint32_t)up(e->rows, 64)), dim3(64), 0, s, (int)e->rows, space.parts, word(space.keys[1]),
+                                   reinterpret_cast<const uint16_t*>(base + space.counts), word(space.keys[0]), word(space.order[0]));
+            return;
+        }
+        for (int pass = 0; pass < space.passes; ++pass) {
+            uint32_t *keys_to = word(space.keys[pass & 1]), *order_to = word(space.order[pass & 1]);
+            hipLaunchKernelGGL(sort_count_kernel<TOKEN>, dim3(space.tiles + (pass ? 0 : clear.blocks)), dim3(DIGITS), 0, s, a, 8 * pass, keys, word(space.counts), space.tiles, clear);
+            hipLaunchKernelGGL(sort_scan_kernel, dim3(DIGITS), dim3(DIGITS), 0, s, word(space.counts), space.tiles);
+            hipLaunchKernelGGL(sort_place_kernel<TOKEN>, dim3((uint32_t)space.tiles), dim3(DIGITS), 0, s, a, 8 * pass, keys, order, word(space.counts), space.tiles, keys_to, order_to);
+            keys = keys_to;
+            order = order_to;
+        }
+    });
+    if (!e->rows) return tokens_launched(call);
+    SumArgs b{};
+    b.dy = dy->data_dev;
+    b.dy_row = dy->row;
+    b.dtable = dtable->data_dev;
+    b.table_row = dtable->row;
+    b.table_matrix = dtable->matrix;
+    b.keys = keys;
+    b.order = order;
+    b.partial = reinterpret_cast<float*>(base + space.partial);
+    b.vocab = e->vocab;
+    b.rows = (int32_t)e->rows;
+    b.dim = (int32_t)e->dim;
+    b.chunks = space.chunks;
+    b.col_blocks = (int32_t)up(e->dim, 64 * 16 / dtype_size(e->dtype));  // (shorter rows: one, of 64 columns)
+    b.none = none;
+    b.scale = (float)e->scale;
+    const int64_t waves = (int64_t)b.chunks * b.col_blocks;  // (below 2^24: dy fits the memory)
     with_types(e->dtype, 4, [&](auto t, auto) {
         using T = decltype(t);
-        if (sums) hipLaunchKernelGGL(sum_runs_kernel<T>, dim3(sums), dim3(256), 0, s, a);
-        hipLaunchKernelGGL(join_and_clear_kernel<T>, dim3(sums + clear), dim3(256), 0, s, a, sums);
+        auto sum = [&](auto sum_runs, auto join_runs) {
+            hipLaunchKernelGGL(sum_runs, dim3((uint32_t)up(waves, 4)), dim3(256), 0, s, b);
+            if (e->rows > PIECE) hipLaunchKernelGGL(join_runs, dim3((uint32_t)std::min<int64_t>(waves, 1 << 20)), dim3(256), 0, s, b);
+        };
+        constexpr int E = 16 / sizeof(T);
+        if (e->dim < E)
+            sum(sum_runs_kernel<T, 1>, join_runs_kernel<T, 1>);
+        else
+            sum(sum_runs_kernel<T, E>, join_runs_kernel<T, E>);
     });
     return tokens_launched(call);
 }

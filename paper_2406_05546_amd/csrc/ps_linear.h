@@ -91,21 +91,36 @@ __device__ __forceinline__ int count_tiles(const Groups& gs, int size, int bound
     return min(total, bound);
 }
 
-// The group that has row r, or -1: the last one that begins at r or before, if it ends behind it.
-__device__ __forceinline__ int group_of_row(const Groups& gs, int64_t r)
+// The group that has row `first` + lane, for a whole wavefront: the last one that begins there or before, if it ends behind it; -1 for
+// rows of none.  One look at the offsets for every power of 64 groups, and one for 64 that begin among the rows: next to kernels that
+// fill the memory's queues, each one takes microseconds.
+__device__ __forceinline__ int groups_of_rows(const Groups& gs, int64_t first)
 {
-    if (!gs.offsets) return 0;
-    int lo = 0, hi = gs.n;  // groups before lo begin at r or before, those from hi on behind it
+    const int lane = threadIdx.x & 63;
+    const int64_t r = first + lane;
+    if (!gs.offsets) return r < gs.rows ? 0 : -1;
+    auto begins = [&](int g) __attribute__((always_inline)) { return min(max(gs.offsets[g], 0), gs.rows); };
+    const int end_of_all = begins(gs.n);
+    int lo = 0, hi = gs.n;  // groups before lo begin at `first` or before, those from hi on behind it
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (min(max(gs.offsets[mid], 0), gs.rows) <= r)
-            lo = mid + 1;
-        else
-            hi = mid;
+        const int step = (hi - lo + 63) >> 6, g = lo + lane * step;
+        const int before = __popcll(__ballot(g < hi && begins(min(g, gs.n)) <= first));
+        if (before == 0) break;
+        hi = min(hi, lo + before * step);
+        lo = lo + (before - 1) * step + 1;
     }
-    if (lo == 0) return -1;
-    const GroupRows rows = group_rows(gs, lo - 1);
-    return r >= rows.begin && r < rows.end ? lo - 1 : -1;
+    int group = lo - 1;
+    for (int g0 = lo; g0 < gs.n; g0 += 64) {
+        const int begin = g0 + lane < gs.n ? begins(g0 + lane) : 0x7fffffff;
+        unsigned long long among = __ballot(begin <= first + 63);
+        // ascending, so those that begin among the rows are the first lanes' (if the offsets are none, any of them may be)
+        for (; among; among &= among - 1) {
+            const int i = __builtin_ctzll(among);
+            if (__builtin_amdgcn_readlane(begin, i) <= r) group = g0 + i;
+        }
+        if (__builtin_amdgcn_readlane(begin, 63) > first + 63) break;
+    }
+    return group >= 0 && r < gs.rows && (group + 1 < gs.n || r < end_of_all) ? group : -1;
 }
 
 // The group and the first row of the `tile`-th piece of `size` rows when the groups are cut up one after the other; false

@@ -9,6 +9,7 @@
 #include "ps_tokens.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace ps {
 namespace {
@@ -103,8 +104,10 @@ struct ForwardArgs {
     const void *logits, *tokens;
     float *logp, *norm, *top_logp;
     int32_t* top_tokens;
+    float* part_sums;      // [row][part][3], where a row is cut into parts
+    uint64_t* part_lists;  // [row][part][top]
     int64_t row, token_stride, rows;
-    int32_t vocab, token_bytes, top;
+    int32_t vocab, token_bytes, top, parts, part_rounds;
     float scale;
 };
 
@@ -121,7 +124,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
 {
     const float m = fmaxf(a.m, b.m);
     auto part = [&](const Sums& x, float& s, float& u) __attribute__((always_inline)) {
-        const float d = x.m == m ? 0.f : fmaxf((x.m - m) * c, NEVER), f = exp2f(d);
+        const float d = x.m == m ? 0.f : fmaxf((x.m - m) * c, NEVER), f = __builtin_amdgcn_exp2f(d);
         s = x.s * f;
         u = (x.u + d * x.s) * f;
     };
@@ -130,52 +133,114 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
     part(b, s1, u1);
     return {m, s0 + s1, u0 + u1};
 }
+__device__ __forceinline__ Sums join_lanes(Sums x, float c)
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) x = join(x, Sums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.u, off, 64)}, c);
+    return x;
+}
 
-// WAVES wavefronts take a row, each 64 * VECTORS * 16 bytes at a time.  Bound by memory; behind it by the vector ALU: about ten
-// operations and an exponential for a value.
+// What a row's sums and its token give; one thread.
+template <class T>
+__device__ __forceinline__ void finish_row(const ForwardArgs& a, int64_t row, const Sums& x, int64_t token, float at_token)
+{
+    const bool none = x.m == negative_infinity() && x.s == 0.f;
+    const float log_s = logf(x.s);  // -infinity where there is none
+    a.norm[row * 3] = x.m;
+    a.norm[row * 3 + 1] = log_s;
+    a.norm[row * 3 + 2] = none ? 0.f : log_s - LN2 * (x.u / x.s);
+    if (a.logp) a.logp[row] = token < 0 || token >= a.vocab ? 0.f : none ? negative_infinity() : (at_token - x.m) * a.scale - log_s;
+}
+// The row's token and its logit, asked for before they are needed
+template <class T>
+__device__ __forceinline__ int64_t take_token(const ForwardArgs& a, int64_t row, float& at_token)
+{
+    int64_t t = -1;
+    if (a.logp) t = token_of_row(a.tokens, a.token_bytes, row * a.token_stride);
+    const T* z = static_cast<const T*>(a.logits) + row * a.row;
+    at_token = to_float(z[min(max(t, (int64_t)0), (int64_t)a.vocab - 1)]);
+    return t;
+}
+
+// Merges lists of `top` keys each, in order, 0 behind the last: `threads` threads, of which this is number t, write the best `top` to
+// `best` (in LDS, 0 behind the last).  A key's place is how many are before it, in its own list and, by halving, in the others.
+__device__ __forceinline__ void merge(const uint64_t* lists, int stride, int n_lists, int top, uint64_t* best, int t, int threads)
+{
+    for (int i = t; i < n_lists * top; i += threads) {
+        const int of = i / top, at = i % top;
+        const uint64_t key = lists[of * stride + at];
+        if (!key) continue;
+        int place = at;
+        for (int k = 0; k < n_lists; ++k) {
+            if (k == of) continue;
+            int n = 0;  // keys of list k that are above
+#pragma unroll
+            for (int half = 32; half; half >>= 1)
+                if (n + half <= top && lists[k * stride + n + half - 1] > key) n += half;
+            place += n;
+        }
+        if (place < top) best[place] = key;
+    }
+}
+__device__ __forceinline__ void write_best(const ForwardArgs& a, int64_t row, int place, uint64_t key, const Sums& x)
+{
+    a.top_logp[row * a.top + place] = key ? (value_of(key) - x.m) * a.scale - logf(x.s) : negative_infinity();
+    a.top_tokens[row * a.top + place] = key ? index_of(key) : -1;
+}
+
+// WAVES wavefronts take a row, or a part of one, in rounds of VECTORS times 16 bytes to a lane; the next round is asked for before the present
+// one is worked on.  Where rows are few, parts of them are blocks of their own, and join_parts_kernel finishes.  Bound by memory; behind it by
+// the vector ALU: about ten operations and an exponential for a value.
 constexpr int VECTORS = 4;
 
 template <class T, int WAVES, bool TOP>
-__global__ __launch_bounds__(WAVES * 64 < 256 ? 256 : WAVES * 64) void logprob_kernel(ForwardArgs a)
+__global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
 {
-    constexpr int E = 16 / sizeof(T), ROWS = WAVES < 4 ? 4 / WAVES : 1;  // rows of a block
+    constexpr int E = 16 / sizeof(T), ROWS = 4 / WAVES;  // rows of a block
     constexpr int EACH = 64 * VECTORS * E;
-    __shared__ uint64_t lists[TOP ? ROWS * WAVES * LIST : 1];
-    __shared__ Sums meet[ROWS * WAVES];
-    __shared__ int counts[ROWS * WAVES];
-    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), w = wave % WAVES;
+    __shared__ uint64_t lists[TOP ? 4 * LIST : 1], best_of_row[TOP ? ROWS * PS_LOGPROB_MAX_TOP : 1];
+    __shared__ Sums meet[4];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), w = wave % WAVES, of = wave / WAVES;
     const float c = a.scale * LOG2E;
-    const int64_t step = (int64_t)gridDim.x * ROWS;
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += step) {
-        const int64_t row = row0 + wave / WAVES;
-        const bool there = row < a.rows;
-        const T* const z = static_cast<const T*>(a.logits) + (there ? row : 0) * a.row;
+    const int64_t total = a.rows * a.parts;
+    for (int64_t block = (int64_t)blockIdx.x * ROWS; block < total; block += (int64_t)gridDim.x * ROWS) {
+        const bool there = block + of < total;
+        const int64_t item = there ? block + of : 0, row = item / a.parts;
+        const int part = (int)(item - row * a.parts);
+        const T* const z = static_cast<const T*>(a.logits) + row * a.row;
+        float at_token = 0.f;
+        const int64_t token = a.parts == 1 ? take_token<T>(a, row, at_token) : -1;
+        const int64_t begin = (int64_t)part * a.part_rounds * (WAVES * EACH);
+        const int64_t end = there ? min(begin + (int64_t)a.part_rounds * (WAVES * EACH), (int64_t)a.vocab) : 0;
         Sums sums{negative_infinity(), 0.f, 0.f};
         Best best{lists + (TOP ? wave * LIST : 0), 0, a.top, 0};
-        for (int64_t base = (int64_t)w * EACH; there && base < a.vocab; base += WAVES * EACH) {
-            T raw[VECTORS][E];
+        // Vector j of a lane: columns base + j * 64 E + lane E on.  WHOLE: all of them are there; else a vector that would go past the end ends
+        // with it, and what it has in common with others, `again` values, is left out; so nothing is read in a branch, where the
+        // compiler would wait for it.
+        auto take = [&](int64_t base, T (&raw)[VECTORS][E], bool whole) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < VECTORS; ++j) {
                 const int64_t at = base + j * 64 * E + lane * E;
-                if (at + E <= a.vocab) {
-                    __builtin_memcpy(raw[j], z + at, 16);
-                } else {
-                    const T* p = z + at;
-                    asm volatile("" : "+v"(p));
-#pragma unroll
-                    for (int e = 0; e < E; ++e) raw[j][e] = at + e < a.vocab ? p[e] : from_float<T>(negative_infinity());
-                }
+                __builtin_memcpy(raw[j], z + (whole ? at : min(at, end - E)), 16);
             }
+        };
+        auto round = [&](int64_t base, const T (&raw)[VECTORS][E], auto whole) __attribute__((always_inline)) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            auto value = [&](int j, int e) __attribute__((always_inline)) {
+                if constexpr (WHOLE) return to_float(raw[j][e]);
+                const int64_t at = base + j * 64 * E + lane * E;
+                return (int64_t)e < at - min(at, end - E) ? negative_infinity() : to_float(raw[j][e]);
+            };
             float high = negative_infinity(), highs[VECTORS];
 #pragma unroll
             for (int j = 0; j < VECTORS; ++j) {
                 highs[j] = negative_infinity();
 #pragma unroll
-                for (int e = 0; e < E; ++e) highs[j] = fmaxf(highs[j], to_float(raw[j][e]));
+                for (int e = 0; e < E; ++e) highs[j] = fmaxf(highs[j], value(j, e));
                 high = fmaxf(high, highs[j]);
             }
             if (high > sums.m) {
-                const float d = sums.m == negative_infinity() ? 0.f : fmaxf((sums.m - high) * c, NEVER), f = exp2f(d);
+                const float d = fmaxf((sums.m - high) * c, NEVER), f = __builtin_amdgcn_exp2f(d);  // (nothing yet: 0)
                 sums.u = (sums.u + d * sums.s) * f;
                 sums.s *= f;
                 sums.m = high;
@@ -185,7 +250,7 @@ __global__ __launch_bounds__(WAVES * 64 < 256 ? 256 : WAVES * 64) void logprob_k
             for (int j = 0; j < VECTORS; ++j)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float t = (to_float(raw[j][e]) - m) * c, p = __builtin_amdgcn_exp2f(t);
+                    const float t = (value(j, e) - m) * c, p = __builtin_amdgcn_exp2f(t);
                     sums.s += p;
                     sums.u = fmaf(p, fmaxf(t, NEVER), sums.u);
                 }
@@ -200,72 +265,114 @@ __global__ __launch_bounds__(WAVES * 64 < 256 ? 256 : WAVES * 64) void logprob_k
 #pragma unroll
                     for (int j = 0; j < VECTORS; ++j) {
                         if (!__ballot(highs[j] >= from && highs[j] > negative_infinity())) continue;
+                        const int64_t at = base + j * 64 * E + lane * E;
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
-                            const float v = to_float(raw[j][e]);
-                            best.add(v >= from && v > negative_infinity(), v, (int)(base + j * 64 * E + lane * E + e));
+                            const float v = value(j, e);
+                            best.add(v >= from && v > negative_infinity(), v, (int)(WHOLE ? at : min(at, end - E)) + e);
                         }
                     }
                     if (best.count >= a.top) best.cut();
                 }
             }
-        }
+        };
+        if (a.vocab >= E) {
+            int64_t base = begin + w * EACH;
+            T now[VECTORS][E], then[VECTORS][E];
+            if (base + EACH <= end) take(base, now, true);
+            for (; base + EACH <= end; base += WAVES * EACH) {
+                if (base + (WAVES + 1) * EACH <= end) take(base + WAVES * EACH, then, true);
+                round(base, now, std::true_type{});
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) sums = join(sums, Sums{__shfl_xor(sums.m, off, 64), __shfl_xor(sums.s, off, 64), __shfl_xor(sums.u, off, 64)}, c);
+                for (int j = 0; j < VECTORS; ++j)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) now[j][e] = then[j][e];
+            }
+            if (base < end) {
+                take(base, now, false);
+                round(base, now, std::false_type{});
+            }
+        } else if (there && w == 0) {
+            // a row shorter than 16 bytes, in the last elements of a vector as it would be there
+            T raw[VECTORS][E];
+#pragma unroll
+            for (int j = 0; j < VECTORS; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e) raw[j][e] = from_float<T>(negative_infinity());
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int i = e - (E - a.vocab);
+                const T v = z[max(i, 0)];
+                if (lane == 0 && i >= 0) raw[0][e] = v;
+            }
+            round(a.vocab - E, raw, std::true_type{});
+        }
+        sums = join_lanes(sums, c);
         if constexpr (TOP) {
             best.cut();  // in order, also where there are fewer
-            if (lane == 0) counts[wave] = best.count;
+            if (lane < a.top && lane >= best.count) best.list[lane] = 0;
         }
-        if (WAVES > 1) {
+        if constexpr (WAVES > 1) {
             if (lane == 0) meet[wave] = sums;
+            if (TOP && threadIdx.x < (uint32_t)a.top) best_of_row[threadIdx.x] = 0;
             __syncthreads();
             sums = meet[0];
+#pragma unroll
             for (int k = 1; k < WAVES; ++k) sums = join(sums, meet[k], c);
+            if constexpr (TOP) {
+                merge(lists, LIST, WAVES, a.top, best_of_row, threadIdx.x, 256);
+                __syncthreads();
+            }
         } else {
             __builtin_amdgcn_wave_barrier();
         }
-        if (there) {
-            const bool none = sums.m == negative_infinity() && sums.s == 0.f;
-            const float log_s = logf(sums.s);  // -infinity where there is none
-            if (w == 0 && lane == 0) {
-                a.norm[row * 3] = sums.m;
-                a.norm[row * 3 + 1] = log_s;
-                a.norm[row * 3 + 2] = none ? 0.f : log_s - LN2 * (sums.u / sums.s);
-                if (a.logp) {
-                    const int64_t t = token_of_row(a.tokens, a.token_bytes, row * a.token_stride);
-                    float v = 0.f;
-                    if (t >= 0 && t < a.vocab) v = none ? negative_infinity() : (to_float(z[t]) - sums.m) * a.scale - log_s;
-                    a.logp[row] = v;
+        if (there && w == 0) {
+            const uint64_t* const kept = WAVES > 1 ? best_of_row : best.list;
+            if (a.parts > 1) {
+                if (lane == 0) {
+                    a.part_sums[item * 3] = sums.m;
+                    a.part_sums[item * 3 + 1] = sums.s;
+                    a.part_sums[item * 3 + 2] = sums.u;
                 }
-            }
-            if constexpr (TOP) {
-                // the lists of the row's wavefronts, each in order: an entry's place is how many are before it
-                const int first = wave / WAVES * WAVES;
-                int total = 0;
-                for (int k = 0; k < WAVES; ++k) total += counts[first + k];
-                for (int i = w * 64 + lane; i < WAVES * a.top; i += WAVES * 64) {
-                    const int of = i / a.top, at = i % a.top;
-                    if (at >= counts[first + of]) continue;
-                    const uint64_t key = lists[(first + of) * LIST + at];
-                    int place = at;
-                    for (int k = 0; k < WAVES; ++k) {
-                        if (k == of) continue;
-                        const int n = counts[first + k];
-                        for (int x = 0; x < n; ++x) place += lists[(first + k) * LIST + x] > key;
-                    }
-                    if (place < a.top) {
-                        a.top_logp[row * a.top + place] = (value_of(key) - sums.m) * a.scale - log_s;
-                        a.top_tokens[row * a.top + place] = index_of(key);
-                    }
-                }
-                for (int i = total + w * 64 + lane; i < a.top; i += WAVES * 64) {
-                    a.top_logp[row * a.top + i] = negative_infinity();
-                    a.top_tokens[row * a.top + i] = -1;
-                }
+                if (TOP && lane < a.top) a.part_lists[item * a.top + lane] = kept[lane];
+            } else {
+                if (lane == 0) finish_row<T>(a, row, sums, token, at_token);
+                if (TOP && lane < a.top) write_best(a, row, lane, kept[lane], sums);
             }
         }
         if (WAVES > 1) __syncthreads();  // what met in LDS is written again
     }
+}
+
+// Finishes rows that were cut into parts: a block to a row.
+constexpr int MOST_PARTS = 64;
+
+template <class T, bool TOP>
+__global__ __launch_bounds__(256) void join_parts_kernel(ForwardArgs a)
+{
+    __shared__ uint64_t lists[TOP ? MOST_PARTS * PS_LOGPROB_MAX_TOP : 1], best[TOP ? PS_LOGPROB_MAX_TOP : 1];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    const float c = a.scale * LOG2E;
+    float at_token;
+    const int64_t token = take_token<T>(a, row, at_token);
+    if constexpr (TOP) {
+        for (int i = threadIdx.x; i < a.parts * a.top; i += 256) lists[i] = a.part_lists[row * a.parts * a.top + i];
+        if (threadIdx.x < (uint32_t)a.top) best[threadIdx.x] = 0;
+    }
+    Sums x{negative_infinity(), 0.f, 0.f};
+    if (lane < a.parts) {
+        const float* p = a.part_sums + (row * a.parts + lane) * 3;
+        x = Sums{p[0], p[1], p[2]};
+    }
+    x = join_lanes(x, c);
+    if constexpr (TOP) {
+        __syncthreads();
+        merge(lists, a.top, a.parts, a.top, best, threadIdx.x, 256);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) finish_row<T>(a, row, x, token, at_token);
+    if (TOP && threadIdx.x < (uint32_t)a.top) write_best(a, row, threadIdx.x, best[threadIdx.x], x);
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
@@ -287,40 +394,25 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
     const int64_t total = a.rows * a.per_row;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
         const int64_t row = b / a.per_row;
-        const int base = (int)(b - row * a.per_row) * EACH + threadIdx.x * E;
+        const int first = (int)(b - row * a.per_row) * EACH, base = first + threadIdx.x * E;
         const T* const z = static_cast<const T*>(a.logits) + row * a.row;
         T* const out = static_cast<T*>(a.dlogits) + row * a.out_row;
-        T raw[VECTORS][E];
-#pragma unroll
-        for (int j = 0; j < VECTORS; ++j) {
-            const int64_t at = base + (int64_t)j * 256 * E;
-            if (at + E <= a.vocab) {
-                __builtin_memcpy(raw[j], z + at, 16);
-            } else {
-                const T* p = z + at;
-                asm volatile("" : "+v"(p));
-#pragma unroll
-                for (int e = 0; e < E; ++e) raw[j][e] = at + e < a.vocab ? p[e] : T{};
-            }
-        }
-        const float m = a.norm[row * 3], c = a.scale * LOG2E, log2_s = a.norm[row * 3 + 1] * LOG2E;
+        const float m = a.norm[row * 3], c = a.scale * LOG2E, log2_s = a.norm[row * 3 + 1] * LOG2E, entropy = a.norm[row * 3 + 2];
         int64_t token = -1;
         float gl = 0.f;
         if (a.dlogp) {
             token = token_of_row(a.tokens, a.token_bytes, row * a.token_stride);
-            if (token >= 0 && token < a.vocab) gl = a.dlogp[row * a.dlogp_stride];
+            gl = a.dlogp[row * a.dlogp_stride];
+            if (token < 0 || token >= a.vocab) gl = 0.f;
         }
         const float gh = a.dentropy ? a.dentropy[row * a.dentropy_stride] : 0.f;
-        const float A = -a.scale * (gl + gh * a.norm[row * 3 + 2]), B = -a.scale * gh * LN2;
+        const float A = -a.scale * (gl + gh * entropy), B = -a.scale * gh * LN2;
         const bool none = m == negative_infinity() && log2_s == negative_infinity();
-#pragma unroll
-        for (int j = 0; j < VECTORS; ++j) {
-            const int64_t at = base + (int64_t)j * 256 * E;
-            if (at >= a.vocab) continue;
+        auto give = [&](int64_t at, int n, const T (&raw)[E]) __attribute__((always_inline)) {
             float d[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float t = (to_float(raw[j][e]) - m) * c - log2_s;
+                const float t = (to_float(raw[e]) - m) * c - log2_s;
                 d[e] = __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, NEVER), A);
             }
             if (token >= at && token < at + E) {
@@ -332,7 +424,28 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
 #pragma unroll
                 for (int e = 0; e < E; ++e) d[e] = 0.f;
             }
-            store_columns(out + at, (int)min((int64_t)E, a.vocab - at), d);
+            store_columns(out + at, n, d);
+        };
+        if (first + EACH <= a.vocab) {
+            // without a branch between them, at which the compiler would wait
+            T raw[VECTORS][E];
+#pragma unroll
+            for (int j = 0; j < VECTORS; ++j) __builtin_memcpy(raw[j], z + base + j * 256 * E, 16);
+#pragma unroll
+            for (int j = 0; j < VECTORS; ++j) give(base + j * 256 * E, E, raw[j]);
+        } else {
+            for (int at = base; at < a.vocab; at += 256 * E) {
+                const int n = min(E, a.vocab - at);
+                T raw[E] = {};
+                if (n == E) {
+                    __builtin_memcpy(raw, z + at, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e < n) raw[e] = z[at + e];
+                }
+                give(at, n, raw);
+            }
         }
     }
 }
@@ -356,18 +469,31 @@ ps_status check_numbers(const char* call, const char* name, const void* p, int64
     return PS_OK;
 }
 
+// Parts of a row, so many rounds of four wavefronts each: as many as make eight blocks for a compute unit of all rows, one where
+// there are as many rows.
+struct Cut {
+    int parts, rounds;
+};
+Cut cut_rows(const ps_logprob& l)
+{
+    const int64_t round = 4 * 64 * VECTORS * 16 / dtype_size(l.dtype), rounds = (l.vocab + round - 1) / round;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, MOST_PARTS), l.rows ? 8 * COMPUTE_UNITS / l.rows : 1));
+    const int64_t each = (rounds + parts - 1) / parts;
+    return {(int)((rounds + each - 1) / each), (int)each};
+}
+uint64_t sums_bytes(const ps_logprob& l, const Cut& c) { return ((uint64_t)l.rows * c.parts * 12 + 255) / 256 * 256; }
+
 template <class T, bool TOP>
 void start_forward(const ForwardArgs& a, hipStream_t s)
 {
-    // a wavefront to a row of a few rounds, sixteen where rows are too few to fill the chip with four
-    constexpr int ROUND = 64 * VECTORS * 16 / (int)sizeof(T);
+    constexpr int ROUND = 64 * VECTORS * 16 / (int)sizeof(T);  // of a wavefront
     const int64_t most = 1 << 20;
-    if (a.vocab <= ROUND)
+    if (a.vocab <= ROUND) {
         hipLaunchKernelGGL((logprob_kernel<T, 1, TOP>), dim3((uint32_t)std::min((a.rows + 3) / 4, most)), dim3(256), 0, s, a);
-    else if (a.rows > 2 * COMPUTE_UNITS || a.vocab <= 4 * ROUND)
-        hipLaunchKernelGGL((logprob_kernel<T, 4, TOP>), dim3((uint32_t)std::min(a.rows, most)), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((logprob_kernel<T, 16, TOP>), dim3((uint32_t)std::min(a.rows, most)), dim3(1024), 0, s, a);
+        return;
+    }
+    hipLaunchKernelGGL((logprob_kernel<T, 4, TOP>), dim3((uint32_t)std::min(a.rows * a.parts, most)), dim3(256), 0, s, a);
+    if (a.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, TOP>), dim3((uint32_t)a.rows), dim3(256), 0, s, a);
 }
 
 template <class F>
@@ -384,8 +510,19 @@ void with_type(int dtype, F f)
 }  // namespace
 }  // namespace ps
 
+extern "C" ps_status ps_logprob_workspace_bytes(const ps_logprob* l, uint64_t* bytes_out)
+{
+    using namespace ps;
+    const ps_status st = check_logprob("ps_logprob_workspace_bytes", l);
+    if (st != PS_OK) return st;
+    if (!bytes_out) return dense_fail(PS_EINVAL, "ps_logprob_workspace_bytes: no place for the result");
+    const Cut cut = cut_rows(*l);
+    *bytes_out = cut.parts > 1 ? sums_bytes(*l, cut) + (uint64_t)l->rows * cut.parts * l->top * 8 : 0;
+    return PS_OK;
+}
+
 extern "C" ps_status ps_logprob_forward(const ps_logprob* l, const ps_tokens* tokens, const ps_matrix* logits, float* logp, float* norm, float* top_logp,
-                                        int32_t* top_tokens, void* hip_stream)
+                                        int32_t* top_tokens, void* workspace, uint64_t workspace_bytes, void* hip_stream)
 {
     using namespace ps;
     static const char call[] = "ps_logprob_forward";
@@ -398,7 +535,16 @@ extern "C" ps_status ps_logprob_forward(const ps_logprob* l, const ps_tokens* to
     for (const void* p : {(const void*)logp, (const void*)norm, (const void*)top_logp, (const void*)top_tokens})
         if ((st = check_numbers(call, "result", p, 0)) != PS_OK) return st;
     if (!l->rows) return PS_OK;
+    const Cut cut = cut_rows(*l);
+    uint64_t need = 0;
+    if ((st = ps_logprob_workspace_bytes(l, &need)) != PS_OK) return st;
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
+    if (workspace_bytes < need) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
     ForwardArgs a{};
+    a.parts = cut.parts;
+    a.part_rounds = cut.rounds;
+    a.part_sums = static_cast<float*>(workspace);
+    a.part_lists = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + sums_bytes(*l, cut));
     a.logits = logits->data_dev;
     a.row = logits->row;
     if (logp) {

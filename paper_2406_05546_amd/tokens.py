@@ -18,7 +18,7 @@ from .dense import _dtype, _ints, _matrix, _refuse
 LOGPROB_MAX_TOP = 32
 MAX_VOCAB = 1 << 22
 
-EXPORTS = ["ps_embedding_forward", "ps_embedding_workspace_bytes", "ps_embedding_backward", "ps_logprob_forward", "ps_logprob_backward"]
+EXPORTS = ["ps_embedding_forward", "ps_embedding_workspace_bytes", "ps_embedding_backward", "ps_logprob_workspace_bytes", "ps_logprob_forward", "ps_logprob_backward"]
 
 
 class ps_tokens(ctypes.Structure):
@@ -50,7 +50,8 @@ def _library() -> ctypes.CDLL:
                 "ps_embedding_forward": 5 * [vp],
                 "ps_embedding_workspace_bytes": 2 * [vp],
                 "ps_embedding_backward": 5 * [vp] + [u64, vp],
-                "ps_logprob_forward": 8 * [vp],
+                "ps_logprob_workspace_bytes": 2 * [vp],
+                "ps_logprob_forward": 8 * [vp] + [u64, vp],
                 "ps_logprob_backward": 8 * [vp]}.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, ctypes.c_int
@@ -99,6 +100,16 @@ def _call(call: str, name: str, device, *args) -> None:
     st = getattr(_library(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != PS_OK:
         raise PsError(call, st, (_library().ps_dense_last_error() or b"").decode())
+
+
+def _workspace(call: str, name: str, device):
+    """A workspace for what the arguments describe (None if none is needed), and its size."""
+    a = _arguments
+    st = getattr(_library(), name)(a.at, a.at_need)
+    if st != PS_OK:
+        raise PsError(call, st, (_library().ps_dense_last_error() or b"").decode())
+    need = a.need.value
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None, need
 
 
 def _on_gpu(call: str, name: str, t) -> None:
@@ -163,11 +174,7 @@ def _embedding_backward(dy, tokens, offsets, vocab, scale, dtable):
     a = _arguments
     _EMBEDDING.pack_into(a.memory, 0, dtype, groups, 1, rows, vocab, dim, at_offsets, 0, scale, *given,
                          *_matrix(call, "dy", dy, device, dy.dtype, (rows, dim)), *_matrix(call, "dtable", dtable, device, dy.dtype, shape, offsets is not None))
-    st = _library().ps_embedding_workspace_bytes(a.at, a.at_need)
-    if st != PS_OK:
-        raise PsError(call, st, (_library().ps_dense_last_error() or b"").decode())
-    need = a.need.value
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    ws, need = _workspace(call, "ps_embedding_workspace_bytes", device)
     _call(call, call, device, *a.embedding, None if ws is None else ws.data_ptr(), need)
     return dtable
 
@@ -221,8 +228,9 @@ def ps_logprob_forward(logits, tokens=None, scale: float = 1.0, top: int = 0) ->
     a = _arguments
     _LOGPROB.pack_into(a.memory, 0, dtype, top, rows, vocab, scale, *given, *_matrix(call, "logits", logits, device, logits.dtype, (rows, vocab)), *7 * (0,))
     at, at_tokens, at_logits = a.logprob[:3]
+    ws, need = _workspace(call, "ps_logprob_workspace_bytes", device)
     _call(call, call, device, at, at_tokens, at_logits, None if logp is None else logp.data_ptr(), norm.data_ptr(), top_logp.data_ptr() if top else None,
-          top_tokens.data_ptr() if top else None)
+          top_tokens.data_ptr() if top else None, None if ws is None else ws.data_ptr(), need)
     return LogProb(logp, norm, top_logp, top_tokens)
 
 

@@ -95,9 +95,9 @@ def test_workspace_of_a_gradient():
         assert lib().ps_embedding_workspace_bytes(ctypes.byref(embedding(**kw)), ctypes.byref(n)) == ps.PS_OK
         return n.value
     assert need(rows=0) == 0
-    # keys and order of 8 rows in 256 bytes each, two partial rows of 16 floats
-    assert need() == 256 + 256 + 256
-    assert need(rows=8193) > 4 * 4 * 8193  # two of each
+    # keys and order of 8 rows, twice, and counts in 256 bytes each, two partial rows of 16 floats
+    assert need() == 6 * 256
+    assert need(rows=100000) > 4 * 4 * 100000
     e = embedding()
     assert gradient(e, size=need() - 1) == ps.PS_ENOMEM
     assert gradient(e, ws=None) == ps.PS_EINVAL and gradient(e, ws=SOMEWHERE + 8) == ps.PS_EINVAL
@@ -118,10 +118,10 @@ def logprob(**kw):
     return tokens.ps_logprob(**d)
 
 
-def score(l, t=None, logits=None, logp=SOMEWHERE, norm=SOMEWHERE, top_logp=SOMEWHERE, top_tokens=SOMEWHERE):
+def score(l, t=None, logits=None, logp=SOMEWHERE, norm=SOMEWHERE, top_logp=SOMEWHERE, top_tokens=SOMEWHERE, ws=SOMEWHERE, size=HUGE):
     t = t or tokens.ps_tokens(SOMEWHERE, 1, 4)
     logits = logits or dense.ps_matrix(SOMEWHERE, 100, 0)
-    return lib().ps_logprob_forward(ctypes.byref(l), ctypes.byref(t), ctypes.byref(logits), logp, norm, top_logp, top_tokens, None)
+    return lib().ps_logprob_forward(ctypes.byref(l), ctypes.byref(t), ctypes.byref(logits), logp, norm, top_logp, top_tokens, ws, size, None)
 
 
 def score_gradient(l, t=None, logits=None, dlogits=None, norm=SOMEWHERE, dlogp=(SOMEWHERE, 1), dentropy=(SOMEWHERE, 0)):
@@ -146,7 +146,23 @@ def test_results_of_log_probabilities_that_are_refused():
     assert score_gradient(logprob(), norm=None) == ps.PS_EINVAL and score_gradient(logprob(), norm=SOMEWHERE + 1) == ps.PS_EINVAL
     for bad in ((SOMEWHERE + 2, 1), (SOMEWHERE, -1), (SOMEWHERE, (1 << 22) + 1)):
         assert score_gradient(logprob(), dlogp=bad) == ps.PS_EINVAL and score_gradient(logprob(), dentropy=bad) == ps.PS_EINVAL
-    assert lib().ps_logprob_forward(None, None, None, None, None, None, None, None) == ps.PS_EINVAL
+    assert lib().ps_logprob_forward(None, None, None, None, None, None, None, None, 0, None) == ps.PS_EINVAL
+
+
+def test_workspace_of_log_probabilities():
+    def need(**kw):
+        n = ctypes.c_uint64(0)
+        assert lib().ps_logprob_workspace_bytes(ctypes.byref(logprob(**kw)), ctypes.byref(n)) == ps.PS_OK
+        return n.value
+    assert need() == 0 and need(rows=0, vocab=1 << 20) == 0 and need(rows=1 << 14, vocab=1 << 20) == 0
+    # one long row: parts of 8192 logits, three sums and the alternatives of each
+    assert need(rows=1, vocab=65536) == 256 and need(rows=1, vocab=65536, top=5) == 256 + 8 * 5 * 8
+    long = logprob(rows=1, vocab=65536, top=5)
+    logits = dense.ps_matrix(SOMEWHERE, 65536, 0)
+    assert score(long, logits=logits, size=256 + 319) == ps.PS_ENOMEM
+    assert score(long, logits=logits, ws=None) == ps.PS_EINVAL and score(long, logits=logits, ws=SOMEWHERE + 8) == ps.PS_EINVAL
+    assert lib().ps_logprob_workspace_bytes(ctypes.byref(long), None) == ps.PS_EINVAL
+    assert lib().ps_logprob_workspace_bytes(ctypes.byref(logprob(top=33)), None) == ps.PS_EINVAL
 
 
 def test_tensors_that_are_refused():
