@@ -77,7 +77,7 @@ typedef struct {
  *                             among equals; behind the last token with a probability, -infinity and -1.
  * A logit of -infinity has probability 0.  A row of nothing else has -infinity, -infinity and 0 in norm, -infinity as log
  * probability, and no alternatives.  A row with a NaN or +infinity has NaN in what is a number (the largest excepted; NaN is no
- * alternative).  logp, top_logp and top_tokens may be NULL (the last two for top = 0 only), tokens without logp. */
+ * alternative).  The sums' order goes by the number of rows and by where a row begins in its 16 bytes.  logp, top_logp and top_tokens may be NULL (the last two for top = 0 only), tokens without logp. */
 PS_API ps_status ps_logprob_workspace_bytes(const ps_logprob* l, uint64_t* bytes_out);
 PS_API ps_status ps_logprob_forward(const ps_logprob* l, const ps_tokens* tokens, const ps_matrix* logits, float* logp_dev, float* norm_dev,
                                     float* top_logp_dev, int32_t* top_tokens_dev, void* workspace_dev, uint64_t workspace_bytes,

@@ -14,12 +14,13 @@
 namespace ps {
 namespace {
 
+constexpr int VECTORS = 4;  // of 16 bytes that a lane asks for together
 constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 constexpr float NEVER = -300.f;  // 2^NEVER is 0, and times NEVER too: what -infinity is taken to where t is multiplied
 
 __device__ __forceinline__ float negative_infinity() { return __uint_as_float(0xff800000u); }
 
-// ---- the best of a row ---------------------------------------------------------------------------------------------------
+// ---- keys of values ------------------------------------------------------------------------------------------------------
 
 // Values in the order of their keys: the larger value first, among equals the lower index.  0 is no key of a value.
 __device__ __forceinline__ uint32_t ordered(float v)
@@ -34,69 +35,6 @@ __device__ __forceinline__ float value_of(uint64_t key)
 }
 __device__ __forceinline__ uint64_t key_of(float v, int index) { return (uint64_t)ordered(v) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
-
-// A wavefront's candidates: a list in LDS, in no order until `cut` keeps the best `top` of it in theirs.
-constexpr int LIST = 256;
-
-struct Best {
-    uint64_t* list;
-    int count, top;
-    uint64_t least;  // what a candidate has to be above: 0, or the last of `top` that were kept
-
-    __device__ __forceinline__ void cut()
-    {
-        const int lane = threadIdx.x & 63;
-        __builtin_amdgcn_wave_barrier();
-        uint64_t mine[LIST / 64];
-        int rank[LIST / 64];
-#pragma unroll
-        for (int i = 0; i < LIST / 64; ++i) {
-            rank[i] = 0;
-            mine[i] = i * 64 + lane < count ? list[i * 64 + lane] : 0;
-        }
-#pragma unroll 4
-        for (int k = 0; k < count; ++k) {
-            const uint64_t other = list[k];
-#pragma unroll
-            for (int i = 0; i < LIST / 64; ++i) rank[i] += other > mine[i];
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < LIST / 64; ++i)
-            if (i * 64 + lane < count && rank[i] < top) list[rank[i]] = mine[i];
-        __builtin_amdgcn_wave_barrier();
-        if (count >= top) {
-            count = top;
-            least = list[top - 1];
-        }
-    }
-    // One value from each lane that has one
-    __device__ __forceinline__ void add(bool has, float v, int index)
-    {
-        uint64_t key = key_of(v, index);
-        has = has && key > least;
-        unsigned long long who = __ballot(has);
-        if (!who) return;
-        if (count + __popcll(who) > LIST) {
-            cut();
-            has = has && key > least;
-            who = __ballot(has);
-        }
-        if (has) list[count + __popcll(who & ((1ull << (threadIdx.x & 63)) - 1))] = key;
-        count += __popcll(who);
-    }
-};
-
-// The k-th largest of one value from each lane (of their `ordered` numbers).
-__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t o, int k)
-{
-    uint32_t least = 0;
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t more = least | 1u << b;
-        if (__popcll(__ballot(o >= more)) >= k) least = more;
-    }
-    return least;
-}
 
 // ---- forward -----------------------------------------------------------------------------------------------------------
 
@@ -162,83 +100,258 @@ __device__ __forceinline__ int64_t take_token(const ForwardArgs& a, int64_t row,
     return t;
 }
 
-// Merges lists of `top` keys each, in order, 0 behind the last: `threads` threads, of which this is number t, write the best `top` to
-// `best` (in LDS, 0 behind the last).  A key's place is how many are before it, in its own list and, by halving, in the others.
-__device__ __forceinline__ void merge(const uint64_t* lists, int stride, int n_lists, int top, uint64_t* best, int t, int threads)
-{
-    for (int i = t; i < n_lists * top; i += threads) {
-        const int of = i / top, at = i % top;
-        const uint64_t key = lists[of * stride + at];
-        if (!key) continue;
-        int place = at;
-        for (int k = 0; k < n_lists; ++k) {
-            if (k == of) continue;
-            int n = 0;  // keys of list k that are above
-#pragma unroll
-            for (int half = 32; half; half >>= 1)
-                if (n + half <= top && lists[k * stride + n + half - 1] > key) n += half;
-            place += n;
-        }
-        if (place < top) best[place] = key;
-    }
-}
 __device__ __forceinline__ void write_best(const ForwardArgs& a, int64_t row, int place, uint64_t key, const Sums& x)
 {
     a.top_logp[row * a.top + place] = key ? (value_of(key) - x.m) * a.scale - logf(x.s) : negative_infinity();
     a.top_tokens[row * a.top + place] = key ? index_of(key) : -1;
 }
 
-// WAVES wavefronts take a row, or a part of one, in rounds of VECTORS times 16 bytes to a lane; the next round is asked for before the present
+// A row (or part of one) as WAVES wavefronts see it: vectors of 16 bytes at multiples of 16 bytes in memory, of which the row begins `ahead`
+// values behind the first one's beginning.  Vector v has columns v * E - ahead on; those from `first` to `end` are the part's.
+template <class T, int WAVES>
+struct Range {
+    static constexpr int E = 16 / sizeof(T), THREADS = WAVES * 64;
+    const T* z;
+    int first, end, ahead, vocab;
+
+    __device__ __forceinline__ int column(int v) const { return v * E - ahead; }
+    // A vector that goes past an end of the row is read where the row's first or last one is, so that nothing is read in a branch, where the compiler
+    // would wait for it, or beside the row; what is no column of the vector, or the vector none of the range, becomes -infinity.  Gives the
+    // column of raw[0].
+    __device__ __forceinline__ int take(int v, T (&raw)[E]) const
+    {
+        const int at = column(v);
+        int from = at;
+        if (vocab >= E) {
+            from = min(max(at, 0), vocab - E);
+            __builtin_memcpy(raw, z + from, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) raw[e] = z[min(max(at + e, 0), vocab - 1)];
+        }
+        return from;
+    }
+    __device__ __forceinline__ void leave_out(int v, int from, T (&raw)[E]) const
+    {
+        // from + e is in the vector and the row
+        const int at = column(v), lo = max(at, 0) - from, hi = v < end ? min(at + E, vocab) - from : 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) raw[e] = e >= lo && e < hi ? raw[e] : from_float<T>(negative_infinity());
+    }
+};
+
+// The best `top` values of a range.  Each lane knows the largest of its own values; the top-th largest of these is a value that at least
+// `top` values reach, and only lanes whose largest reaches it can have one of the best: these lanes' vectors, few, are read again, and
+// what reaches it is listed.  Where more than LIST do (equal values), what is above it is listed, and then the first that equal it; where that is
+// too much as well (an order made for it), the top-th value itself is found bit by bit.  A value's place is the number of
+// listed keys above its own, so the order in which they were listed does not matter.
+constexpr int LIST = 256;
+template <int WAVES>
+struct Scratch {
+    uint64_t list[LIST + PS_LOGPROB_MAX_TOP], best[PS_LOGPROB_MAX_TOP];
+    float high[WAVES * 64];
+    uint16_t lanes[WAVES * 64];
+    int n_lanes, count, wave_count[WAVES];
+    uint32_t from;
+};
+
+template <int WAVES>
+__device__ __forceinline__ void meet_all()
+{
+    if constexpr (WAVES > 1)
+        __syncthreads();
+    else
+        __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront in order
+}
+
+// The k-th largest of the lanes' values, its lower 16 bits left out: reached by as many.  For a whole wavefront.
+template <int WAVES>
+__device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k)
+{
+    uint32_t o[WAVES], least = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) o[i] = ordered(high[i * 64 + (threadIdx.x & 63)]);
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t more = least | 1u << b;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) n += __popcll(__ballot(o[i] >= more));
+        if (n >= k) least = more;
+    }
+    return least;
+}
+
+template <class T, int WAVES>
+__device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<WAVES>& s, int top, int rounds_of_lane, float high)
+{
+    constexpr int E = Range<T, WAVES>::E, THREADS = Range<T, WAVES>::THREADS;
+    const int t = threadIdx.x % THREADS, wave = t / 64, lane = t & 63;
+    s.high[t] = high;
+    if (t == 0) s.n_lanes = s.count = 0;
+    if (t < top) s.best[t] = 0;
+    meet_all<WAVES>();
+    if (wave == 0) {
+        const uint32_t from = kth_of_lanes<WAVES>(s.high, top);
+        if (lane == 0) s.from = from;
+    }
+    meet_all<WAVES>();
+    uint32_t from = s.from;
+    if (high > negative_infinity() && ordered(high) >= from) s.lanes[atomicAdd(&s.n_lanes, 1)] = (uint16_t)t;
+    meet_all<WAVES>();
+    auto list = [&](bool has, float v, int index) __attribute__((always_inline)) {
+        if (!has) return;
+        const int place = atomicAdd(&s.count, 1);
+        if (place < LIST) s.list[place] = key_of(v, index);
+    };
+    // whether v is a value, and reaches or passes a number of `ordered`
+    auto reaches = [](float v, uint32_t o) __attribute__((always_inline)) { return v > negative_infinity() && ordered(v) >= o; };
+    auto passes = [](float v, uint32_t o) __attribute__((always_inline)) { return v > negative_infinity() && ordered(v) > o; };
+    const int each = rounds_of_lane * VECTORS, items = s.n_lanes * each;  // vectors of a lane, and of all these lanes
+    for (int i = t; i < items; i += THREADS) {
+        const int q = s.lanes[i / each], n = i % each;
+        const int v = r.first + ((n / VECTORS * WAVES + q / 64) * VECTORS + n % VECTORS) * 64 + (q & 63);
+        T raw[E];
+        const int at = r.take(v, raw);
+        r.leave_out(v, at, raw);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = to_float(raw[e]);
+            list(reaches(x, from), x, at + e);
+        }
+    }
+    meet_all<WAVES>();
+    int n = s.count;
+    if (n > LIST) {
+        auto every = [&](auto f) __attribute__((always_inline)) {  // all values of the range
+            for (int v = r.first + t; v < r.end; v += THREADS) {
+                T raw[E];
+                const int at = r.take(v, raw);
+                r.leave_out(v, at, raw);
+#pragma unroll
+                for (int e = 0; e < E; ++e) f(to_float(raw[e]), at + e);
+            }
+        };
+        auto list_above = [&]() __attribute__((always_inline)) {
+            meet_all<WAVES>();
+            if (t == 0) s.count = 0;
+            meet_all<WAVES>();
+            every([&](float x, int index) { list(passes(x, from), x, index); });
+            meet_all<WAVES>();
+            return s.count;
+        };
+        n = list_above();
+        if (n > LIST) {
+            from = 0;
+            for (int b = 31; b >= 0; --b) {
+                meet_all<WAVES>();
+                if (t == 0) s.count = 0;
+                meet_all<WAVES>();
+                int mine = 0;
+                every([&](float x, int) { mine += reaches(x, from | 1u << b); });
+                atomicAdd(&s.count, mine);
+                meet_all<WAVES>();
+                if (s.count >= top) from |= 1u << b;
+            }
+            n = list_above();  // fewer than `top`
+        }
+        // the first ones that equal it
+        for (int v0 = r.first; n < top && v0 < r.end; v0 += THREADS) {
+            T raw[E];
+            const int at = r.take(v0 + t, raw);
+            r.leave_out(v0 + t, at, raw);
+            int mine = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = to_float(raw[e]);
+                mine += reaches(x, from) && !passes(x, from);
+            }
+            int upto = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += other;
+            }
+            if (lane == 63) s.wave_count[wave] = upto;
+            meet_all<WAVES>();
+            int place = n + upto - mine, all = 0;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                if (k < wave) place += s.wave_count[k];
+                all += s.wave_count[k];
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = to_float(raw[e]);
+                if (!reaches(x, from) || passes(x, from)) continue;
+                if (place < top) s.list[place] = key_of(x, at + e);
+                ++place;
+            }
+            n = min(n + all, top);
+            meet_all<WAVES>();
+        }
+    }
+    for (int i = t; i < n; i += THREADS) {
+        const uint64_t key = s.list[i];
+        int place = 0;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) place += s.list[k] > key;
+        if (place < top) s.best[place] = key;
+    }
+    meet_all<WAVES>();
+}
+
+// WAVES wavefronts take a row, or a part of one, in rounds of VECTORS vectors to a lane; the next round is asked for before the present
 // one is worked on.  Where rows are few, parts of them are blocks of their own, and join_parts_kernel finishes.  Bound by memory; behind it by
 // the vector ALU: about ten operations and an exponential for a value.
-constexpr int VECTORS = 4;
-
 template <class T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
 {
     constexpr int E = 16 / sizeof(T), ROWS = 4 / WAVES;  // rows of a block
-    constexpr int EACH = 64 * VECTORS * E;
-    __shared__ uint64_t lists[TOP ? 4 * LIST : 1], best_of_row[TOP ? ROWS * PS_LOGPROB_MAX_TOP : 1];
+    constexpr int EACH = 64 * VECTORS;                   // vectors of a wavefront in a round
+    __shared__ Scratch<WAVES> scratch[TOP ? ROWS : 1];
     __shared__ Sums meet[4];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), w = wave % WAVES, of = wave / WAVES;
     const float c = a.scale * LOG2E;
     const int64_t total = a.rows * a.parts;
     for (int64_t block = (int64_t)blockIdx.x * ROWS; block < total; block += (int64_t)gridDim.x * ROWS) {
         const bool there = block + of < total;
-        const int64_t item = there ? block + of : 0, row = item / a.parts;
+        const int64_t item = there ? block + of : total - 1, row = item / a.parts;
         const int part = (int)(item - row * a.parts);
-        const T* const z = static_cast<const T*>(a.logits) + row * a.row;
+        Range<T, WAVES> r;
+        r.z = static_cast<const T*>(a.logits) + row * a.row;
+        r.vocab = a.vocab;
+        r.ahead = (int)(reinterpret_cast<uintptr_t>(r.z) / sizeof(T) % E);
+        const int vectors = (a.vocab + r.ahead + E - 1) / E, of_part = a.part_rounds * (WAVES * EACH);
+        r.first = part * of_part;
+        r.end = part + 1 < a.parts ? min(r.first + of_part, vectors) : vectors;
         float at_token = 0.f;
         const int64_t token = a.parts == 1 ? take_token<T>(a, row, at_token) : -1;
-        const int64_t begin = (int64_t)part * a.part_rounds * (WAVES * EACH);
-        const int64_t end = there ? min(begin + (int64_t)a.part_rounds * (WAVES * EACH), (int64_t)a.vocab) : 0;
         Sums sums{negative_infinity(), 0.f, 0.f};
-        Best best{lists + (TOP ? wave * LIST : 0), 0, a.top, 0};
-        // Vector j of a lane: columns base + j * 64 E + lane E on.  WHOLE: all of them are there; else a vector that would go past the end ends
-        // with it, and what it has in common with others, `again` values, is left out; so nothing is read in a branch, where the
-        // compiler would wait for it.
-        auto take = [&](int64_t base, T (&raw)[VECTORS][E], bool whole) __attribute__((always_inline)) {
+        // rounds whose vectors are all whole, and those with the row's first and last ones
+        auto whole = [&](int v) __attribute__((always_inline)) { return r.column(v) >= 0 && r.column(v + EACH) <= a.vocab && v + EACH <= r.end; };
+        auto take = [&](int v, T (&raw)[VECTORS][E]) __attribute__((always_inline)) {
+            if (whole(v)) {
+                const T* from = r.z + r.column(v + lane);
 #pragma unroll
-            for (int j = 0; j < VECTORS; ++j) {
-                const int64_t at = base + j * 64 * E + lane * E;
-                __builtin_memcpy(raw[j], z + (whole ? at : min(at, end - E)), 16);
+                for (int j = 0; j < VECTORS; ++j) __builtin_memcpy(raw[j], from + j * 64 * E, 16);
+            } else {
+                int at[VECTORS];
+#pragma unroll
+                for (int j = 0; j < VECTORS; ++j) at[j] = r.take(v + j * 64 + lane, raw[j]);
+#pragma unroll
+                for (int j = 0; j < VECTORS; ++j) r.leave_out(v + j * 64 + lane, at[j], raw[j]);
             }
         };
-        auto round = [&](int64_t base, const T (&raw)[VECTORS][E], auto whole) __attribute__((always_inline)) {
-            constexpr bool WHOLE = decltype(whole)::value;
-            auto value = [&](int j, int e) __attribute__((always_inline)) {
-                if constexpr (WHOLE) return to_float(raw[j][e]);
-                const int64_t at = base + j * 64 * E + lane * E;
-                return (int64_t)e < at - min(at, end - E) ? negative_infinity() : to_float(raw[j][e]);
-            };
-            float high = negative_infinity(), highs[VECTORS];
+        T now[VECTORS][E], then[VECTORS][E];
+        int v = r.first + w * EACH;
+        if (v < r.end) take(v, now);
+        for (; v < r.end; v += WAVES * EACH) {
+            if (v + WAVES * EACH < r.end) take(v + WAVES * EACH, then);
+            float high = negative_infinity();
 #pragma unroll
-            for (int j = 0; j < VECTORS; ++j) {
-                highs[j] = negative_infinity();
+            for (int j = 0; j < VECTORS; ++j)
 #pragma unroll
-                for (int e = 0; e < E; ++e) highs[j] = fmaxf(highs[j], value(j, e));
-                high = fmaxf(high, highs[j]);
-            }
+                for (int e = 0; e < E; ++e) high = fmaxf(high, to_float(now[j][e]));
             if (high > sums.m) {
                 const float d = fmaxf((sums.m - high) * c, NEVER), f = __builtin_amdgcn_exp2f(d);  // (nothing yet: 0)
                 sums.u = (sums.u + d * sums.s) * f;
@@ -250,97 +363,39 @@ __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
             for (int j = 0; j < VECTORS; ++j)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float t = (value(j, e) - m) * c, p = __builtin_amdgcn_exp2f(t);
+                    const float t = (to_float(now[j][e]) - m) * c, p = __builtin_amdgcn_exp2f(t);
                     sums.s += p;
                     sums.u = fmaf(p, fmaxf(t, NEVER), sums.u);
                 }
-            if constexpr (TOP) {
-                // Values of later rounds have higher indexes, so those that only equal the last kept one come too late.
-                const float over = best.least ? value_of(best.least) : negative_infinity();
-                const unsigned long long some = __ballot(high > over);
-                if (some) {
-                    // the largest values of `top` lanes are `top` values: what is below all of these is no candidate
-                    float from = over;
-                    if (__popcll(some) >= a.top) from = fmaxf(from, value_of((uint64_t)kth_of_lanes(ordered(high), a.top) << 32));
-#pragma unroll
-                    for (int j = 0; j < VECTORS; ++j) {
-                        if (!__ballot(highs[j] >= from && highs[j] > negative_infinity())) continue;
-                        const int64_t at = base + j * 64 * E + lane * E;
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float v = value(j, e);
-                            best.add(v >= from && v > negative_infinity(), v, (int)(WHOLE ? at : min(at, end - E)) + e);
-                        }
-                    }
-                    if (best.count >= a.top) best.cut();
-                }
-            }
-        };
-        if (a.vocab >= E) {
-            int64_t base = begin + w * EACH;
-            T now[VECTORS][E], then[VECTORS][E];
-            if (base + EACH <= end) take(base, now, true);
-            for (; base + EACH <= end; base += WAVES * EACH) {
-                if (base + (WAVES + 1) * EACH <= end) take(base + WAVES * EACH, then, true);
-                round(base, now, std::true_type{});
-#pragma unroll
-                for (int j = 0; j < VECTORS; ++j)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) now[j][e] = then[j][e];
-            }
-            if (base < end) {
-                take(base, now, false);
-                round(base, now, std::false_type{});
-            }
-        } else if (there && w == 0) {
-            // a row shorter than 16 bytes, in the last elements of a vector as it would be there
-            T raw[VECTORS][E];
 #pragma unroll
             for (int j = 0; j < VECTORS; ++j)
 #pragma unroll
-                for (int e = 0; e < E; ++e) raw[j][e] = from_float<T>(negative_infinity());
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = e - (E - a.vocab);
-                const T v = z[max(i, 0)];
-                if (lane == 0 && i >= 0) raw[0][e] = v;
-            }
-            round(a.vocab - E, raw, std::true_type{});
+                for (int e = 0; e < E; ++e) now[j][e] = then[j][e];
         }
+        const float high = sums.m;
         sums = join_lanes(sums, c);
-        if constexpr (TOP) {
-            best.cut();  // in order, also where there are fewer
-            if (lane < a.top && lane >= best.count) best.list[lane] = 0;
-        }
+        if constexpr (TOP) best_of_range<T, WAVES>(r, scratch[of], a.top, (r.end - r.first + WAVES * EACH - 1) / (WAVES * EACH), high);
         if constexpr (WAVES > 1) {
             if (lane == 0) meet[wave] = sums;
-            if (TOP && threadIdx.x < (uint32_t)a.top) best_of_row[threadIdx.x] = 0;
             __syncthreads();
             sums = meet[0];
 #pragma unroll
             for (int k = 1; k < WAVES; ++k) sums = join(sums, meet[k], c);
-            if constexpr (TOP) {
-                merge(lists, LIST, WAVES, a.top, best_of_row, threadIdx.x, 256);
-                __syncthreads();
-            }
-        } else {
-            __builtin_amdgcn_wave_barrier();
         }
         if (there && w == 0) {
-            const uint64_t* const kept = WAVES > 1 ? best_of_row : best.list;
             if (a.parts > 1) {
                 if (lane == 0) {
                     a.part_sums[item * 3] = sums.m;
                     a.part_sums[item * 3 + 1] = sums.s;
                     a.part_sums[item * 3 + 2] = sums.u;
                 }
-                if (TOP && lane < a.top) a.part_lists[item * a.top + lane] = kept[lane];
+                if (TOP && lane < a.top) a.part_lists[item * a.top + lane] = scratch[of].best[lane];
             } else {
                 if (lane == 0) finish_row<T>(a, row, sums, token, at_token);
-                if (TOP && lane < a.top) write_best(a, row, lane, kept[lane], sums);
+                if (TOP && lane < a.top) write_best(a, row, lane, scratch[of].best[lane], sums);
             }
         }
-        if (WAVES > 1) __syncthreads();  // what met in LDS is written again
+        meet_all<WAVES>();  // what is in LDS is written again
     }
 }
 
@@ -350,27 +405,48 @@ constexpr int MOST_PARTS = 64;
 template <class T, bool TOP>
 __global__ __launch_bounds__(256) void join_parts_kernel(ForwardArgs a)
 {
-    __shared__ uint64_t lists[TOP ? MOST_PARTS * PS_LOGPROB_MAX_TOP : 1], best[TOP ? PS_LOGPROB_MAX_TOP : 1];
+    __shared__ uint64_t list[TOP ? MOST_PARTS * PS_LOGPROB_MAX_TOP : 1], best[TOP ? PS_LOGPROB_MAX_TOP : 1];
+    __shared__ float high[64];
+    __shared__ int count;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63;
     const float c = a.scale * LOG2E;
     float at_token;
     const int64_t token = take_token<T>(a, row, at_token);
-    if constexpr (TOP) {
-        for (int i = threadIdx.x; i < a.parts * a.top; i += 256) lists[i] = a.part_lists[row * a.parts * a.top + i];
-        if (threadIdx.x < (uint32_t)a.top) best[threadIdx.x] = 0;
-    }
     Sums x{negative_infinity(), 0.f, 0.f};
     if (lane < a.parts) {
         const float* p = a.part_sums + (row * a.parts + lane) * 3;
         x = Sums{p[0], p[1], p[2]};
     }
-    x = join_lanes(x, c);
     if constexpr (TOP) {
+        // Of parts that have i keys or more each, the i-th keys of n parts are reached by n * i: none of the best is below the n-th largest
+        // i-th key, where n * i is `top` or more.
+        const uint64_t* const lists = a.part_lists + row * a.parts * a.top;
+        const int i = (a.top + a.parts - 1) / a.parts, n = (a.top + i - 1) / i;
+        if (threadIdx.x < 64) {
+            const uint64_t key = lists[min(lane, a.parts - 1) * a.top + i - 1];
+            high[lane] = lane < a.parts && key ? value_of(key) : negative_infinity();
+        }
+        if (threadIdx.x < (uint32_t)a.top) best[threadIdx.x] = 0;
+        if (threadIdx.x == 0) count = 0;
         __syncthreads();
-        merge(lists, a.top, a.parts, a.top, best, threadIdx.x, 256);
+        const uint32_t from = kth_of_lanes<1>(high, n);
+        for (int k = threadIdx.x; k < a.parts * a.top; k += 256) {
+            const uint64_t key = lists[k];
+            if (key && (uint32_t)(key >> 32) >= from) list[atomicAdd(&count, 1)] = key;
+        }
+        __syncthreads();
+        // the order in which they were listed does not matter
+        for (int k = threadIdx.x; k < count; k += 256) {
+            const uint64_t key = list[k];
+            int place = 0;
+#pragma unroll 8
+            for (int o = 0; o < count; ++o) place += list[o] > key;
+            if (place < a.top) best[place] = key;
+        }
         __syncthreads();
     }
+    x = join_lanes(x, c);
     if (threadIdx.x == 0) finish_row<T>(a, row, x, token, at_token);
     if (TOP && threadIdx.x < (uint32_t)a.top) write_best(a, row, threadIdx.x, best[threadIdx.x], x);
 }
@@ -476,7 +552,7 @@ struct Cut {
 };
 Cut cut_rows(const ps_logprob& l)
 {
-    const int64_t round = 4 * 64 * VECTORS * 16 / dtype_size(l.dtype), rounds = (l.vocab + round - 1) / round;
+    const int64_t round = 4 * 64 * VECTORS * 16 / dtype_size(l.dtype), rounds = (l.vocab + round - 1) / round;  // (a part more for what is ahead of a row)
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, MOST_PARTS), l.rows ? 8 * COMPUTE_UNITS / l.rows : 1));
     const int64_t each = (rounds + parts - 1) / parts;
     return {(int)((rounds + each - 1) / each), (int)each};
