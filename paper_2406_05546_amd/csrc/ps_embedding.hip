@@ -362,6 +362,18 @@ __device__ __forceinline__ T* row_of_key(const SumArgs& a, uint32_t key)
     return static_cast<T*>(a.dtable) + (int64_t)g * a.table_matrix + (int64_t)v * a.table_row;
 }
 
+// E values as they were read
+template <class T, int E>
+struct Held {
+    uintx4 bits;
+    __device__ __forceinline__ float value(int e) const { return element<T>(bits, e); }
+};
+template <class T>
+struct Held<T, 1> {
+    T bits;
+    __device__ __forceinline__ float value(int) const { return to_float(bits); }
+};
+
 // Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.  A lane
 // whose columns would go past the row's end takes the last E of the row, which others have too (E is 1 for rows shorter than 16 bytes).  Bound by
 // memory: SUM_AHEAD rows are asked for while as many are added up, without a branch between them, at which the compiler would wait.
@@ -398,12 +410,12 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
     const unsigned long long ends = (pieces | ~exist) >> 1;
     const unsigned long long goes_on = exist >> 1 & ~(begins >> 1), starts_run = begins & pieces;
     float sum[E] = {};
-    T now[SUM_AHEAD][E], then[SUM_AHEAD][E];
-    auto take = [&](int at, T (&raw)[SUM_AHEAD][E]) __attribute__((always_inline)) {
+    Held<T, E> now[SUM_AHEAD], then[SUM_AHEAD];
+    auto take = [&](int at, Held<T, E> (&raw)[SUM_AHEAD]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < SUM_AHEAD; ++u) {
             const int64_t r = (uint32_t)__builtin_amdgcn_readlane(row, min(at + u, to - 1));
-            __builtin_memcpy(raw[u], static_cast<const T*>(a.dy) + r * a.dy_row + col, sizeof(raw[u]));
+            __builtin_memcpy(&raw[u].bits, static_cast<const T*>(a.dy) + r * a.dy_row + col, sizeof(T) * E);
         }
     };
     take(from, now);
@@ -416,7 +428,7 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
             const bool first = pieces >> place & 1;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float x = to_float(now[u][e]);
+                const float x = now[u].value(e);
                 sum[e] = first ? x : sum[e] + x;
             }
             if (!(ends >> place & 1) || !there) continue;
@@ -432,9 +444,7 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
             }
         }
 #pragma unroll
-        for (int u = 0; u < SUM_AHEAD; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) now[u][e] = then[u][e];
+        for (int u = 0; u < SUM_AHEAD; ++u) now[u] = then[u];
     }
 }
 

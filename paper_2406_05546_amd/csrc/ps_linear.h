@@ -28,6 +28,20 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int LINEAR_XCDS = 8, COMPUTE_UNITS = 256;
 
+#if defined(__HIPCC__)
+// Value e of 16 bytes.  Values that wait in registers stay packed this way; arrays of 16-bit ones take a register each.
+template <class T>
+__device__ __forceinline__ float element(const uintx4& x, int e)
+{
+    if constexpr (sizeof(T) == 4)
+        return __uint_as_float(x[e]);
+    else if constexpr (__is_same(T, bf16_t))
+        return __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+    else
+        return to_float(f16_t{(uint16_t)(x[e / 2] >> (e & 1) * 16)});
+}
+#endif
+
 // ---------------------------------------------------------------------------------------------------------------
 // Groups
 

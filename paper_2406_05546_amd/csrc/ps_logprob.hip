@@ -116,27 +116,36 @@ struct Range {
 
     __device__ __forceinline__ int column(int v) const { return v * E - ahead; }
     // A vector that goes past an end of the row is read where the row's first or last one is, so that nothing is read in a branch, where the compiler
-    // would wait for it, or beside the row; what is no column of the vector, or the vector none of the range, becomes -infinity.  Gives the
-    // column of raw[0].
-    __device__ __forceinline__ int take(int v, T (&raw)[E]) const
+    // would wait for it, or beside the row; `leave_out` makes -infinity of what is no column of the vector, or of a vector of none of the
+    // range's.  `from`: the column of the first value that was read.
+    __device__ __forceinline__ int from(int v) const { return vocab >= E ? min(max(column(v), 0), vocab - E) : column(v); }
+    __device__ __forceinline__ void take(int v, uintx4& raw) const
     {
-        const int at = column(v);
-        int from = at;
         if (vocab >= E) {
-            from = min(max(at, 0), vocab - E);
-            __builtin_memcpy(raw, z + from, 16);
+            __builtin_memcpy(&raw, z + from(v), 16);
         } else {
+            T x[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) raw[e] = z[min(max(at + e, 0), vocab - 1)];
+            for (int e = 0; e < E; ++e) x[e] = z[min(max(column(v) + e, 0), vocab - 1)];
+            __builtin_memcpy(&raw, x, 16);
         }
-        return from;
     }
-    __device__ __forceinline__ void leave_out(int v, int from, T (&raw)[E]) const
+    __device__ __forceinline__ void leave_out(int v, uintx4& raw) const
     {
         // from + e is in the vector and the row
-        const int at = column(v), lo = max(at, 0) - from, hi = v < end ? min(at + E, vocab) - from : 0;
+        const int at = column(v), lo = max(at, 0) - from(v), hi = v < end ? min(at + E, vocab) - from(v) : 0;
+        constexpr int IN_DWORD = E / 4;
+        constexpr uint32_t LEFT_OUT = sizeof(T) == 4 ? 0xff800000u : __is_same(T, bf16_t) ? 0xff80ff80u : 0xfc00fc00u;
 #pragma unroll
-        for (int e = 0; e < E; ++e) raw[e] = e >= lo && e < hi ? raw[e] : from_float<T>(negative_infinity());
+        for (int i = 0; i < 4; ++i) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int k = 0; k < IN_DWORD; ++k) {
+                const int e = i * IN_DWORD + k;
+                in |= e >= lo && e < hi ? (IN_DWORD == 1 ? ~0u : 0xffffu << 16 * k) : 0u;
+            }
+            raw[i] = (raw[i] & in) | (LEFT_OUT & ~in);
+        }
     }
 };
 
@@ -182,7 +191,7 @@ __device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k)
 }
 
 template <class T, int WAVES>
-__device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<WAVES>& s, int top, int rounds_of_lane, float high)
+__device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<WAVES>& s, int top, int each, float high)
 {
     constexpr int E = Range<T, WAVES>::E, THREADS = Range<T, WAVES>::THREADS;
     const int t = threadIdx.x % THREADS, wave = t / 64, lane = t & 63;
@@ -206,16 +215,17 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
     // whether v is a value, and reaches or passes a number of `ordered`
     auto reaches = [](float v, uint32_t o) __attribute__((always_inline)) { return v > negative_infinity() && ordered(v) >= o; };
     auto passes = [](float v, uint32_t o) __attribute__((always_inline)) { return v > negative_infinity() && ordered(v) > o; };
-    const int each = rounds_of_lane * VECTORS, items = s.n_lanes * each;  // vectors of a lane, and of all these lanes
+    const int items = s.n_lanes * each;  // `each` vectors of a lane
     for (int i = t; i < items; i += THREADS) {
         const int q = s.lanes[i / each], n = i % each;
-        const int v = r.first + ((n / VECTORS * WAVES + q / 64) * VECTORS + n % VECTORS) * 64 + (q & 63);
-        T raw[E];
-        const int at = r.take(v, raw);
-        r.leave_out(v, at, raw);
+        const int v = r.first + (n * WAVES + q / 64) * 64 + (q & 63);
+        uintx4 raw;
+        const int at = r.from(v);
+        r.take(v, raw);
+        r.leave_out(v, raw);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = to_float(raw[e]);
+            const float x = element<T>(raw, e);
             list(reaches(x, from), x, at + e);
         }
     }
@@ -224,11 +234,12 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
     if (n > LIST) {
         auto every = [&](auto f) __attribute__((always_inline)) {  // all values of the range
             for (int v = r.first + t; v < r.end; v += THREADS) {
-                T raw[E];
-                const int at = r.take(v, raw);
-                r.leave_out(v, at, raw);
+                uintx4 raw;
+                const int at = r.from(v);
+                r.take(v, raw);
+                r.leave_out(v, raw);
 #pragma unroll
-                for (int e = 0; e < E; ++e) f(to_float(raw[e]), at + e);
+                for (int e = 0; e < E; ++e) f(element<T>(raw, e), at + e);
             }
         };
         auto list_above = [&]() __attribute__((always_inline)) {
@@ -256,13 +267,14 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
         }
         // the first ones that equal it
         for (int v0 = r.first; n < top && v0 < r.end; v0 += THREADS) {
-            T raw[E];
-            const int at = r.take(v0 + t, raw);
-            r.leave_out(v0 + t, at, raw);
+            uintx4 raw;
+            const int at = r.from(v0 + t);
+            r.take(v0 + t, raw);
+            r.leave_out(v0 + t, raw);
             int mine = 0;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float x = to_float(raw[e]);
+                const float x = element<T>(raw, e);
                 mine += reaches(x, from) && !passes(x, from);
             }
             int upto = mine;
@@ -281,7 +293,7 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float x = to_float(raw[e]);
+                const float x = element<T>(raw, e);
                 if (!reaches(x, from) || passes(x, from)) continue;
                 if (place < top) s.list[place] = key_of(x, at + e);
                 ++place;
@@ -307,7 +319,7 @@ template <class T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
 {
     constexpr int E = 16 / sizeof(T), ROWS = 4 / WAVES;  // rows of a block
-    constexpr int EACH = 64 * VECTORS;                   // vectors of a wavefront in a round
+    constexpr int EACH = 64 * VECTORS;                   // vectors of a wavefront in a round, 64 of each 64 * WAVES
     __shared__ Scratch<WAVES> scratch[TOP ? ROWS : 1];
     __shared__ Sums meet[4];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), w = wave % WAVES, of = wave / WAVES;
@@ -327,31 +339,18 @@ __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
         float at_token = 0.f;
         const int64_t token = a.parts == 1 ? take_token<T>(a, row, at_token) : -1;
         Sums sums{negative_infinity(), 0.f, 0.f};
-        // rounds whose vectors are all whole, and those with the row's first and last ones
-        auto whole = [&](int v) __attribute__((always_inline)) { return r.column(v) >= 0 && r.column(v + EACH) <= a.vocab && v + EACH <= r.end; };
-        auto take = [&](int v, T (&raw)[VECTORS][E]) __attribute__((always_inline)) {
-            if (whole(v)) {
-                const T* from = r.z + r.column(v + lane);
+        // Vector j of a round is v + j * WAVES * 64; `all` of n from v on are whole ones of the range.
+        auto all = [&](int v, int n) __attribute__((always_inline)) { return r.column(v) >= 0 && r.column(v + n) <= a.vocab && v + n <= r.end; };
+        auto take = [&](int v, uintx4 (&raw)[VECTORS]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < VECTORS; ++j) __builtin_memcpy(raw[j], from + j * 64 * E, 16);
-            } else {
-                int at[VECTORS];
-#pragma unroll
-                for (int j = 0; j < VECTORS; ++j) at[j] = r.take(v + j * 64 + lane, raw[j]);
-#pragma unroll
-                for (int j = 0; j < VECTORS; ++j) r.leave_out(v + j * 64 + lane, at[j], raw[j]);
-            }
+            for (int j = 0; j < VECTORS; ++j) r.take(v + j * WAVES * 64 + lane, raw[j]);
         };
-        T now[VECTORS][E], then[VECTORS][E];
-        int v = r.first + w * EACH;
-        if (v < r.end) take(v, now);
-        for (; v < r.end; v += WAVES * EACH) {
-            if (v + WAVES * EACH < r.end) take(v + WAVES * EACH, then);
+        auto add = [&](const auto& raw) __attribute__((always_inline)) {
             float high = negative_infinity();
+            for (const uintx4& x : raw) {
 #pragma unroll
-            for (int j = 0; j < VECTORS; ++j)
-#pragma unroll
-                for (int e = 0; e < E; ++e) high = fmaxf(high, to_float(now[j][e]));
+                for (int e = 0; e < E; ++e) high = fmaxf(high, element<T>(x, e));
+            }
             if (high > sums.m) {
                 const float d = fmaxf((sums.m - high) * c, NEVER), f = __builtin_amdgcn_exp2f(d);  // (nothing yet: 0)
                 sums.u = (sums.u + d * sums.s) * f;
@@ -359,22 +358,38 @@ __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
                 sums.m = high;
             }
             const float m = sums.m == negative_infinity() ? 0.f : sums.m;
-#pragma unroll
-            for (int j = 0; j < VECTORS; ++j)
+            for (const uintx4& x : raw) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float t = (to_float(now[j][e]) - m) * c, p = __builtin_amdgcn_exp2f(t);
+                    const float t = (element<T>(x, e) - m) * c, p = __builtin_amdgcn_exp2f(t);
                     sums.s += p;
                     sums.u = fmaf(p, fmaxf(t, NEVER), sums.u);
                 }
+            }
+        };
+        uintx4 now[VECTORS], then[VECTORS];
+        int v = r.first + w * 64;
+        if (v < r.end) take(v, now);
+        for (; v < r.end; v += WAVES * EACH) {
+            if (v + WAVES * EACH < r.end) take(v + WAVES * EACH, then);
+            if (all(v, (VECTORS - 1) * WAVES * 64 + 64)) {
+                add(now);
+            } else {
 #pragma unroll
-            for (int j = 0; j < VECTORS; ++j)
+                for (int j = 0; j < VECTORS; ++j) {
+                    const int vj = v + j * WAVES * 64;
+                    if (vj >= r.end) continue;
+                    uintx4 one[1] = {now[j]};
+                    if (!all(vj, 64)) r.leave_out(vj + lane, one[0]);
+                    add(one);
+                }
+            }
 #pragma unroll
-                for (int e = 0; e < E; ++e) now[j][e] = then[j][e];
+            for (int j = 0; j < VECTORS; ++j) now[j] = then[j];
         }
         const float high = sums.m;
         sums = join_lanes(sums, c);
-        if constexpr (TOP) best_of_range<T, WAVES>(r, scratch[of], a.top, (r.end - r.first + WAVES * EACH - 1) / (WAVES * EACH), high);
+        if constexpr (TOP) best_of_range<T, WAVES>(r, scratch[of], a.top, (r.end - r.first + WAVES * 64 - 1) / (WAVES * 64), high);
         if constexpr (WAVES > 1) {
             if (lane == 0) meet[wave] = sums;
             __syncthreads();
@@ -484,11 +499,11 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
         const float gh = a.dentropy ? a.dentropy[row * a.dentropy_stride] : 0.f;
         const float A = -a.scale * (gl + gh * entropy), B = -a.scale * gh * LN2;
         const bool none = m == negative_infinity() && log2_s == negative_infinity();
-        auto give = [&](int64_t at, int n, const T (&raw)[E]) __attribute__((always_inline)) {
+        auto give = [&](int64_t at, int n, const uintx4& raw) __attribute__((always_inline)) {
             float d[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float t = (to_float(raw[e]) - m) * c - log2_s;
+                const float t = (element<T>(raw, e) - m) * c - log2_s;
                 d[e] = __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, NEVER), A);
             }
             if (token >= at && token < at + E) {
@@ -504,21 +519,23 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
         };
         if (first + EACH <= a.vocab) {
             // without a branch between them, at which the compiler would wait
-            T raw[VECTORS][E];
+            uintx4 raw[VECTORS];
 #pragma unroll
-            for (int j = 0; j < VECTORS; ++j) __builtin_memcpy(raw[j], z + base + j * 256 * E, 16);
+            for (int j = 0; j < VECTORS; ++j) __builtin_memcpy(&raw[j], z + base + j * 256 * E, 16);
 #pragma unroll
             for (int j = 0; j < VECTORS; ++j) give(base + j * 256 * E, E, raw[j]);
         } else {
             for (int at = base; at < a.vocab; at += 256 * E) {
                 const int n = min(E, a.vocab - at);
-                T raw[E] = {};
+                T x[E] = {};
+                uintx4 raw;
                 if (n == E) {
-                    __builtin_memcpy(raw, z + at, 16);
+                    __builtin_memcpy(&raw, z + at, 16);
                 } else {
 #pragma unroll
                     for (int e = 0; e < E; ++e)
-                        if (e < n) raw[e] = z[at + e];
+                        if (e < n) x[e] = z[at + e];
+                    __builtin_memcpy(&raw, x, 16);
                 }
                 give(at, n, raw);
             }
