@@ -341,10 +341,14 @@ struct SumArgs {
     float scale;
 };
 
-// The first place of `key` among the sorted keys before `end`, where it is itself.  For a whole wavefront.
+// The first place of `key` among the sorted keys before `end`, where it is itself.  For a whole wavefront: one look at the 64 before, and
+// one for every power of 64 of the rest.
 __device__ __forceinline__ int first_place(const uint32_t* keys, uint32_t key, int end)
 {
-    int lo = 0, hi = end;  // keys before lo are below, the one at hi is not
+    const int near = end - 64 + (int)(threadIdx.x & 63);
+    const int same = __popcll(__ballot(near >= 0 && keys[max(near, 0)] == key));
+    if (same < 64) return end - same;
+    int lo = 0, hi = end - 64;  // keys before lo are below, the one at hi is not
     while (lo < hi) {
         const int step = (hi - lo + 63) >> 6, p = lo + (int)(threadIdx.x & 63) * step;
         const int below = __popcll(__ballot(p < hi && keys[p] < key));  // lanes in order
