@@ -495,8 +495,17 @@ template <class T>
 __device__ __forceinline__ void keep(const Epilogue& e, const float (&bias)[8], int64_t row, int col, int valid, const float (&v)[8])
 {
     float z[8];
+    if (e.bias) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = i < valid ? to_float(from_float<T>(e.bias ? v[i] + bias[i] : v[i])) : 0.f;
+        for (int i = 0; i < 8; ++i) z[i] = to_float(from_float<T>(v[i] + bias[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = to_float(from_float<T>(v[i]));
+    }
+    if (valid < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = i < valid ? z[i] : 0.f;
+    }
     checkpoint_store(e.codes + row * e.codes_row, e.scales + row * e.scales_row, col, valid, z);
 }
 template <class T, bool RESIDUAL, int N>
@@ -1039,7 +1048,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void linear_kernel(Product p)
         // took 5 us a tile).
         // What comes to LDS for the next tile is older than the stores here, and the loads of what is added
         // wait for it too; so the bias is there before, once for the tile.
-        const Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
+        Epilogue epi = argument().epi;  // copies: behind a store the argument would be read again
+        if constexpr (KEPT) epi.pre = nullptr;
         const int rows = argument().out_rows, cols = argument().out_cols;
         constexpr int PIECES = FINISH_PIECES, LANES = TC * 2, AT_ONCE = 64 / LANES;  // lanes of a row, rows at once
         const Tile done = tile;
