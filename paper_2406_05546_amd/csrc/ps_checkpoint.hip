@@ -6,28 +6,6 @@ namespace {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-struct CodeArgs {
-    void* x;
-    uint8_t *codes, *scales;
-    int64_t x_row, row, scale_row, rows;
-    int32_t cols, cols_to, pieces, each, act;  // pieces of eight columns of a row; rows of a block
-    Groups groups;
-};
-
-// A block takes `each` rows (up to 64), a thread pieces of eight columns of them.  Bound by memory: CODE_AHEAD pieces are asked for together,
-// without a branch between them, at which the compiler would wait; a row's last piece, where it is partial, is read again.
-constexpr int CODE_AHEAD = 4;
-
-struct Piece {
-    int64_t row;
-    int col, n;  // n: columns that exist
-};
-__device__ __forceinline__ Piece piece_of(const CodeArgs& a, int64_t first, int item)
-{
-    const int line = (int)((uint32_t)item / (uint32_t)a.pieces), col = (int)((uint32_t)item % (uint32_t)a.pieces) * 8;
-    return {first + line, col, min(8, a.cols - col)};
-}
-
 template <class T>
 __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
 {
@@ -67,41 +45,7 @@ __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
 template <class T>
 __global__ __launch_bounds__(256) void decode_kernel(CodeArgs a)
 {
-    for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
-        const int items = (int)min((int64_t)a.each, a.rows - first) * a.pieces;
-        for (int at = threadIdx.x; at < items; at += 256 * CODE_AHEAD) {
-            uint32_t code[CODE_AHEAD][2];
-            uint8_t scale[CODE_AHEAD];
-            Piece p[CODE_AHEAD];
-#pragma unroll
-            for (int i = 0; i < CODE_AHEAD; ++i) {
-                p[i] = piece_of(a, first, min(at + i * 256, items - 1));
-                if (a.cols >= 8) __builtin_memcpy(code[i], a.codes + p[i].row * a.row + min(p[i].col, a.cols - 8), 8);
-                scale[i] = a.scales[p[i].row * a.scale_row + min(p[i].col, a.cols - 1) / PS_CHECKPOINT_BLOCK];
-            }
-#pragma unroll
-            for (int i = 0; i < CODE_AHEAD; ++i) {
-                if (at + i * 256 >= items) continue;
-                float v[8];
-                if (p[i].n < 8) {
-                    load_codes(a.codes + p[i].row * a.row + p[i].col, p[i].n, code[i]);
-                    if (p[i].n <= 0) scale[i] = 127;  // behind the columns: 0 whatever is there
-                }
-                checkpoint_decode(code[i], scale[i], v);
-                if (a.act == PS_ACT_RELU) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_RELU>(v[e]);
-                } else if (a.act == PS_ACT_GELU) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_GELU>(v[e]);
-                } else if (a.act == PS_ACT_SILU) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = activate<PS_ACT_SILU>(v[e]);
-                }
-                store_columns(static_cast<T*>(a.x) + p[i].row * a.x_row + p[i].col, min(8, a.cols_to - p[i].col), v);
-            }
-        }
-    }
+    decode_rows<T>(a, blockIdx.x, gridDim.x);
 }
 
 template <class F>
@@ -132,10 +76,10 @@ CodeArgs code_args(const Groups& groups, int64_t rows, int64_t cols, const ps_ma
 }
 
 // Rows of 2048 pieces together, or fewer where that leaves less than eight blocks to a compute unit.
-dim3 code_grid(CodeArgs& a)
+uint32_t code_blocks(CodeArgs& a)
 {
     a.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2048 / a.pieces), a.rows / (8 * COMPUTE_UNITS)));
-    return dim3((uint32_t)std::min<int64_t>(up(a.rows, a.each), 1 << 22));
+    return (uint32_t)std::min<int64_t>(up(a.rows, a.each), 1 << 22);
 }
 
 ps_status check_matrix_of_codes(const char* call, int32_t dtype, int64_t rows, int64_t cols, const ps_matrix* x, const ps_checkpoint* c)
@@ -168,18 +112,23 @@ ps_status check_checkpoint(const char* call, const char* name, const ps_checkpoi
 void launch_checkpoint_encode(int dtype, const Groups& groups, int64_t rows, int64_t cols, const ps_matrix& x, const ps_checkpoint& to, hipStream_t s)
 {
     CodeArgs a = code_args(groups, rows, cols, x, to);
-    const dim3 grid = code_grid(a);
+    const dim3 grid(code_blocks(a));
     with_type(dtype, [&](auto t) { hipLaunchKernelGGL(encode_kernel<decltype(t)>, grid, dim3(256), 0, s, a); });
 }
 
-void launch_checkpoint_decode(int dtype, int64_t rows, int64_t cols, const ps_checkpoint& from, int activation, const ps_matrix& x, int64_t cols_to, hipStream_t s)
+CodeArgs decode_args(int64_t rows, int64_t cols, const ps_checkpoint& from, int activation, const ps_matrix& x, int64_t cols_to, uint32_t* blocks)
 {
     CodeArgs a = code_args(Groups{}, rows, cols, x, from);
     a.cols_to = (int32_t)cols_to;
     a.pieces = (int32_t)up(cols_to, 8);
     a.act = activation;
-    const dim3 grid = code_grid(a);
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(decode_kernel<decltype(t)>, grid, dim3(256), 0, s, a); });
+    *blocks = code_blocks(a);
+    return a;
+}
+
+void launch_checkpoint_decode(int dtype, const CodeArgs& a, uint32_t blocks, hipStream_t s)
+{
+    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(decode_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, s, a); });
 }
 
 }  // namespace ps
@@ -203,6 +152,8 @@ extern "C" ps_status ps_checkpoint_decode(int32_t dtype, int64_t rows, int64_t c
     if (st != PS_OK) return st;
     if (activation < PS_ACT_NONE || activation > PS_ACT_SILU) return dense_fail(PS_EINVAL, "%s: unknown activation", call);
     if (!rows) return PS_OK;
-    launch_checkpoint_decode(dtype, rows, cols, *from, activation, *x, cols, static_cast<hipStream_t>(hip_stream));
+    uint32_t blocks;
+    const CodeArgs a = decode_args(rows, cols, *from, activation, *x, cols, &blocks);
+    launch_checkpoint_decode(dtype, a, blocks, static_cast<hipStream_t>(hip_stream));
     return launched(call);
 }

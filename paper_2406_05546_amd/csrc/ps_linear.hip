@@ -41,11 +41,21 @@ struct SlopeArgs {
 // 114 -> 88-104 us, 3.9-4.6 TB/s; 8192 x 512 13.8 -> 9.6).
 constexpr int SLOPE_COLS = 512;
 
+//
+// CODES: pre comes in 8 bits, and blocks with a blockIdx.y from `slopes` on decode x, of which the weight gradient is made, where that is in 8
+// bits, too (backward of 16384 rows 512 -> 2048 138 -> 132 us).
 template <class T, bool CODES>
-__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, CodeArgs x8, uint32_t slopes, uint32_t x8_blocks)
 {
     constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
     __shared__ float meet[3][64][9];
+    if constexpr (CODES) {
+        if (blockIdx.y >= slopes) {
+            const uint32_t block = (blockIdx.y - slopes) * gridDim.x + blockIdx.x;
+            if (block < x8_blocks) decode_rows<T>(x8, block, x8_blocks);
+            return;
+        }
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int g = blockIdx.y / a.parts, part = blockIdx.y % a.parts;
     const GroupRows rows = group_rows(a.groups, g);
@@ -607,6 +617,15 @@ ps_status backward(const char* call, const ps_linear* l, const ps_matrix* dy, co
     const ps_matrix none{nullptr, 0, 0};
     ps_matrix dz = dy ? *dy : none;
     if (act) dz = ps_matrix{base + space.dz, space.dz_row, 0};
+    // x in 8 bits, as it is read: beside dz if that is formed from 8 bits, too
+    const Padded to = padded(*l);
+    ps_matrix xm = x ? *x : none;
+    CodeArgs decode{};
+    uint32_t decode_blocks = 0;
+    if (x8 && want_dw) {
+        xm = ps_matrix{base + space.x, to.in, 0};
+        if (l->rows) decode = decode_args(l->rows, l->in_features, *x8, x_activation, xm, to.in, &decode_blocks);
+    }
     if (act || want_db) {
         SlopeArgs a{};
         a.dy = dy ? dy->data_dev : nullptr;
@@ -629,18 +648,23 @@ ps_status backward(const char* call, const ps_linear* l, const ps_matrix* dy, co
         const int64_t many = (int64_t)l->n_groups * space.parts;
         with_type(l->dtype, [&](auto t) {
             using T = decltype(t);
-            const dim3 grid((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many);
-            if (a.scales)
-                hipLaunchKernelGGL((slope_kernel<T, true>), grid, dim3(256), 0, s, a);
-            else
-                hipLaunchKernelGGL((slope_kernel<T, false>), grid, dim3(256), 0, s, a);
+            dim3 grid((uint32_t)up(l->out_features, SLOPE_COLS), (uint32_t)many);
+            if (a.scales) {
+                uint32_t beside = decode_blocks;
+                if (many + up(decode_blocks, grid.x) > 65535) beside = 0;
+                grid.y += (uint32_t)up(beside, grid.x);
+                hipLaunchKernelGGL((slope_kernel<T, true>), grid, dim3(256), 0, s, a, decode, (uint32_t)many, beside);
+                if (beside) decode_blocks = 0;
+            } else {
+                hipLaunchKernelGGL((slope_kernel<T, false>), grid, dim3(256), 0, s, a, decode, (uint32_t)many, 0u);
+            }
             if (want_db)
                 hipLaunchKernelGGL(bias_sum_kernel<T>, dim3((uint32_t)up(l->out_features, BIAS_COLS), (uint32_t)l->n_groups), dim3(BIAS_COLS * BIAS_SHARES), 0, s, a.partial,
                                    static_cast<T*>(db->data_dev), db->matrix, (int)l->out_features, space.parts);
         });
     }
+    if (decode_blocks) launch_checkpoint_decode(l->dtype, decode, decode_blocks, s);
     float* const partial = reinterpret_cast<float*>(base + space.partial);
-    const Padded to = padded(*l);
     const bool pad_dx = want_dx && space.pad_dx, pad_dw = want_dw && space.pad_dw;
     ps_matrix dzp = dz;
     if ((pad_dx || pad_dw) && !act) dzp = pad(*l, dz, 1, l->rows, l->out_features, l->rows, to.out, base + space.dz, s);
@@ -659,11 +683,6 @@ ps_status backward(const char* call, const ps_linear* l, const ps_matrix* dy, co
         e.out = dw->data_dev;
         e.out_row = dw->row;
         e.out_matrix = dw->matrix;
-        ps_matrix xm = x ? *x : none;
-        if (x8) {
-            xm = ps_matrix{base + space.x, to.in, 0};
-            if (l->rows) launch_checkpoint_decode(l->dtype, l->rows, l->in_features, *x8, x_activation, xm, to.in, s);
-        }
         const bool direct = direct_possible(*l, DW) && aligned16(*l, dz, l->rows, 1) && aligned16(*l, xm, l->rows, 1);
         if (pad_dw)
             run_product(*l, DW, true, true, dzp, x8 ? xm : pad(*l, xm, 1, l->rows, l->in_features, l->rows, to.in, base + space.x, s), e, partial, s);
