@@ -6,7 +6,11 @@ step takes all of them when it is back.
 
 Everything is allocated when the server is made.  The master weights and the two states of every tensor are part of one
 buffer each, a tensor beginning at a multiple of 256 elements (a block of an 8-bit state); a gradient row and a weight version
-have the same layout, so the layers' operators read a version's matrices in place and write gradients where the step reads them."""
+have the same layout, so the layers' operators read a version's matrices in place and write gradients where the step reads them.
+
+With --vocab the inputs are tokens, so many of them (--context) to a row, whose vectors, rows of a table, are the first layer's
+input; with --checkpoint a layer's pre-activations, in 8 bits, are all that is kept for the backward pass, which makes the next layer's input
+from them again."""
 from __future__ import annotations
 
 import argparse
@@ -14,29 +18,36 @@ from typing import List, Optional, Sequence
 
 import torch
 
-from . import dense
+from . import dense, tokens
 
 _ALIGN = dense.ADAMW_BLOCK
 
 
 class MlpServer:
     """widths: features of the input, of every hidden layer (with `activation`) and the logits.  The master weights are fp32, versions and
-    gradients of `dtype`.  capacity: gradients that the buffer holds."""
+    gradients of `dtype`.  capacity: gradients that the buffer holds.  vocab: the inputs are rows of `context` tokens (0 .. vocab - 1; others
+    are padding), a vector of widths[0] / context features for each.  checkpoint: what the backward pass needs is kept in 8 bits."""
 
     def __init__(self, widths: Sequence[int], n_versions: int, capacity: int, dtype=torch.bfloat16, activation: str = "gelu",
-                 state_bits: int = 8, weight_decay: float = 0.01, seed: int = 0, device: str = "cuda:0"):
+                 state_bits: int = 8, weight_decay: float = 0.01, seed: int = 0, device: str = "cuda:0", vocab: int = 0, context: int = 1,
+                 checkpoint: bool = False):
         if len(widths) < 2 or min(widths) < 1:
             raise ValueError("widths: at least an input and an output, each with a feature or more")
         if n_versions < 1 or capacity < 1:
             raise ValueError("at least one version and room for one gradient")
         if activation not in dense.ACTIVATIONS:
             raise ValueError(f"unknown activation {activation!r}")
-        self.shapes, self.at, total = [], [], 0
+        if vocab < 0 or context < 1 or (vocab and widths[0] % context):
+            raise ValueError("vocab: none or some tokens; widths[0]: as many features for each token of a row")
+        self.vocab, self.context, self.checkpoint = vocab, context, checkpoint
+        self.shapes = [(vocab, widths[0] // context)] if vocab else []
+        self.layers = len(self.shapes)  # number of the first layer's weights
         for fin, fout in zip(widths, widths[1:]):
-            for shape in ((fout, fin), (fout,)):
-                self.shapes.append(shape)
-                self.at.append(total)
-                total += -(-shape[0] * (fin if len(shape) == 2 else 1) // _ALIGN) * _ALIGN
+            self.shapes += [(fout, fin), (fout,)]
+        self.at, total = [], 0
+        for i in range(len(self.shapes)):
+            self.at.append(total)
+            total += -(-self._numel(i) // _ALIGN) * _ALIGN
         self.widths, self.activation, self.n_versions, self.capacity, self.pending, self.steps = list(widths), activation, n_versions, capacity, 0, 0
         self.master = torch.zeros(total, device=device)
         self.fresh = torch.zeros(total, dtype=dtype, device=device)  # the master weights, rounded: what a pull copies
@@ -70,14 +81,21 @@ class MlpServer:
 
     def forward(self, x, offsets, version_of_worker):
         """Logits [rows, out] of the workers' rows (worker g has rows offsets[g] .. offsets[g + 1] - 1 and reads version
-        version_of_worker[g]), and what `backward` needs."""
-        parts, kept, n = self._parts(self.versions), [], len(self.widths) - 1
+        version_of_worker[g]), and what `backward` needs.  x: [rows, features], or tokens [rows, context] of int32 or int64."""
+        parts, kept, n, at = self._parts(self.versions), [], len(self.widths) - 1, self.layers
+        if self.vocab:
+            kept.append(x)
+            dim = self.shapes[0][1]
+            x = tokens.ps_grouped_embedding_forward(x.reshape(-1), offsets * self.context, parts[0], dim ** 0.5, version_of_worker).view(x.shape[0], self.widths[0])
+        held = dense.ps_checkpoint_encode(x) if self.checkpoint else x
         for i in range(n):
-            hidden = i + 1 < n
-            pre = torch.empty(x.shape[0], self.widths[i + 1], dtype=x.dtype, device=x.device) if hidden else None
-            y = dense.ps_grouped_linear_forward(x, offsets, parts[2 * i], parts[2 * i + 1], None, self.activation if hidden else "none", version_of_worker, pre=pre)
-            kept.append((x, pre))
-            x = y
+            pre = None
+            if i + 1 < n:
+                shape = x.shape[0], self.widths[i + 1]
+                pre = dense.ps_checkpoint_empty(*shape, x.device) if self.checkpoint else torch.empty(shape, dtype=x.dtype, device=x.device)
+            x = dense.ps_grouped_linear_forward(x, offsets, parts[at + 2 * i], parts[at + 2 * i + 1], None, "none" if pre is None else self.activation, version_of_worker, pre=pre)
+            kept.append((held, pre))
+            held = pre if self.checkpoint else x
         return x, kept
 
     def backward(self, dlogits, kept, offsets, version_of_worker) -> range:
@@ -86,11 +104,16 @@ class MlpServer:
         if self.pending + workers > self.capacity:
             raise RuntimeError(f"the buffer holds {self.capacity} gradients, {self.pending} are pending and {workers} came")
         rows = range(self.pending, self.pending + workers)
-        weights, grads, dy = self._parts(self.versions), self._parts(self.queue[rows.start:rows.stop]), dlogits
-        for i in reversed(range(len(kept))):
-            x, pre = kept[i]
-            dy, _, _ = dense.ps_grouped_linear_backward(dy, x, offsets, weights[2 * i], "none" if pre is None else self.activation, pre, version_of_worker,
-                                                        need_dx=i > 0, dw=grads[2 * i], db=grads[2 * i + 1])
+        weights, grads, dy, at = self._parts(self.versions), self._parts(self.queue[rows.start:rows.stop]), dlogits, self.layers
+        layers = kept[1:] if self.vocab else kept
+        for i in reversed(range(len(layers))):
+            x, pre = layers[i]
+            dy, _, _ = dense.ps_grouped_linear_backward(dy, x, offsets, weights[at + 2 * i], "none" if pre is None else self.activation, pre, version_of_worker,
+                                                        need_dx=i > 0 or self.vocab > 0, dw=grads[at + 2 * i], db=grads[at + 2 * i + 1],
+                                                        x_activation=self.activation if self.checkpoint and i else "none")
+        if self.vocab:
+            dim = self.shapes[0][1]
+            tokens.ps_grouped_embedding_backward(dy.view(-1, dim), kept[0].reshape(-1), offsets * self.context, self.vocab, dim ** 0.5, dtable=grads[0])
         self.pending = rows.stop
         return rows
 
@@ -100,12 +123,10 @@ class MlpServer:
         logits, kept = self.forward(x, offsets, version_of_worker)
         size = (offsets[1:] - offsets[:-1]).long()
         worker = torch.repeat_interleave(torch.arange(workers, device=x.device), size, output_size=x.shape[0])
-        log_p = torch.log_softmax(logits.float(), 1)
-        dlogits = log_p.exp()
-        dlogits.scatter_add_(1, labels[:, None], torch.full_like(dlogits[:, :1], -1.0))
-        self.backward((dlogits / size[worker][:, None]).to(x.dtype), kept, offsets, version_of_worker)
-        of_row = -log_p.gather(1, labels[:, None]).squeeze(1)
-        return torch.zeros(workers, device=x.device).index_add_(0, worker, of_row) / size.clamp(min=1)
+        p = tokens.ps_logprob_forward(logits, labels)
+        dlogits = tokens.ps_logprob_backward(logits, labels, p.norm, (-1.0 / size)[worker], out=logits)
+        self.backward(dlogits, kept, offsets, version_of_worker)
+        return torch.zeros(workers, device=x.device).index_add_(0, worker, -p.logp) / size.clamp(min=1)
 
     def apply(self, lr: float, mean: bool = True) -> int:
         """One AdamW step with the sum (or mean) of all pending gradients, which leaves the buffer empty; returns how many there were."""
@@ -121,22 +142,30 @@ class MlpServer:
 
 
 def train(rounds: int = 60, down: Optional[range] = None, workers: int = 16, batch: int = 64, widths: Sequence[int] = (256, 512, 512, 10),
-          state_bits: int = 8, lr: float = 2e-3, seed: int = 1, dtype=torch.bfloat16, say=None) -> List[float]:
+          state_bits: int = 8, lr: float = 2e-3, seed: int = 1, dtype=torch.bfloat16, say=None, vocab: int = 0, context: int = 8,
+          checkpoint: bool = False) -> List[float]:
     """Workers learn a random teacher's labels; worker g pulls every (g % 4 + 1)-th round, as far as the server is there
-    (it is not in the rounds of `down`).  Returns the mean loss of every round."""
+    (it is not in the rounds of `down`).  With `vocab` the inputs are `context` random tokens, each of which the teacher gives points to
+    every class.  Returns the mean loss of every round."""
     down = range(rounds // 2, rounds // 2 + 8) if down is None else down
-    server = MlpServer(widths, 4, workers * (len(down) + 1), dtype, state_bits=state_bits, seed=seed)
+    server = MlpServer(widths, 4, workers * (len(down) + 1), dtype, state_bits=state_bits, seed=seed, vocab=vocab, context=context if vocab else 1,
+                       checkpoint=checkpoint)
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    teacher = torch.randn(widths[0], widths[-1], device="cuda", generator=gen)
+    teacher = torch.randn(vocab or widths[0], widths[-1], device="cuda", generator=gen)
     # ragged minibatches: batch, one less, two less, .. rows, and again
     sizes = [max(1, batch - g % 4) for g in range(workers)]
     offsets = torch.tensor([sum(sizes[:g]) for g in range(workers + 1)], dtype=torch.int32).cuda()
     version = torch.tensor([g % 4 for g in range(workers)], dtype=torch.int32).cuda()
     losses = []
     for r in range(rounds):
-        x = torch.randn(sum(sizes), widths[0], device="cuda", generator=gen)
-        loss = server.work(x.to(dtype), (x @ teacher).argmax(1), offsets, version)
+        if vocab:
+            x = torch.randint(0, vocab, (sum(sizes), context), device="cuda", generator=gen)
+            labels = teacher[x].sum(1).argmax(1)
+        else:
+            x = torch.randn(sum(sizes), widths[0], device="cuda", generator=gen)
+            x, labels = x.to(dtype), (x @ teacher).argmax(1)
+        loss = server.work(x, labels, offsets, version)
         losses.append(loss.mean())
         if r not in down:
             n = server.apply(lr)
@@ -158,8 +187,12 @@ def main() -> None:
     p.add_argument("--batch", type=int, default=64)
     p.add_argument("--widths", type=int, nargs="+", default=[256, 512, 512, 10])
     p.add_argument("--state-bits", type=int, choices=[8, 32], default=8)
+    p.add_argument("--vocab", type=int, default=0, help="inputs are tokens, so many different ones")
+    p.add_argument("--context", type=int, default=8, help="tokens of a row")
+    p.add_argument("--checkpoint", action="store_true", help="keep activations in 8 bits for the backward pass")
     a = p.parse_args()
-    train(a.rounds, workers=a.workers, batch=a.batch, widths=a.widths, state_bits=a.state_bits, say=lambda m: print(m, flush=True))
+    train(a.rounds, workers=a.workers, batch=a.batch, widths=a.widths, state_bits=a.state_bits, say=lambda m: print(m, flush=True), vocab=a.vocab,
+          context=a.context, checkpoint=a.checkpoint)
 
 
 if __name__ == "__main__":

@@ -39,7 +39,7 @@ def encode64(x):
     code = torch.where((code == 0) & (a > 0), 1, code)
     code = torch.where(v.isfinite(), code, 127)
     code = code + 128 * (torch.signbit(v) & v.isfinite())
-    return code.view(rows, -1)[:, :cols].to(torch.uint8), (scale + 127).to(torch.uint8)
+    return code.view(rows, blocks * 32)[:, :cols].to(torch.uint8), (scale + 127).to(torch.uint8)
 
 
 def bits(c):
