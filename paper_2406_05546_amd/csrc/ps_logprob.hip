@@ -173,18 +173,25 @@ __device__ __forceinline__ void meet_all()
         __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront in order
 }
 
-// The k-th largest of the lanes' values, its lower 16 bits left out: reached by as many.  For a whole wavefront.
+// The k-th largest of the lanes' values (with more than four wavefronts, of the largest of four lanes each), its lower 16 bits left out:
+// reached by as many.  For a whole wavefront.
 template <int WAVES>
 __device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k)
 {
-    uint32_t o[WAVES], least = 0;
+    constexpr int EACH = WAVES < 4 ? WAVES : 4;
+    uint32_t o[EACH], least = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) o[i] = ordered(high[i * 64 + (threadIdx.x & 63)]);
+    for (int i = 0; i < EACH; ++i) {
+        float v = high[i * 64 + (threadIdx.x & 63)];
+#pragma unroll
+        for (int w = i + EACH; w < WAVES; w += EACH) v = fmaxf(v, high[w * 64 + (threadIdx.x & 63)]);
+        o[i] = ordered(v);
+    }
     for (int b = 31; b >= 16; --b) {
         const uint32_t more = least | 1u << b;
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) n += __popcll(__ballot(o[i] >= more));
+        for (int i = 0; i < EACH; ++i) n += __popcll(__ballot(o[i] >= more));
         if (n >= k) least = more;
     }
     return least;
@@ -316,12 +323,12 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
 // one is worked on.  Where rows are few, parts of them are blocks of their own, and join_parts_kernel finishes.  Bound by memory; behind it by
 // the vector ALU: about ten operations and an exponential for a value.
 template <class T, int WAVES, bool TOP>
-__global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
+__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprob_kernel(ForwardArgs a)
 {
-    constexpr int E = 16 / sizeof(T), ROWS = 4 / WAVES;  // rows of a block
+    constexpr int E = 16 / sizeof(T), ROWS = WAVES < 4 ? 4 / WAVES : 1;  // rows of a block
     constexpr int EACH = 64 * VECTORS;                   // vectors of a wavefront in a round, 64 of each 64 * WAVES
     __shared__ Scratch<WAVES> scratch[TOP ? ROWS : 1];
-    __shared__ Sums meet[4];
+    __shared__ Sums meet[ROWS * WAVES];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), w = wave % WAVES, of = wave / WAVES;
     const float c = a.scale * LOG2E;
     const int64_t total = a.rows * a.parts;
@@ -394,8 +401,10 @@ __global__ __launch_bounds__(256) void logprob_kernel(ForwardArgs a)
             if (lane == 0) meet[wave] = sums;
             __syncthreads();
             sums = meet[0];
+            if (w == 0) {
 #pragma unroll
-            for (int k = 1; k < WAVES; ++k) sums = join(sums, meet[k], c);
+                for (int k = 1; k < WAVES; ++k) sums = join(sums, meet[k], c);
+            }
         }
         if (there && w == 0) {
             if (a.parts > 1) {
@@ -562,6 +571,10 @@ ps_status check_numbers(const char* call, const char* name, const void* p, int64
     return PS_OK;
 }
 
+// Whether sixteen wavefronts take a row: where there is a compute unit for each row, which takes 64 k values in about the time of a second
+// launch (256 rows of 50257 in bf16 with 5 alternatives 20.8 us in parts, 15.4 this way; one of 131072 with 20 17.3 and 17.3, alone 33 and 37).
+bool sixteen(const ps_logprob& l) { return l.rows <= COMPUTE_UNITS && l.vocab <= 65536; }
+
 // Parts of a row, so many rounds of four wavefronts each: as many as make eight blocks for a compute unit of all rows, one where
 // there are as many rows.
 struct Cut {
@@ -569,6 +582,7 @@ struct Cut {
 };
 Cut cut_rows(const ps_logprob& l)
 {
+    if (sixteen(l)) return {1, 0};
     const int64_t round = 4 * 64 * VECTORS * 16 / dtype_size(l.dtype), rounds = (l.vocab + round - 1) / round;  // (a part more for what is ahead of a row)
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, MOST_PARTS), l.rows ? 8 * COMPUTE_UNITS / l.rows : 1));
     const int64_t each = (rounds + parts - 1) / parts;
@@ -583,6 +597,10 @@ void start_forward(const ForwardArgs& a, hipStream_t s)
     const int64_t most = 1 << 20;
     if (a.vocab <= ROUND) {
         hipLaunchKernelGGL((logprob_kernel<T, 1, TOP>), dim3((uint32_t)std::min((a.rows + 3) / 4, most)), dim3(256), 0, s, a);
+        return;
+    }
+    if (a.part_rounds == 0) {
+        hipLaunchKernelGGL((logprob_kernel<T, 16, TOP>), dim3((uint32_t)a.rows), dim3(1024), 0, s, a);
         return;
     }
     hipLaunchKernelGGL((logprob_kernel<T, 4, TOP>), dim3((uint32_t)std::min(a.rows * a.parts, most)), dim3(256), 0, s, a);

@@ -151,7 +151,7 @@ def test_forward(tk, dtype, kind):
 def test_many_rows_and_long_ones(tk, dtype):
     import torch
     t = getattr(torch, dtype)
-    for rows, vocab, top in ((600, 9001, 5), (2050, 300, 3), (1, 131072, 20), (2, 300007, 32), (5000, 10, 0)):
+    for rows, vocab, top in ((600, 9001, 5), (2050, 300, 3), (1, 131072, 20), (2, 300007, 32), (5000, 10, 0), (256, 60001, 7), (257, 60001, 7), (3, 1500000, 32)):
         g = gen(rows)
         z = (torch.randn(rows, vocab, device="cuda", generator=g) * 2).to(t)
         check_forward(tk, z, torch.randint(0, vocab, (rows,), device="cuda", generator=g), 1.0, top)

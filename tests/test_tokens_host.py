@@ -155,11 +155,12 @@ def test_workspace_of_log_probabilities():
         assert lib().ps_logprob_workspace_bytes(ctypes.byref(logprob(**kw)), ctypes.byref(n)) == ps.PS_OK
         return n.value
     assert need() == 0 and need(rows=0, vocab=1 << 20) == 0 and need(rows=1 << 14, vocab=1 << 20) == 0
-    # one long row: parts of 8192 logits, three sums and the alternatives of each
-    assert need(rows=1, vocab=65536) == 256 and need(rows=1, vocab=65536, top=5) == 256 + 8 * 5 * 8
-    long = logprob(rows=1, vocab=65536, top=5)
-    logits = dense.ps_matrix(SOMEWHERE, 65536, 0)
-    assert score(long, logits=logits, size=256 + 319) == ps.PS_ENOMEM
+    # a row that one block takes, and a longer one: parts of 8192 logits, three sums and the alternatives of each
+    assert need(rows=1, vocab=1 << 16, top=5) == 0
+    assert need(rows=1, vocab=1 << 18) == 512 and need(rows=1, vocab=1 << 18, top=5) == 512 + 32 * 5 * 8
+    long = logprob(rows=1, vocab=1 << 18, top=5)
+    logits = dense.ps_matrix(SOMEWHERE, 1 << 18, 0)
+    assert score(long, logits=logits, size=512 + 32 * 5 * 8 - 1) == ps.PS_ENOMEM
     assert score(long, logits=logits, ws=None) == ps.PS_EINVAL and score(long, logits=logits, ws=SOMEWHERE + 8) == ps.PS_EINVAL
     assert lib().ps_logprob_workspace_bytes(ctypes.byref(long), None) == ps.PS_EINVAL
     assert lib().ps_logprob_workspace_bytes(ctypes.byref(logprob(top=33)), None) == ps.PS_EINVAL
