@@ -88,8 +88,9 @@ PS_API ps_status ps_linear_backward(const ps_linear* layer, const ps_matrix* dy,
  * each, as float8_e4m3fn) at codes_dev[r * row + c], scales powers of two (one byte s each for 2^(s - 127), as float8_e8m0fnu,
  * 1 .. 254) at scales_dev[r * scale_row + b]; strides in bytes, any alignment.  Encoding takes the smallest scale from 2^-126
  * on with which the block's largest finite magnitude is at most 448 and rounds to the nearest code, ties to even; but what
- * is not 0 becomes the least code of its sign at the lowest (so a ReLU passes its gradient where it did), and what is not
- * finite becomes NaN, the block's other values staying what they are. */
+ * is not 0 becomes the least code of its sign at the lowest (so a ReLU passes its gradient where it did), what would be rounded
+ * beyond the largest number of x's type becomes the code below, and what is not finite becomes NaN, the block's other values
+ * staying what they are. */
 typedef struct {
     void *codes_dev, *scales_dev;
     int64_t row, scale_row;

@@ -42,14 +42,14 @@ typedef struct {
 typedef struct {
     int32_t dtype; /* ps_dtype of table, rows and gradients */
     int32_t n_groups, n_tables;
-    int64_t rows, vocab, dim; /* n_groups * vocab < 2^31 */
+    int64_t rows, vocab, dim; /* backward: n_groups * vocab < 2^31 */
     const int32_t* offsets_dev;
     const int32_t* table_of_group_dev;
     double scale; /* finite; taken to 32 bits */
 } ps_embedding;
 
 /* out[r] [dim] = scale * table[token of r] [dim], the product rounded once; a row without a token is 0.  Rows in no group
- * are left as they are.  table [n_tables][vocab][dim], out [rows][dim]. */
+ * are left as they are.  table [n_tables][vocab][dim], out [rows][dim], which may not overlap. */
 PS_API ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens* tokens, const ps_matrix* table, const ps_matrix* out,
                                       void* hip_stream);
 

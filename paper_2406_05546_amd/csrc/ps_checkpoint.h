@@ -22,11 +22,17 @@ __device__ __forceinline__ uint32_t largest_of_quad(uint32_t v)
 __device__ __forceinline__ int checkpoint_scale(uint32_t top) { return max((int)((top + 0x1fffffu) >> 23) - 8, 1); }
 __device__ __forceinline__ float inverse_of_scale(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 
-// The codes of a lane's eight values and the block's scale (2^(scale - 127)).  Columns that are not there are 0.
+// A block's largest magnitudes that would be rounded beyond T's largest number (from 248 * 2^8 on to 2^16 in fp16, from 248 * 2^120 on to 2^128
+// in the others) are held as 240 times the scale, which is within half a step, too.
+template <class T>
+constexpr uint32_t CHECKPOINT_LARGE = __is_same(T, f16_t) ? 0x47780000u : 0x7f780000u;  // the bits of those
+
+// The codes of a lane's eight values of type T and the block's scale (2^(scale - 127)).  Columns that are not there are 0.
 //
-// Most values need a product and a conversion.  Those that do not, values that are not finite, or 0, or so small that their code would be 0, are
-// looked for in the largest and smallest magnitudes, and a wavefront that has one takes the way that looks at each value: in the
+// Most values need a product and a conversion.  Others, those that are not finite, or 0, or so small that their code would be 0, or as large as
+// above, are looked for in the largest and smallest magnitudes, and a wavefront that has one takes the way that looks at each value: in the
 // layers' kernels, whose last steps are bound by their instructions (8192 rows 2048 -> 8192 with GELU 285 us, 310 where every value is looked at).
+template <class T>
 __device__ __forceinline__ uint32_t checkpoint_encode(const float (&v)[8], uint32_t (&code)[2])
 {
     uint32_t top = 0, low = ~0u;
@@ -39,7 +45,7 @@ __device__ __forceinline__ uint32_t checkpoint_encode(const float (&v)[8], uint3
     top = largest_of_quad(top);
     int scale = checkpoint_scale(top);
     float inverse = inverse_of_scale(scale), x[8];
-    if (__ballot(top >= 0x7f800000u || __uint_as_float(low) * inverse < 0x1p-9f)) {
+    if (__ballot(top >= CHECKPOINT_LARGE<T> || __uint_as_float(low) * inverse < 0x1p-9f)) {
         top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -49,11 +55,12 @@ __device__ __forceinline__ uint32_t checkpoint_encode(const float (&v)[8], uint3
         top = largest_of_quad(top);
         scale = checkpoint_scale(top);
         inverse = inverse_of_scale(scale);
+        const float most = top >= CHECKPOINT_LARGE<T> ? 240.f : 448.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // what is not 0 is not held as 0: at least 2^-9, the least code; what is not finite as NaN
-            const float least = copysignf(fmaxf(fabsf(v[i] * inverse), 0x1p-9f), v[i]);
-            x[i] = v[i] == 0.f ? v[i] : (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u ? least : __uint_as_float(0x7fc00000u);
+            const float held = copysignf(fminf(fmaxf(fabsf(v[i] * inverse), 0x1p-9f), most), v[i]);
+            x[i] = v[i] == 0.f ? v[i] : (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u ? held : __uint_as_float(0x7fc00000u);
         }
     } else {
 #pragma unroll
@@ -108,10 +115,11 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int n, const uint32_t (&
 
 // Eight columns from `col` (a multiple of 8) of a row, of which `valid` exist: their codes, and once for a block its scale.  Every lane of a
 // quad calls this.
+template <class T>
 __device__ __forceinline__ void checkpoint_store(uint8_t* codes, uint8_t* scales, int col, int valid, const float (&v)[8])
 {
     uint32_t code[2];
-    const uint32_t scale = checkpoint_encode(v, code);
+    const uint32_t scale = checkpoint_encode<T>(v, code);
     if (valid <= 0) return;
     store_codes(codes + col, valid, code);
     if (col % PS_CHECKPOINT_BLOCK == 0) scales[col / PS_CHECKPOINT_BLOCK] = (uint8_t)scale;

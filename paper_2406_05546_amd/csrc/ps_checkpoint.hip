@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
                 }
                 // (all four lanes of a block are there or none is: pieces are whole blocks)
                 const bool there = at + i * 256 < items && (!a.groups.offsets || inside[p[i].row - first]);
-                checkpoint_store(a.codes + p[i].row * a.row, a.scales + p[i].row * a.scale_row, p[i].col, there ? p[i].n : 0, v);
+                checkpoint_store<T>(a.codes + p[i].row * a.row, a.scales + p[i].row * a.scale_row, p[i].col, there ? p[i].n : 0, v);
             }
         }
         if (a.groups.offsets) __syncthreads();  // inside is written again

@@ -518,7 +518,7 @@ ps_status check_embedding(const char* call, const ps_embedding* e, bool forward)
         return dense_fail(PS_EINVAL, "%s: vocab or dim outside 1 .. %d", call, PS_DENSE_MAX_STRIDE);
     if (e->n_groups < 1 || e->n_groups > PS_DENSE_MAX_GROUPS) return dense_fail(PS_EINVAL, "%s: groups outside 1 .. %d", call, PS_DENSE_MAX_GROUPS);
     if (!e->offsets_dev && e->n_groups != 1) return dense_fail(PS_EINVAL, "%s: several groups need offsets", call);
-    if (e->n_groups * e->vocab > INT32_MAX) return dense_fail(PS_EINVAL, "%s: groups times vocab from 2^31 on", call);
+    if (!forward && e->n_groups * e->vocab > INT32_MAX) return dense_fail(PS_EINVAL, "%s: groups times vocab from 2^31 on", call);
     if (forward && (e->n_tables < 1 || (!e->table_of_group_dev && e->n_tables < e->n_groups)))
         return dense_fail(PS_EINVAL, "%s: fewer tables than groups, and no list of which each uses", call);
     if ((reinterpret_cast<uintptr_t>(e->offsets_dev) & 3) || (forward && (reinterpret_cast<uintptr_t>(e->table_of_group_dev) & 3)))

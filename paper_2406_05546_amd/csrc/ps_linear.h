@@ -506,7 +506,7 @@ __device__ __forceinline__ void keep(const Epilogue& e, const float (&bias)[8], 
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = i < valid ? z[i] : 0.f;
     }
-    checkpoint_store(e.codes + row * e.codes_row, e.scales + row * e.scales_row, col, valid, z);
+    checkpoint_store<T>(e.codes + row * e.codes_row, e.scales + row * e.scales_row, col, valid, z);
 }
 template <class T, bool RESIDUAL, int N>
 __device__ __forceinline__ void finish(const Epilogue& e, const float (&bias)[N], const float (&residual)[N], int64_t row, int col, int valid, float (&v)[N])

@@ -37,6 +37,8 @@ def encode64(x):
     up, down = table[hi] - finite, finite - table[lo]
     code = torch.where((down < up) | ((down == up) & (lo % 2 == 0)), lo, hi)
     code = torch.where((code == 0) & (a > 0), 1, code)
+    beyond = table[code] * torch.exp2(scale.double())[:, :, None] > torch.finfo(x.dtype if x.dtype != torch.float64 else torch.float32).max
+    code = torch.where(beyond, code - 1, code)
     code = torch.where(v.isfinite(), code, 127)
     code = code + 128 * (torch.signbit(v) & v.isfinite())
     return code.view(rows, blocks * 32)[:, :cols].to(torch.uint8), (scale + 127).to(torch.uint8)
@@ -119,6 +121,22 @@ def test_decode_with_an_activation(dense, act):
         assert bool(((y.double() - want).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_largest_numbers_stay_finite(dense, dtype):
+    import torch
+    t = getattr(torch, dtype)
+    top = torch.finfo(t).max
+    x = (torch.tensor([1.0, -1.0, 0.999, 0.97, 0.96875, 0.968, 0.9375, 0.5, 1e-4, 0.0], device="cuda", dtype=torch.float64) * top).to(t).repeat(3, 7)
+    c = dense.ps_checkpoint_encode(x)
+    check_encode(c, x)
+    y = dense.ps_checkpoint_decode(c, t)
+    assert bool(y.isfinite().all()) and bool(((y.double() - x.double()).abs() <= x.double().abs() / 16 + top * 2.0 ** -16).all())
+    # beside what is not finite, too
+    x[:, ::9] = INF
+    y = dense.ps_checkpoint_decode(dense.ps_checkpoint_encode(x), t)
+    assert torch.equal(y.isfinite(), x.isfinite())
+
+
 def test_rows_apart_and_at_any_place(dense):
     import torch
     for dtype in TYPES:
@@ -166,6 +184,28 @@ def test_forward_keeps_what_it_would_write(dense, dtype, rows, fin, fout):
         assert torch.equal(y, y8), act
         want = dense.ps_checkpoint_encode(pre)
         assert all(torch.equal(a, b) for a, b in zip(bits(kept), bits(want))), act
+
+
+def test_layers_with_checkpoints_of_any_rows(dense):
+    """Codes and scales that are parts of wider rows, at any place."""
+    import torch
+    for t in (torch.float32, torch.bfloat16):
+        for rows, fin, fout in ((5, 40, 72), (300, 104, 264), (290, 33, 65)):
+            g = gen(rows)
+            x, w, dy = randn(g, t, rows, fin), randn(g, t, fout, fin), randn(g, t, rows, fout)
+
+            def wide(cols):
+                codes, scales = torch.full((rows, cols + 7), 77, device="cuda", dtype=torch.uint8), torch.full((rows, cols // 32 + 4), 99, device="cuda", dtype=torch.uint8)
+                return codes, scales, dense.Checkpoint(codes[:, 3:cols + 3], scales[:, 1:(cols + 31) // 32 + 1])
+            codes, scales, pre = wide(fout)
+            dense.ps_linear_forward(x, w, activation="gelu", pre=pre)
+            plain = dense.ps_checkpoint_empty(rows, fout, "cuda:0")
+            dense.ps_linear_forward(x, w, activation="gelu", pre=plain)
+            assert all(torch.equal(a, b) for a, b in zip(bits(pre), bits(plain)))
+            assert bool((codes[:, :3] == 77).all()) and bool((codes[:, fout + 3:] == 77).all()) and bool((scales[:, 0] == 99).all()) and bool((scales[:, (fout + 31) // 32 + 1:] == 99).all())
+            x8 = dense.ps_checkpoint_encode(x, wide(fin)[2])
+            got, want = dense.ps_linear_backward(dy, x8, w, "gelu", pre=pre), dense.ps_linear_backward(dy, dense.ps_checkpoint_encode(x), w, "gelu", pre=plain)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 @pytest.mark.parametrize("dtype", TYPES)

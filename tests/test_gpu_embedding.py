@@ -183,6 +183,41 @@ def test_gradient_in_groups(tk, rows, vocab, dim, groups):
         assert torch.equal(alone, got[k])
 
 
+@pytest.mark.parametrize("rows,vocab,dim,gap", [(40, 30, 5, 3), (40, 30, 1, 1), (100, 70, 300, 12), (20, 9, 40000, 5), (17000, 50, 24, 40)])
+def test_gradient_in_rows_apart(tk, rows, vocab, dim, gap):
+    """Lines shorter and longer than what a block clears, between others that stay as they are."""
+    import torch
+    for dtype in TYPES:
+        t, g = getattr(torch, dtype), gen(rows + dim)
+        dy, tok = torch.randn(rows, dim, device="cuda", generator=g).to(t), some_tokens("spread", rows, vocab, g)
+        cuts = [0, rows // 3, rows]
+        wide = torch.full((2, vocab + 1, dim + gap), 6.0, device="cuda", dtype=t)
+        out = wide[:, :vocab, 1:dim + 1]
+        tk.ps_grouped_embedding_backward(dy, tok, torch.tensor(cuts, dtype=torch.int32).cuda(), vocab, 0.5, dtable=out)
+        want, off = gradient64(dy.cpu(), tok.cpu(), vocab, 0.5, owner_of(rows, cuts), 2)
+        close(out.cpu(), want, off, "gradient")
+        out.fill_(6.0)
+        assert bool((wide == 6).all())
+
+
+def test_many_groups_that_begin_at_a_row(tk):
+    """Hundreds of empty groups between rows, and more groups than one look takes."""
+    import torch
+    g, rows, groups = gen(4), 150, 5000
+    cuts = sorted(torch.randint(0, 10, (groups + 1,), generator=torch.Generator().manual_seed(1)).tolist())
+    cuts[-700:] = sorted(torch.randint(10, rows, (700,), generator=torch.Generator().manual_seed(2)).tolist())
+    offsets, index = torch.tensor(cuts, dtype=torch.int32).cuda(), (torch.arange(groups) % 7).to(torch.int32)
+    table, tok = torch.randn(7, 20, 12, device="cuda", generator=g), torch.randint(0, 20, (rows,), device="cuda", generator=g)
+    out = torch.zeros(rows, 12, device="cuda")
+    tk.ps_grouped_embedding_forward(tok, offsets, table, 1.0, index.cuda(), out=out)
+    owner = owner_of(rows, cuts)
+    assert torch.equal(out.cpu().double(), look64(tok.cpu(), table.cpu(), 1.0, owner, index.tolist(), torch.zeros(rows, 12)))
+    dy = torch.randn(rows, 3, device="cuda", generator=g)
+    got = tk.ps_grouped_embedding_backward(dy, tok, offsets, 20)
+    want, off = gradient64(dy.cpu(), tok.cpu(), 20, 1.0, owner, groups)
+    close(got.cpu(), want, off, "gradients")
+
+
 def test_offsets_of_any_contents_stay_inside(tk):
     import torch
     g = gen(3)
