@@ -12,7 +12,7 @@
 namespace ps {
 namespace {
 
-int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
 
@@ -135,54 +135,79 @@ __device__ __forceinline__ void clear_block(const ClearArgs& a, uint32_t block)
     }
 }
 
-// Up to RANK_MOST rows: a row's place is the number of keys below its own, and of equal ones before it, which is counted.  Wavefronts compare
-// the keys of their RANK_ROWS rows with RANK_KEYS others, 32-bit comparisons of which the chip does 1.9e13 in a second (16384 rows:
-// 14 us); next to them the table is cleared, which is bound by memory and takes longer for all but small ones.
-constexpr int RANK_ROWS = 256, RANK_KEYS = 1024, RANK_MOST = 16384;
+// Up to RANK_MOST rows: a row's place is the number of keys below its own, and of equal ones before it, which is counted.  A block compares
+// the keys of RANK_ROWS rows, RANK_EACH to a thread, with RANK_KEYS others, which it reads from LDS, four at a time and the same for all
+// lanes; two rows to a thread, so that the comparisons and not these reads are what takes time.  K: keys below 2^24 are compared as floats,
+// whose difference, taken into 0 .. 1 as it is formed, is what is counted (two instructions; an integer comparison has to wait for its
+// result to be added).  16384 rows alone: 27 us with one row and integers, 24 with two, 19 with floats.  Next to them the table is
+// cleared, which is bound by memory.
+constexpr int RANK_THREADS = 256, RANK_EACH = 2, RANK_ROWS = RANK_THREADS * RANK_EACH, RANK_KEYS = 512, RANK_MOST = 16384;
 
-template <class TOKEN>
-__global__ __launch_bounds__(RANK_ROWS) void rank_and_clear_kernel(SortArgs a, uint32_t rank_blocks, int parts, uint32_t* __restrict__ keys, uint16_t* __restrict__ counts, ClearArgs clear)
+__device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) { return a < b; }
+__device__ __forceinline__ float less(float a, float b) { return __builtin_amdgcn_fmed3f(b - a, 0.f, 1.f); }  // whole numbers
+
+template <class TOKEN, class K>
+__global__ __launch_bounds__(RANK_THREADS) void rank_and_clear_kernel(SortArgs a, uint32_t rank_blocks, int parts, uint32_t* __restrict__ keys, uint16_t* __restrict__ counts, ClearArgs clear)
 {
     if (blockIdx.x >= rank_blocks) {
         clear_block(clear, blockIdx.x - rank_blocks);
         return;
     }
-    __shared__ __attribute__((aligned(16))) uint32_t others[RANK_KEYS];
-    const int part = blockIdx.x % parts, r = blockIdx.x / parts * RANK_ROWS + threadIdx.x, first = part * RANK_KEYS;
-    uint32_t there[RANK_KEYS / RANK_ROWS];
+    typedef K Four __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) K others[RANK_KEYS];
+    const int part = blockIdx.x % parts, first = part * RANK_KEYS, lane = threadIdx.x & 63;
+    const int row0 = blockIdx.x / parts * RANK_ROWS + scalar(threadIdx.x & ~63);  // of this wavefront's first 64; the next are RANK_THREADS behind
+    uint32_t there[RANK_KEYS / RANK_THREADS], key[RANK_EACH];
+    K n[RANK_EACH] = {};
 #pragma unroll
-    for (int i = 0; i < RANK_KEYS / RANK_ROWS; ++i) {
-        there[i] = key_of_row<TOKEN>(a, scalar(first + i * RANK_ROWS + (threadIdx.x & ~63)), ~0u);  // (above every key)
+    for (int i = 0; i < RANK_KEYS / RANK_THREADS; ++i) there[i] = key_of_row<TOKEN>(a, first + i * RANK_THREADS + scalar(threadIdx.x & ~63), ~0u);  // (above every key)
+#pragma unroll
+    for (int q = 0; q < RANK_EACH; ++q) key[q] = key_of_row<TOKEN>(a, row0 + q * RANK_THREADS, a.none);
+#pragma unroll
+    for (int i = 0; i < RANK_KEYS / RANK_THREADS; ++i) others[i * RANK_THREADS + threadIdx.x] = (K)there[i];
+    __syncthreads();
+    if (row0 >= a.rows) return;
+    // 64 keys at a time: those of rows before count where they are equal, too, those of rows behind only where they are below, and of the same
+    // 64 rows' the equal ones before are added
+    const int many = min(RANK_KEYS, a.rows - first);
+    for (int k0 = 0; k0 < many; k0 += 64) {
+        K below[RANK_EACH];
+#pragma unroll
+        for (int q = 0; q < RANK_EACH; ++q) below[q] = (K)(key[q] + (first + k0 < row0 + q * RANK_THREADS));
+#pragma unroll
+        for (int k = 0; k < 64; k += 4) {
+            const Four x = *reinterpret_cast<const Four*>(&others[k0 + k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < RANK_EACH; ++q) n[q] += less(x[i], below[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < RANK_EACH; ++q) {
+            if (first + k0 != row0 + q * RANK_THREADS) continue;
+            uint32_t equal = 0;
+            for (int k = 0; k < 63; ++k) equal += (uint32_t)__builtin_amdgcn_readlane(key[q], k) == key[q] && k < lane;
+            n[q] += (K)equal;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < RANK_KEYS / RANK_ROWS; ++i) others[i * RANK_ROWS + threadIdx.x] = there[i];
-    const int wave_first = scalar(r & ~63);
-    const uint32_t key = key_of_row<TOKEN>(a, wave_first, a.none);
-    __syncthreads();
-    // keys of 64 rows before the wavefront's own count where they are equal, too; those of rows behind only where they are below
-    uint32_t n = 0;
-    auto count = [&](int from, int to, uint32_t below) __attribute__((always_inline)) {
-        for (int k = from; k < to; k += 16) {
-            uintx4 x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uintx4*>(&others[k + 4 * i]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) n += x[i / 4][i % 4] < below;
-        }
-    };
-    const int before = min(max(wave_first - first, 0), RANK_KEYS), behind = min(max(wave_first + 64 - first, 0), RANK_KEYS);
-    count(0, before, key + 1);
-    for (int k = before; k < behind; ++k) n += others[k] < key || (others[k] == key && first + k < r);
-    count(behind, RANK_KEYS, key);
-    if (r >= a.rows) return;
-    if (part == 0) keys[r] = key;
-    counts[(int64_t)part * a.rows + r] = (uint16_t)n;
+    for (int q = 0; q < RANK_EACH; ++q) {
+        const int r = row0 + q * RANK_THREADS + lane;
+        if (r >= a.rows) continue;
+        if (part == 0) keys[r] = key[q];
+        counts[(int64_t)part * a.rows + r] = (uint16_t)n[q];
+    }
 }
 
-__global__ __launch_bounds__(64) void rank_place_kernel(int rows, int parts, const uint32_t* __restrict__ keys, const uint16_t* __restrict__ counts, uint32_t* __restrict__ keys_to,
-                                                        uint32_t* __restrict__ order_to)
+// Puts rows in their places.  An eighth of the table is cleared here: that takes as long as this, which mostly waits.
+__global__ __launch_bounds__(RANK_THREADS) void rank_place_kernel(int rows, int parts, uint32_t place_blocks, const uint32_t* __restrict__ keys, const uint16_t* __restrict__ counts,
+                                                               uint32_t* __restrict__ keys_to, uint32_t* __restrict__ order_to, ClearArgs clear)
 {
-    const int r = blockIdx.x * 64 + threadIdx.x;
+    if (blockIdx.x >= place_blocks) {
+        clear_block(clear, clear.blocks - 1 - (blockIdx.x - place_blocks));
+        return;
+    }
+    const int r = blockIdx.x * RANK_THREADS + threadIdx.x;
     if (r >= rows) return;
     uint32_t n = 0;
 #pragma unroll 8
@@ -452,56 +477,84 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
     }
 }
 
-// Adds up the pieces of longer runs.  A block for a chunk and 64 * E columns: the run longer than PIECE that begins in the chunk, if there is
-// one, a quarter of its pieces to each wavefront, one behind the other, and these four sums in order.
+// Adds up the pieces of longer runs, 64 * E columns to a block.  Each of its wavefronts looks at a chunk; if a run longer than PIECE begins
+// there it adds up its pieces, one behind the other, or, where these are more than JOIN_ALONE (so that two such runs at most begin among the
+// block's chunks), leaves them to all wavefronts: a sixteenth to each, and these sums in order.
+constexpr int JOIN_WAVES = 16, JOIN_ALONE = 8;
+
 template <class T, int E>
-__global__ __launch_bounds__(256) void join_runs_kernel(SumArgs a)
+__global__ __launch_bounds__(JOIN_WAVES * 64) void join_runs_kernel(SumArgs a)
 {
-    __shared__ float meet[3][64][E + 1];
+    __shared__ float meet[JOIN_WAVES][64][E + 1];
+    struct Run {
+        uint32_t key;
+        int chunk, pieces;
+    };
+    __shared__ Run long_runs[JOIN_WAVES];  // pieces 0: none
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
-    const int64_t total = (int64_t)a.chunks * a.col_blocks;
+    const int64_t total = up(a.chunks, JOIN_WAVES) * a.col_blocks;
     for (int64_t block = blockIdx.x; block < total; block += gridDim.x) {
-        const int chunk = (int)(block / a.col_blocks), own = (int)(block % a.col_blocks) * 64 * E + lane * E, col = min(own, a.dim - E);
-        const int p0 = chunk * PIECE, p = p0 + lane;
-        const uint32_t key = p < a.rows ? a.keys[p] : ~0u, before = p0 ? a.keys[p0 - 1] : ~0u;
+        const int64_t chunk = block / a.col_blocks * JOIN_WAVES + wave;
+        const int own = (int)(block % a.col_blocks) * 64 * E + lane * E, col = min(own, a.dim - E);
+        auto add_up = [&](int64_t of, int first, int end, float (&sum)[E]) __attribute__((always_inline)) {
+#pragma unroll 8
+            for (int i = first; i < end; ++i) {
+                float x[E];
+                load_n(a.partial + (2 * (of + i) + (i == 0)) * a.dim + col, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] += x[e];
+            }
+        };
+        auto give = [&](uint32_t key, float (&sum)[E]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] *= a.scale;
+            if (own < a.dim) store_n(row_of_key<T>(a, key) + col, sum);
+        };
+        const int64_t p0 = chunk * PIECE, p = p0 + lane;
+        const uint32_t key = p < a.rows ? a.keys[p] : ~0u, before = p0 && p0 < a.rows ? a.keys[p0 - 1] : ~0u;
         const uint32_t previous = __shfl_up(key, 1, 64), later = __shfl_down(key, PIECE, 64);
         const bool differs = lane ? key != previous : p0 == 0 || key != before;
         const unsigned long long longer = __ballot(lane < PIECE && differs && p + PIECE < a.rows && key < a.none && key == later);
-        if (!longer) continue;  // (the same in all wavefronts)
-        const int at = __builtin_ctzll(longer);
-        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(key, at);
-        // its pieces: those whose first place has the key, counted 64 at a time
-        int pieces = 0;
-        for (bool more = true; more; pieces += 64) {
-            const int64_t q = p0 + at + (int64_t)(pieces + lane) * PIECE;
-            const unsigned long long same = __ballot(q < a.rows && a.keys[min(q, (int64_t)a.rows - 1)] == k);
-            more = same == ~0ull;
-            if (!more) pieces += __popcll(same) - 64;
+        Run run{0, (int)chunk, 0};
+        if (longer) {
+            const int at = __builtin_ctzll(longer);
+            run.key = (uint32_t)__builtin_amdgcn_readlane(key, at);
+            // its pieces: those whose first place has the key, counted 64 at a time
+            for (bool more = true; more; run.pieces += 64) {
+                const int64_t q = p0 + at + (int64_t)(run.pieces + lane) * PIECE;
+                const unsigned long long same = __ballot(q < a.rows && a.keys[min(q, (int64_t)a.rows - 1)] == run.key);
+                more = same == ~0ull;
+                if (!more) run.pieces += __popcll(same) - 64;
+            }
+            if (run.pieces <= JOIN_ALONE) {
+                float sum[E] = {};
+                add_up(chunk, 0, run.pieces, sum);
+                give(run.key, sum);
+                run.pieces = 0;
+            }
         }
-        const int each = (pieces + 3) / 4, first = min(wave * each, pieces), end = min(first + each, pieces);
-        float sum[E] = {};
-#pragma unroll 8
-        for (int i = first; i < end; ++i) {
-            float x[E];
-            load_n(a.partial + (2 * (int64_t)(chunk + i) + (i == 0)) * a.dim + col, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] += x[e];
-        }
-        if (wave) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) meet[wave - 1][lane][e] = sum[e];
-        }
+        if (lane == 0) long_runs[wave] = run;
         __syncthreads();
-        if (wave == 0 && own < a.dim) {
+        for (int k = 0; k < JOIN_WAVES; ++k) {
+            const Run of = long_runs[k];
+            if (!of.pieces) continue;  // (the same in all wavefronts)
+            const int each = (of.pieces + JOIN_WAVES - 1) / JOIN_WAVES, first = min(wave * each, of.pieces);
+            float sum[E] = {};
+            add_up(of.chunk, first, min(first + each, of.pieces), sum);
 #pragma unroll
-            for (int w = 0; w < 3; ++w)
+            for (int e = 0; e < E; ++e) meet[wave][lane][e] = sum[e];
+            __syncthreads();
+            if (wave == k) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += meet[w][lane][e];
+                for (int e = 0; e < E; ++e) sum[e] = meet[0][lane][e];
+                for (int w = 1; w < JOIN_WAVES; ++w)
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] *= a.scale;
-            store_n(row_of_key<T>(a, k) + col, sum);
+                    for (int e = 0; e < E; ++e) sum[e] += meet[w][lane][e];
+                give(of.key, sum);
+            }
+            __syncthreads();  // what met is written again
         }
-        __syncthreads();  // what met is written again
+        __syncthreads();  // and the list
     }
 }
 
@@ -704,13 +757,15 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
         using TOKEN = decltype(token);
         if (!space.tiles) {
             const uint32_t ranks = (uint32_t)(up(e->rows, RANK_ROWS) * space.parts);
-            hipLaunchKernelGGL(rank_and_clear_kernel<TOKEN>, dim3(ranks + clear.blocks), dim3(RANK_ROWS), 0, s, a, ranks, space.parts, word(space.keys[1]),
+            const uint32_t places = (uint32_t)up(e->rows, RANK_THREADS), later = places ? clear.blocks / 8 : 0;
+            const auto rank = none < 1 << 24 ? rank_and_clear_kernel<TOKEN, float> : rank_and_clear_kernel<TOKEN, uint32_t>;
+            hipLaunchKernelGGL(rank, dim3(ranks + clear.blocks - later), dim3(RANK_THREADS), 0, s, a, ranks, space.parts, word(space.keys[1]),
                                reinterpret_cast<uint16_t*>(base + space.counts), clear);
             keys = word(space.keys[0]);
             order = word(space.order[0]);
-            if (e->rows)
-                hipLaunchKernelGGL(rank_place_kernel, dim3((uint32_t)up(e->rows, 64)), dim3(64), 0, s, (int)e->rows, space.parts, word(space.keys[1]),
-                                   reinterpret_cast<const uint16_t*>(base + space.counts), word(space.keys[0]), word(space.order[0]));
+            if (places)
+                hipLaunchKernelGGL(rank_place_kernel, dim3(places + later), dim3(RANK_THREADS), 0, s, (int)e->rows, space.parts, places, word(space.keys[1]),
+                                   reinterpret_cast<const uint16_t*>(base + space.counts), word(space.keys[0]), word(space.order[0]), clear);
             return;
         }
         for (int pass = 0; pass < space.passes; ++pass) {
@@ -744,7 +799,7 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
         using T = decltype(t);
         auto sum = [&](auto sum_runs, auto join_runs) {
             hipLaunchKernelGGL(sum_runs, dim3((uint32_t)up(waves, 4)), dim3(256), 0, s, b);
-            if (e->rows > PIECE) hipLaunchKernelGGL(join_runs, dim3((uint32_t)std::min<int64_t>(waves, 1 << 20)), dim3(256), 0, s, b);
+            if (e->rows > PIECE) hipLaunchKernelGGL(join_runs, dim3((uint32_t)std::min<int64_t>(up(b.chunks, JOIN_WAVES) * b.col_blocks, 1 << 18)), dim3(JOIN_WAVES * 64), 0, s, b);
         };
         constexpr int E = 16 / sizeof(T);
         if (e->dim < E)

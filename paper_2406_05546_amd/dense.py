@@ -130,7 +130,7 @@ _CHECKPOINT = "QQqq"
 _CHECKPOINT_BYTES = struct.calcsize("<" + _CHECKPOINT)
 assert _LAYER_BYTES == ctypes.sizeof(ps_linear) and _MATRIX_BYTES == ctypes.sizeof(ps_matrix) and _CHECKPOINT_BYTES == ctypes.sizeof(ps_checkpoint)
 _PACK = {n: struct.Struct(_LAYER + n * _MATRIX).pack_into for n in (6, 7)}
-_PACK_CHECKPOINT = struct.Struct("<" + _CHECKPOINT).pack_into
+_PACK_MATRIX, _PACK_CHECKPOINT = struct.Struct("<" + _MATRIX).pack_into, struct.Struct("<" + _CHECKPOINT).pack_into
 _ABSENT = (0, 0, 0)
 
 
@@ -220,15 +220,15 @@ def ps_checkpoint_empty(rows: int, cols: int, device) -> Checkpoint:
                       torch.empty(rows, -(-cols // CHECKPOINT_BLOCK), dtype=torch.float8_e8m0fnu, device=device))
 
 
-def _code_call(call: str, dtype: int, x, c: Checkpoint, encode: bool, act: int) -> None:
-    device, shape = x.device, tuple(x.shape)
+def _code_call(call: str, dtype: int, x, device, shape, kept, encode: bool, act: int) -> None:
+    """kept: the fields of the checkpoint."""
     index = device.index
     if index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _code_call(call, dtype, x, c, encode, act)
+            return _code_call(call, dtype, x, device, shape, kept, encode, act)
     a = _arguments
-    struct.pack_into("<" + _MATRIX, a.memory, _LAYER_BYTES, *_matrix(call, "x", x, device, x.dtype, shape))
-    _PACK_CHECKPOINT(a.memory, a.of_checkpoints[0], *_kept(call, "the checkpoint", c, device, shape))
+    _PACK_MATRIX(a.memory, _LAYER_BYTES, *_matrix(call, "x", x, device, x.dtype, shape))
+    _PACK_CHECKPOINT(a.memory, a.of_checkpoints[0], *kept)
     lib, at, kept, stream = _library(), a.at_matrices[0], a.at + a.of_checkpoints[0], torch._C._cuda_getCurrentRawStream(index)
     st = lib.ps_checkpoint_encode(dtype, *shape, at, kept, stream) if encode else lib.ps_checkpoint_decode(dtype, *shape, kept, act, at, stream)
     if st != PS_OK:
@@ -240,11 +240,16 @@ def ps_checkpoint_encode(x, out: Optional[Checkpoint] = None) -> Checkpoint:
     2^-15 of their block's largest on.  What is not 0 is not held as 0; what is not finite is held as NaN."""
     call = "ps_checkpoint_encode"
     dtype = _dtype(call, "x", x)
-    if x.dim() != 2 or x.device.type != "cuda":
+    device, shape = x.device, x.shape
+    if len(shape) != 2 or device.type != "cuda":
         _refuse(call, "x is [rows, cols] on a GPU")
-    c = ps_checkpoint_empty(*x.shape, x.device) if out is None else out
-    _code_call(call, dtype, x, c, True, 0)
-    return c
+    if out is None:
+        out = ps_checkpoint_empty(*shape, device)
+        kept = out.codes.data_ptr(), out.scales.data_ptr(), shape[1], -(-shape[1] // CHECKPOINT_BLOCK)
+    else:
+        kept = _kept(call, "out", out, device, shape)
+    _code_call(call, dtype, x, device, shape, kept, True, 0)
+    return out
 
 
 def ps_checkpoint_decode(c: Checkpoint, dtype=torch.bfloat16, activation: str = "none", out=None):
@@ -258,7 +263,7 @@ def ps_checkpoint_decode(c: Checkpoint, dtype=torch.bfloat16, activation: str = 
     x = torch.empty(c.shape, dtype=dtype, device=c.device) if out is None else out
     if x.shape != c.shape or x.device != c.device:
         _refuse(call, f"out has the shape {tuple(x.shape)} on {x.device}, not {tuple(c.shape)} on {c.device}")
-    _code_call(call, _dtype(call, "out", x), x, c, False, act)
+    _code_call(call, _dtype(call, "out", x), x, c.device, c.shape, _kept(call, "the checkpoint", c, c.device, c.shape), False, act)
     return x
 
 

@@ -91,13 +91,13 @@ def _tokens(call: str, t, device, rows: Optional[int] = None):
     return t.data_ptr(), t.stride(0), size
 
 
-def _call(call: str, name: str, device, *args) -> None:
+def _call(call: str, device, *args) -> None:
     """Calls the library on the current stream of the device."""
     index = device.index
     if index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _call(call, name, device, *args)
-    st = getattr(_library(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+            return _call(call, device, *args)
+    st = getattr(_library(), call)(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != PS_OK:
         raise PsError(call, st, (_library().ps_dense_last_error() or b"").decode())
 
@@ -142,7 +142,7 @@ def _embedding_forward(tokens, offsets, table, scale, table_of_group, out):
     a = _arguments
     _EMBEDDING.pack_into(a.memory, 0, dtype, groups, shape[0] if grouped else 1, of_out[0], shape[-2], shape[-1], at_offsets, at_index, scale, *given,
                          *_matrix(call, "table", table, device, table.dtype, shape, grouped), *_matrix(call, "out", y, device, table.dtype, of_out))
-    _call(call, call, device, *a.embedding)
+    _call(call, device, *a.embedding)
     return y
 
 
@@ -175,7 +175,7 @@ def _embedding_backward(dy, tokens, offsets, vocab, scale, dtable):
     _EMBEDDING.pack_into(a.memory, 0, dtype, groups, 1, rows, vocab, dim, at_offsets, 0, scale, *given,
                          *_matrix(call, "dy", dy, device, dy.dtype, (rows, dim)), *_matrix(call, "dtable", dtable, device, dy.dtype, shape, offsets is not None))
     ws, need = _workspace(call, "ps_embedding_workspace_bytes", device)
-    _call(call, call, device, *a.embedding, None if ws is None else ws.data_ptr(), need)
+    _call(call, device, *a.embedding, None if ws is None else ws.data_ptr(), need)
     return dtable
 
 
@@ -229,7 +229,7 @@ def ps_logprob_forward(logits, tokens=None, scale: float = 1.0, top: int = 0) ->
     _LOGPROB.pack_into(a.memory, 0, dtype, top, rows, vocab, scale, *given, *_matrix(call, "logits", logits, device, logits.dtype, (rows, vocab)), *7 * (0,))
     at, at_tokens, at_logits = a.logprob[:3]
     ws, need = _workspace(call, "ps_logprob_workspace_bytes", device)
-    _call(call, call, device, at, at_tokens, at_logits, None if logp is None else logp.data_ptr(), norm.data_ptr(), top_logp.data_ptr() if top else None,
+    _call(call, device, at, at_tokens, at_logits, None if logp is None else logp.data_ptr(), norm.data_ptr(), top_logp.data_ptr() if top else None,
           top_tokens.data_ptr() if top else None, None if ws is None else ws.data_ptr(), need)
     return LogProb(logp, norm, top_logp, top_tokens)
 
@@ -258,5 +258,5 @@ def ps_logprob_backward(logits, tokens, norm, dlogp=None, dentropy=None, scale: 
     _LOGPROB.pack_into(a.memory, 0, dtype, 0, rows, vocab, scale, *given, *_matrix(call, "logits", logits, device, logits.dtype, shape),
                        *_matrix(call, "out", d, device, logits.dtype, shape), *_numbers(call, "dlogp", dlogp, device, rows), *_numbers(call, "dentropy", dentropy, device, rows))
     at, at_tokens, at_logits, at_out, at_dlogp, at_dentropy = a.logprob
-    _call(call, call, device, at, at_tokens, at_logits, norm.data_ptr(), at_dlogp, at_dentropy, at_out)
+    _call(call, device, at, at_tokens, at_logits, norm.data_ptr(), at_dlogp, at_dentropy, at_out)
     return d

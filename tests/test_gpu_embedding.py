@@ -145,7 +145,7 @@ def some_tokens(kind, rows, vocab, g):
 # runs and chunks around 32 places, one block's sort and several, one to four digits
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows,vocab,dim", [(0, 5, 8), (1, 1, 1), (31, 4, 8), (32, 300, 33), (33, 2, 520), (64, 1, 7), (65, 70000, 3), (1000, 255, 24), (1000, 256, 24), (8192, 300, 5),
-                                            (8193, 300, 5), (20000, 70000, 2), (30000, 11, 9)])
+                                            (8193, 300, 5), (20000, 70000, 2), (30000, 11, 9), (3000, 1 << 22, 1), (16384, 3, 4)])
 def test_gradient(tk, kind, rows, vocab, dim):
     import torch
     g = gen(rows + vocab + dim)
@@ -181,6 +181,19 @@ def test_gradient_in_groups(tk, rows, vocab, dim, groups):
     for k in (0, groups // 2, groups - 1):
         alone = tk.ps_embedding_backward(dy[cuts[k]:cuts[k + 1]], tok[cuts[k]:cuts[k + 1]], vocab, -0.25)
         assert torch.equal(alone, got[k])
+
+
+def test_keys_of_more_than_24_bits(tk):
+    """Workers' tokens whose numbers, with the workers', pass what 32-bit floats hold."""
+    import torch
+    g, rows, vocab, groups = gen(2), 5000, 1 << 20, 20
+    cuts = [rows * i // groups for i in range(groups + 1)]
+    # neighbours, high and low, so that keys differ by one
+    tok = torch.randint(0, 4, (rows,), device="cuda", generator=g) + torch.where(torch.rand(rows, device="cuda", generator=g) < 0.5, 0, vocab - 4)
+    dy = torch.randn(rows, 1, device="cuda", generator=g)
+    got = tk.ps_grouped_embedding_backward(dy, tok, torch.tensor(cuts, dtype=torch.int32).cuda(), vocab)
+    want, off = gradient64(dy.cpu(), tok.cpu(), vocab, 1.0, owner_of(rows, cuts), groups)
+    close(got.cpu(), want, off, "gradients")
 
 
 @pytest.mark.parametrize("rows,vocab,dim,gap", [(40, 30, 5, 3), (40, 30, 1, 1), (100, 70, 300, 12), (20, 9, 40000, 5), (17000, 50, 24, 40)])
