@@ -231,7 +231,7 @@ __device__ __forceinline__ void rank_keys(TileCounts& c, const uint32_t (&key)[T
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int d = lane; d < DIGITS; d += 64) c.at[wave][d] = 0;
-    __builtin_amdgcn_wave_barrier();
+    wave_meets();
     const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
     for (int i = 0; i < TILE_EACH; ++i) {
@@ -244,9 +244,9 @@ __device__ __forceinline__ void rank_keys(TileCounts& c, const uint32_t (&key)[T
             same &= bit ? set : ~set;
         }
         const uint32_t before = c.at[wave][d];
-        __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront in order: all have read before one of them counts on
+        wave_meets();  // all have read before one of them counts on
         if (!(same & below)) c.at[wave][d] = before + __popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        wave_meets();
         rank[i] = before + __popcll(same & below);
     }
 }

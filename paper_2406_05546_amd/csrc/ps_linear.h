@@ -61,6 +61,15 @@ struct GroupRows {
 
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// What lanes of a wavefront wrote to LDS before this is what its lanes read behind it: LDS serves a wavefront in order, so nothing is
+// waited for, but the compiler moves and keeps nothing across it.
+__device__ __forceinline__ void wave_meets()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ GroupRows group_rows(const Groups& gs, int g)
 {
     if (!gs.offsets) return {g, 0, gs.rows};

@@ -9,7 +9,6 @@
 #include "ps_tokens.h"
 
 #include <cmath>
-#include <type_traits>
 
 namespace ps {
 namespace {
@@ -151,8 +150,9 @@ struct Range {
 
 // The best `top` values of a range.  Each lane knows the largest of its own values; the top-th largest of these is a value that at least
 // `top` values reach, and only lanes whose largest reaches it can have one of the best: these lanes' vectors, few, are read again, and
-// what reaches it is listed.  Where more than LIST do (equal values), what is above it is listed, and then the first that equal it; where that is
-// too much as well (an order made for it), the top-th value itself is found bit by bit.  A value's place is the number of
+// what reaches it (but for its lower bits) is listed.  Where more than LIST do (equal values), what is above it is listed, and then the first that
+// equal it (4096 rows of 50257 equal values in bf16 take 4 times as long as random ones); where that is too much as well (an order made for
+// it), the top-th value itself is found bit by bit.  A value's place is the number of
 // listed keys above its own, so the order in which they were listed does not matter.
 constexpr int LIST = 256;
 template <int WAVES>
@@ -170,16 +170,16 @@ __device__ __forceinline__ void meet_all()
     if constexpr (WAVES > 1)
         __syncthreads();
     else
-        __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront in order
+        wave_meets();
 }
 
-// The k-th largest of the lanes' values (with more than four wavefronts, of the largest of four lanes each), its lower 16 bits left out:
-// reached by as many.  For a whole wavefront.
+// The k-th largest of the lanes' values (with more than four wavefronts, of the largest of four lanes each), from bit `high_bit` to `low_bit` of
+// its number; what is above is in `least`, what is below left out, so that as many reach it.  For a whole wavefront.
 template <int WAVES>
-__device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k)
+__device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k, uint32_t least = 0, int high_bit = 31, int low_bit = 16)
 {
     constexpr int EACH = WAVES < 4 ? WAVES : 4;
-    uint32_t o[EACH], least = 0;
+    uint32_t o[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         float v = high[i * 64 + (threadIdx.x & 63)];
@@ -187,7 +187,7 @@ __device__ __forceinline__ uint32_t kth_of_lanes(const float* high, int k)
         for (int w = i + EACH; w < WAVES; w += EACH) v = fmaxf(v, high[w * 64 + (threadIdx.x & 63)]);
         o[i] = ordered(v);
     }
-    for (int b = 31; b >= 16; --b) {
+    for (int b = high_bit; b >= low_bit; --b) {
         const uint32_t more = least | 1u << b;
         int n = 0;
 #pragma unroll
@@ -257,6 +257,13 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
             meet_all<WAVES>();
             return s.count;
         };
+        // the top-th largest lane's value to its last bit, so that what equals it is told from what is above
+        if (wave == 0) {
+            from = kth_of_lanes<WAVES>(s.high, top, from, 15, 0);
+            if (lane == 0) s.from = from;
+        }
+        meet_all<WAVES>();
+        from = s.from;
         n = list_above();
         if (n > LIST) {
             from = 0;
@@ -320,7 +327,7 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
 }
 
 // WAVES wavefronts take a row, or a part of one, in rounds of VECTORS vectors to a lane; the next round is asked for before the present
-// one is worked on.  Where rows are few, parts of them are blocks of their own, and join_parts_kernel finishes.  Bound by memory; behind it by
+// one is worked on.  Where rows are few, parts of them are blocks of their own, and join_row_kernel finishes.  Bound by memory; behind it by
 // the vector ALU: about ten operations and an exponential for a value.
 template <class T, int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprob_kernel(ForwardArgs a)
@@ -427,7 +434,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprob_kernel(F
 constexpr int MOST_PARTS = 64;
 
 template <class T, bool TOP>
-__global__ __launch_bounds__(256) void join_parts_kernel(ForwardArgs a)
+__global__ __launch_bounds__(256) void join_row_kernel(ForwardArgs a)
 {
     __shared__ uint64_t list[TOP ? MOST_PARTS * PS_LOGPROB_MAX_TOP : 1], best[TOP ? PS_LOGPROB_MAX_TOP : 1];
     __shared__ float high[64];
@@ -604,7 +611,7 @@ void start_forward(const ForwardArgs& a, hipStream_t s)
         return;
     }
     hipLaunchKernelGGL((logprob_kernel<T, 4, TOP>), dim3((uint32_t)std::min(a.rows * a.parts, most)), dim3(256), 0, s, a);
-    if (a.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, TOP>), dim3((uint32_t)a.rows), dim3(256), 0, s, a);
+    if (a.parts > 1) hipLaunchKernelGGL((join_row_kernel<T, TOP>), dim3((uint32_t)a.rows), dim3(256), 0, s, a);
 }
 
 template <class F>

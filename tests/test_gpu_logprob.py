@@ -157,6 +157,21 @@ def test_many_rows_and_long_ones(tk, dtype):
         check_forward(tk, z, torch.randint(0, vocab, (rows,), device="cuda", generator=g), 1.0, top)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(5, 2000), (3, 8192), (2, 50000), (300, 20000), (2, 131072)])
+def test_large_values_that_few_lanes_have(tk, dtype, rows, vocab):
+    """A row's vectors of 16 bytes go to 64, 256 or 1024 lanes in turn.  Where fewer lanes than there are alternatives have all that is large, the
+    alternatives are not told by the lanes' largest values."""
+    import torch
+    t, g = getattr(torch, dtype), gen(vocab)
+    vector = torch.arange(vocab, device="cuda") // (16 // t.itemsize)
+    for period in (64, 256, 1024):
+        z = torch.randn(rows, vocab, device="cuda", generator=g)
+        z = torch.where(vector % period < 31, z + 50, z).to(t)
+        check_forward(tk, z, None, 1.0, 32)
+        check_forward(tk, torch.where(vector % period < 3, z + 50, 0).to(t), None, 1.0, 4)  # and many equal ones below
+
+
 def test_rows_apart_and_at_any_place(tk):
     import torch
     for dtype in TYPES:
