@@ -27,7 +27,8 @@ struct LookupArgs {
 
 // A block takes `each` rows (up to 64).  Its first wavefront finds where they come from, one row to a lane; then every thread takes
 // pieces of E columns, LOOKUP_AHEAD of them asked for together.  A row's last piece ends with the row, and so covers columns of the one
-// before again: no piece is partial (E is 1 for rows shorter than 16 bytes).
+// before again: no piece is partial (E is 1 for rows shorter than 16 bytes).  Bound by memory: 16384 rows of 2048 in bf16 from eight tables for 64
+// groups 22.7 us, 5.9 TB/s.
 constexpr int LOOKUP_AHEAD = 4;
 constexpr int64_t NO_GROUP = -1, NO_TOKEN = -2;
 
@@ -140,7 +141,8 @@ __device__ __forceinline__ void clear_block(const ClearArgs& a, uint32_t block)
 // lanes; two rows to a thread, so that the comparisons and not these reads are what takes time.  K: keys below 2^24 are compared as floats,
 // whose difference, taken into 0 .. 1 as it is formed, is what is counted (two instructions; an integer comparison has to wait for its
 // result to be added).  16384 rows alone: 27 us with one row and integers, 24 with two, 19 with floats.  Next to them the table is
-// cleared, which is bound by memory.
+// cleared, which is bound by memory: with 206 MB of it 29 us.  By ranks, and by the sort below, all of the call with 256 columns and 1000
+// tokens in bf16: 8192 rows 27.9 and 37.0 us, 16384 34.7 and 37.9, 24576 47.0 and 39.5.
 constexpr int RANK_THREADS = 256, RANK_EACH = 2, RANK_ROWS = RANK_THREADS * RANK_EACH, RANK_KEYS = 512, RANK_MOST = 16384;
 
 __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) { return a < b; }
@@ -353,6 +355,7 @@ __global__ __launch_bounds__(DIGITS) void sort_place_kernel(SortArgs a, int shif
 // the gradient, those of a longer run go to `partial`, of which each PIECE places in the order have two rows: for the piece, not the
 // first of its run, that begins in them, and for the first piece of a run longer than that.  (There cannot be more: two pieces
 // of a run begin PIECE places apart.)
+// Pieces of 32 rows, and four or sixteen rows ahead, took as long, within 3 %.
 constexpr int PIECE = 16, SUM_AHEAD = 8;
 
 struct SumArgs {
@@ -406,6 +409,7 @@ struct Held<T, 1> {
 // Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.  A lane
 // whose columns would go past the row's end takes the last E of the row, which others have too (E is 1 for rows shorter than 16 bytes).  Bound by
 // memory: SUM_AHEAD rows are asked for while as many are added up, without a branch between them, at which the compiler would wait.
+// 16384 rows of 2048 in bf16 over 50257 tokens 24 us, 3.7 TB/s.
 template <class T, int E>
 __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
 {
@@ -479,7 +483,8 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
 
 // Adds up the pieces of longer runs, 64 * E columns to a block.  Each of its wavefronts looks at a chunk; if a run longer than PIECE begins
 // there it adds up its pieces, one behind the other, or, where these are more than JOIN_ALONE (so that two such runs at most begin among the
-// block's chunks), leaves them to all wavefronts: a sixteenth to each, and these sums in order.
+// block's chunks), leaves them to all wavefronts: a sixteenth to each, and these sums in order.  Bound by trips to memory that wait for each other:
+// 16384 rows of 2048 6.9 us (12.3 with up to 32 pieces to a wavefront alone).
 constexpr int JOIN_WAVES = 16, JOIN_ALONE = 8;
 
 template <class T, int E>
@@ -706,7 +711,8 @@ extern "C" ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens
     a.dim = (int32_t)e->dim;
     const int wide = 16 / dtype_size(e->dtype);
     a.pieces = (int32_t)(e->dim < wide ? e->dim : up(e->dim, wide));
-    // rows of 32 KB together, or fewer where that leaves less than four blocks to a compute unit
+    // Rows of 32 KB together, or fewer where that leaves less than four blocks to a compute unit.  (bf16, us: one to a
+    // block for 64 rows of 4096 7.0, 64 34.5; eight for 16384 of 2048 in 64 groups 22.1, one 31.2, 64 26.4; 64 for 65536 of 64 8.4, one 56.8.)
     a.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2048 / a.pieces), e->rows / (4 * COMPUTE_UNITS)));
     a.scale = (float)e->scale;
     a.groups = groups_of(*e);

@@ -328,7 +328,8 @@ __device__ __forceinline__ void best_of_range(const Range<T, WAVES>& r, Scratch<
 
 // WAVES wavefronts take a row, or a part of one, in rounds of VECTORS vectors to a lane; the next round is asked for before the present
 // one is worked on.  Where rows are few, parts of them are blocks of their own, and join_row_kernel finishes.  Bound by memory; behind it by
-// the vector ALU: about ten operations and an exponential for a value.
+// the vector ALU: about ten operations and an exponential for a value.  bf16, 4096 rows of 50257: 83 us, 4.9 TB/s, with 5 alternatives 90; fp32 144 and
+// 152 us, 5.7 TB/s.
 template <class T, int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprob_kernel(ForwardArgs a)
 {
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprob_kernel(F
     }
 }
 
-// Finishes rows that were cut into parts: a block to a row.
+// Finishes rows that were cut into parts: a block to a row.  Bound by its dependent trips to memory: 4.6 us for one row in 16 parts.
 constexpr int MOST_PARTS = 64;
 
 template <class T, bool TOP>
@@ -494,6 +495,7 @@ struct BackwardArgs {
 };
 
 // dz = scale (gl ([j is the token] - p) - gh p (log p + H)), so -p (A + B t) with t = log2 p, A = scale (gl + gh H), B = scale gh ln 2.
+// Bound by memory: bf16 8192 rows of 32768 184 us, 5.8 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
 {
@@ -582,8 +584,9 @@ ps_status check_numbers(const char* call, const char* name, const void* p, int64
 // launch (256 rows of 50257 in bf16 with 5 alternatives 20.8 us in parts, 15.4 this way; one of 131072 with 20 17.3 and 17.3, alone 33 and 37).
 bool sixteen(const ps_logprob& l) { return l.rows <= COMPUTE_UNITS && l.vocab <= 65536; }
 
-// Parts of a row, so many rounds of four wavefronts each: as many as make eight blocks for a compute unit of all rows, one where
-// there are as many rows.
+// Parts of a row, so many rounds of four wavefronts each: as many as make two blocks for a compute unit of all rows, one where there are as
+// many rows.  (Two blocks, and eight, with 5 alternatives, us: bf16 512 rows of 20000 13.0 and 17.6, of 131072 31.3 and 36.7, 128 of 131072 16.7
+// and 20.4, one 16.7 and 15.8; fp32 512 of 50000 21.5 and 30.2.)
 struct Cut {
     int parts, rounds;
 };
@@ -591,7 +594,7 @@ Cut cut_rows(const ps_logprob& l)
 {
     if (sixteen(l)) return {1, 0};
     const int64_t round = 4 * 64 * VECTORS * 16 / dtype_size(l.dtype), rounds = (l.vocab + round - 1) / round;  // (a part more for what is ahead of a row)
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, MOST_PARTS), l.rows ? 8 * COMPUTE_UNITS / l.rows : 1));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, MOST_PARTS), l.rows ? 2 * COMPUTE_UNITS / l.rows : 1));
     const int64_t each = (rounds + parts - 1) / parts;
     return {(int)((rounds + each - 1) / each), (int)each};
 }
@@ -600,9 +603,13 @@ uint64_t sums_bytes(const ps_logprob& l, const Cut& c) { return ((uint64_t)l.row
 template <class T, bool TOP>
 void start_forward(const ForwardArgs& a, hipStream_t s)
 {
+    // One wavefront to a row that it takes in one round, and in up to eight where there are rows for two wavefronts to a SIMD: no row waits for
+    // four.  (One, and four, without and with 5 alternatives, us: bf16 2048 rows of 8000 10.3 13.3, 11.0 17.8; 8192 of 4000 17.9 22.7, 26.1 53.5, of
+    // 16000 47.7 61.6, 52.0 73.2; 2048 of 20000 as long; 4096 of 50257 with alternatives 98, 91; fp32 16384 of 4000 42.3 56.5, 44.5 99.9, 8192 of 8000 43.5 59.8, 41.2
+    // 61.8.)
     constexpr int ROUND = 64 * VECTORS * 16 / (int)sizeof(T);  // of a wavefront
     const int64_t most = 1 << 20;
-    if (a.vocab <= ROUND) {
+    if (a.vocab <= ROUND || (a.vocab <= 8 * ROUND && a.rows >= 8 * COMPUTE_UNITS)) {
         hipLaunchKernelGGL((logprob_kernel<T, 1, TOP>), dim3((uint32_t)std::min((a.rows + 3) / 4, most)), dim3(256), 0, s, a);
         return;
     }
