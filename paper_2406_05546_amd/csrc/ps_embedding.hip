@@ -2,12 +2,14 @@
 //
 // The gradient is summed over sorted tokens: rows are put in the order of (group, token), those of equal ones staying in the order
 // that they have, and so the rows of one sum lie one behind the other.  No atomics: the same order every time.  The table is cleared
-// as a whole beside the sorting, and the tokens that are there are written over it.
+// as a whole beside the sorting, and the tokens that are there are written over it.  A few rows take one launch, in which every block
+// sorts what belongs to its part of the table.
 #include "../../include/ps_tokens.h"
 #include "ps_linear.h"
 #include "ps_tokens.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace ps {
 namespace {
@@ -141,7 +143,7 @@ __device__ __forceinline__ void clear_block(const ClearArgs& a, uint32_t block)
 // lanes; two rows to a thread, so that the comparisons and not these reads are what takes time.  K: keys below 2^24 are compared as floats,
 // whose difference, taken into 0 .. 1 as it is formed, is what is counted (two instructions; an integer comparison has to wait for its
 // result to be added).  16384 rows alone: 27 us with one row and integers, 24 with two, 19 with floats.  Next to them the table is
-// cleared, which is bound by memory: with 206 MB of it 29 us.  By ranks, and by the sort below, all of the call with 256 columns and 1000
+// cleared, which is bound by memory: with 206 MB of it 34 us.  By ranks, and by the sort below, all of the call with 256 columns and 1000
 // tokens in bf16: 8192 rows 27.9 and 37.0 us, 16384 34.7 and 37.9, 24576 47.0 and 39.5.
 constexpr int RANK_THREADS = 256, RANK_EACH = 2, RANK_ROWS = RANK_THREADS * RANK_EACH, RANK_KEYS = 512, RANK_MOST = 16384;
 
@@ -220,6 +222,7 @@ __global__ __launch_bounds__(RANK_THREADS) void rank_place_kernel(int rows, int 
 
 // More rows: a stable radix sort of their keys, 8 bits at a time.  A tile of keys is ranked by a block: every wavefront has 64 at a time,
 // finds with eight ballots which of them have the same digit, and counts them in a column of its own, so that equal digits stay in order.
+// Bound by latency: 32768 rows 4.7, 4.0 and 5.6 us for the three launches of a pass.
 constexpr int DIGITS = 256, TILE_WAVES = 4, TILE_EACH = 4, SORT_TILE = TILE_WAVES * 64 * TILE_EACH;
 static_assert(TILE_WAVES * 64 == DIGITS, "a thread for each digit");
 
@@ -394,6 +397,15 @@ __device__ __forceinline__ T* row_of_key(const SumArgs& a, uint32_t key)
     return static_cast<T*>(a.dtable) + (int64_t)g * a.table_matrix + (int64_t)v * a.table_row;
 }
 
+// The product as 32 bits hold it: the compiler would make one instruction of it and the rounding to 16 bits where it finds them together, whose
+// results differ now and then.
+__device__ __forceinline__ float scaled(float v, float scale)
+{
+    v *= scale;
+    asm("" : "+v"(v));
+    return v;
+}
+
 // E values as they were read
 template <class T, int E>
 struct Held {
@@ -409,7 +421,7 @@ struct Held<T, 1> {
 // Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.  A lane
 // whose columns would go past the row's end takes the last E of the row, which others have too (E is 1 for rows shorter than 16 bytes).  Bound by
 // memory: SUM_AHEAD rows are asked for while as many are added up, without a branch between them, at which the compiler would wait.
-// 16384 rows of 2048 in bf16 over 50257 tokens 24 us, 3.7 TB/s.
+// 16384 rows of 2048 in bf16 over 50257 tokens 24 us, 3.7 TB/s (28 beside what the clearing left to be written).
 template <class T, int E>
 __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
 {
@@ -470,7 +482,7 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
             if (whole_start && !(goes_on >> place & 1)) {
                 float v[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[e] = sum[e] * a.scale;
+                for (int e = 0; e < E; ++e) v[e] = scaled(sum[e], a.scale);
                 store_n(row_of_key<T>(a, (uint32_t)__builtin_amdgcn_readlane(key, place)) + col, v);
             } else {
                 store_n(a.partial + (2 * (int64_t)chunk + whole_start) * a.dim + col, sum);
@@ -512,7 +524,7 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_runs_kernel(SumArgs a)
         };
         auto give = [&](uint32_t key, float (&sum)[E]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] *= a.scale;
+            for (int e = 0; e < E; ++e) sum[e] = scaled(sum[e], a.scale);
             if (own < a.dim) store_n(row_of_key<T>(a, key) + col, sum);
         };
         const int64_t p0 = chunk * PIECE, p = p0 + lane;
@@ -563,6 +575,194 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_runs_kernel(SumArgs a)
     }
 }
 
+// ---- fewer rows: one launch ----------------------------------------------------------------------------------------------
+
+struct FewArgs {
+    const void *dy, *tokens;
+    void* dtable;
+    const int32_t* offsets;
+    int64_t dy_row, table_row, table_matrix, token_stride, vocab;
+    int32_t rows, dim, shift, col_blocks;  // a block has every (2^shift)-th row of a group's table
+    float scale;
+};
+
+// A block has rows of one group's table, evenly apart so that frequent tokens, which are often the first ones, are many blocks'; of wide rows 64 * E
+// columns.  It looks at all of the group's tokens, puts the rows that have its own in their order (in LDS: counts, then places, equal
+// ones as they were), clears what nothing is added to and adds up the rest.  Sums are formed in the order that the kernels above have:
+// the same bits.  Bound by trips to memory, offsets, tokens, rows, and by the clearing; a token that all rows have, by the one block that adds them up, for
+// which there are eight wavefronts (four: 64 rows 13 us, 16 there; 256 equal ones 41, 32) and registers for six of them to a SIMD.
+constexpr int FEW_WAVES = 8, FEW_MOST = 512, FEW_UNITS = 16, FEW_BYTES = 65536, FEW_AHEAD = 8;
+
+template <class TOKEN, class T, int E>
+__global__ __launch_bounds__(FEW_WAVES * 64, 6) void few_rows_kernel(FewArgs a)
+{
+    extern __shared__ uint16_t order[];  // rows, counted from the group's first, in the order of their tokens
+    __shared__ union {
+        uint32_t at[FEW_WAVES][DIGITS];
+        float meet[FEW_UNITS][E][64];
+    } s;
+    __shared__ uint32_t begins[DIGITS + 1], wave_sum[DIGITS / 64];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
+    const int col_block = blockIdx.x % a.col_blocks, block = blockIdx.x / a.col_blocks, g = block >> a.shift;
+    const int64_t others = (1ll << a.shift) - 1, v0 = block & others;
+    const int n = (int)((a.vocab - v0 + others) >> a.shift);
+    if (n <= 0) return;
+    const int begin = a.offsets ? min(max(a.offsets[g], 0), a.rows) : 0, end = a.offsets ? min(max(a.offsets[g + 1], 0), a.rows) : a.rows;
+    T* const table = static_cast<T*>(a.dtable) + g * a.table_matrix + v0 * a.table_row;
+    const int64_t table_row = a.table_row << a.shift;
+    for (int i = threadIdx.x; i < FEW_WAVES * DIGITS; i += FEW_WAVES * 64) s.at[0][i] = 0;
+
+    // A wavefront has one stretch of the group's rows, and visits those of the block's tokens 64 rows at a time: with the token's place among the block's,
+    // which lanes have the same, and the row.
+    const int per = (int)up(max(end - begin, 0), FEW_WAVES * 64) * 64, w0 = begin + wave * per, w1 = min(w0 + per, end);
+    auto visit = [&](auto f) __attribute__((always_inline)) {
+        for (int first = w0; first < w1; first += 64 * TILE_EACH) {
+            int64_t t[TILE_EACH];
+#pragma unroll
+            for (int i = 0; i < TILE_EACH; ++i) t[i] = static_cast<const TOKEN*>(a.tokens)[(int64_t)min(first + i * 64 + lane, w1 - 1) * a.token_stride];
+#pragma unroll
+            for (int i = 0; i < TILE_EACH; ++i) {
+                const int row = first + i * 64 + lane;
+                const bool in = row < w1 && t[i] >= 0 && t[i] < a.vocab && (t[i] & others) == v0;
+                unsigned long long same = __ballot(in);
+                if (!same) continue;
+                const uint32_t d = in ? (uint32_t)(t[i] >> a.shift) : 0;
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                    const bool bit = d >> b & 1;
+                    const unsigned long long set = __ballot(bit);
+                    same &= bit ? set : ~set;
+                }
+                if (in) f(d, same, row);
+                wave_meets();
+            }
+        }
+    };
+    const unsigned long long below = (1ull << lane) - 1;
+    bool some = false;
+    __syncthreads();
+    visit([&](uint32_t d, unsigned long long same, int) __attribute__((always_inline)) {
+        some = true;
+        if (!(same & below)) s.at[wave][d] += __popcll(same);
+    });
+    some = __syncthreads_or(some);
+    if (some) {
+        uint32_t total = 0;
+        if (threadIdx.x < DIGITS)
+            for (int w = 0; w < FEW_WAVES; ++w) total += s.at[w][threadIdx.x];
+        uint32_t upto = total;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t other = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += other;
+        }
+        if (lane == 63 && wave < DIGITS / 64) wave_sum[wave] = upto;
+        __syncthreads();
+        if (threadIdx.x < DIGITS) {
+            uint32_t to = upto - total;
+            for (int w = 0; w < wave; ++w) to += wave_sum[w];
+            begins[threadIdx.x] = to;
+            if (threadIdx.x == DIGITS - 1) begins[DIGITS] = to + total;
+            for (int w = 0; w < FEW_WAVES; ++w) {
+                const uint32_t here = s.at[w][threadIdx.x];
+                s.at[w][threadIdx.x] = to;
+                to += here;
+            }
+        }
+        __syncthreads();
+        visit([&](uint32_t d, unsigned long long same, int row) __attribute__((always_inline)) {
+            const uint32_t first = s.at[wave][d];
+            wave_meets();  // all have read before one of them counts on
+            if (!(same & below)) s.at[wave][d] = first + __popcll(same);
+            order[first + __popcll(same & below)] = (uint16_t)(row - begin);
+        });
+        __syncthreads();
+    }
+
+    // the rows of the table that nothing is added to
+    constexpr int WIDE = 64 * E * (int)sizeof(T);
+    const int64_t from_byte = (int64_t)col_block * WIDE, to_byte = min(from_byte + WIDE, (int64_t)a.dim * (int)sizeof(T));
+    const int pieces = (int)((to_byte - from_byte + 15) / 16), together = FEW_WAVES * 64 / pieces;
+    for (int i = threadIdx.x / pieces; i < n; i += together)
+        if ((int)threadIdx.x < together * pieces && !(some && begins[i + 1] > begins[i]))
+            clear_line(reinterpret_cast<char*>(table + i * table_row), from_byte, to_byte, sizeof(T), threadIdx.x % pieces, pieces);
+    if (!some) return;
+
+    const int own = col_block * 64 * E + lane * E, col = min(own, a.dim - E);
+    // Rows from .. to of a run that begins at `run`: `sum` of the last piece, `sums` of all of them.
+    auto add_up = [&](int run, int from, int to, float (&sum)[E], float (&sums)[E]) __attribute__((always_inline)) {
+        auto some_rows = [&](int at, auto ahead) __attribute__((always_inline)) {
+            constexpr int AHEAD = ahead;
+            Held<T, E> now[AHEAD];
+            const int rows = order[min(at + (lane & (AHEAD - 1)), to - 1)];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                __builtin_memcpy(&now[u].bits, static_cast<const T*>(a.dy) + (int64_t)(begin + __builtin_amdgcn_readlane(rows, u)) * a.dy_row + col, sizeof(T) * E);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int place = at + u;
+                if (place >= to) continue;
+                const bool first = (place - run) % PIECE == 0, last = (place - run) % PIECE == PIECE - 1 || place == to - 1;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float x = now[u].value(e);
+                    sum[e] = first ? x : sum[e] + x;
+                    if (last) sums[e] += sum[e];
+                }
+            }
+        };
+        if (to - from <= 2)
+            some_rows(from, std::integral_constant<int, 2>{});
+        else
+            for (int at = from; at < to; at += FEW_AHEAD) some_rows(at, std::integral_constant<int, FEW_AHEAD>{});
+    };
+    auto give = [&](int i, float (&sum)[E]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = scaled(sum[e], a.scale);
+        if (own < a.dim) store_n(table + i * table_row + col, sum);
+    };
+    // Runs of one piece: a wavefront has every FEW_WAVES-th.  Longer ones afterwards, by all of them, as join_runs_kernel adds them up.
+    int k = 0;
+    unsigned long long longer[DIGITS / 64];
+#pragma unroll
+    for (int i0 = 0; i0 < DIGITS; i0 += 64) {
+        const int many = i0 + lane < n ? (int)(begins[i0 + lane + 1] - begins[i0 + lane]) : 0;
+        longer[i0 / 64] = __ballot(many > PIECE);
+        for (unsigned long long runs = __ballot(many > 0 && many <= PIECE); runs; runs &= runs - 1, ++k) {
+            if (k % FEW_WAVES != wave) continue;
+            const int i = i0 + __builtin_ctzll(runs), run = scalar((int)begins[i]);
+            float sum[E], sums[E] = {};
+            add_up(run, run, scalar((int)begins[i + 1]), sum, sums);
+            give(i, sum);
+        }
+    }
+    __syncthreads();  // (nothing else is left in `at`)
+    k = 0;
+#pragma unroll
+    for (int i0 = 0; i0 < DIGITS; i0 += 64)
+        for (unsigned long long runs = longer[i0 / 64]; runs; runs &= runs - 1, ++k) {
+            const int i = i0 + __builtin_ctzll(runs), run = scalar((int)begins[i]), end_of_run = scalar((int)begins[i + 1]);
+            const int count = (int)up(end_of_run - run, PIECE), each = count <= JOIN_ALONE ? 1 : (int)up(count, FEW_UNITS), units = (int)up(count, each);
+            for (int u = wave; u < units; u += FEW_WAVES) {
+                float sum[E], sums[E] = {};
+                add_up(run, run + u * each * PIECE, min(run + (u + 1) * each * PIECE, end_of_run), sum, sums);
+#pragma unroll
+                for (int e = 0; e < E; ++e) s.meet[u][e][lane] = sums[e];
+            }
+            __syncthreads();
+            if (wave == k % FEW_WAVES) {
+                float sum[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    sum[e] = s.meet[0][e][lane];
+                    for (int u = 1; u < units; ++u) sum[e] += s.meet[u][e][lane];
+                }
+                give(i, sum);
+            }
+            __syncthreads();  // what met is written again
+        }
+}
+
 // ---- entry points --------------------------------------------------------------------------------------------------------
 
 Groups groups_of(const ps_embedding& e) { return Groups{e.offsets_dev, e.table_of_group_dev, e.n_groups, e.n_tables, (int32_t)e.rows}; }
@@ -593,6 +793,7 @@ struct GradientSpace {
 GradientSpace gradient_space(const ps_embedding& e)
 {
     GradientSpace g{};
+    if (e.rows <= FEW_MOST) return g;
     const uint64_t none = (uint64_t)e.n_groups * e.vocab;
     while (none >> (8 * g.passes)) ++g.passes;
     g.chunks = (int)up(e.rows, PIECE);
@@ -752,6 +953,37 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
     if (space.total && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
     if (workspace_bytes < space.total) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    // One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 14.9 19.7, 512 of
+    // 1024 over 50257 27.1 33.2, all of one token 41.8 32.6, 512 of 4096 over 30000 55.6 60.6, 59.1 59.6; fp32 256 of 192 in 64 groups over 4096 39.4
+    // 50.5, all in one group 37.7 50.4.  For 1024 of 1024 over 32000 22.6 30.3, but 53.0 30.6.)
+    if (e->rows && e->rows <= FEW_MOST) {
+        const int size = dtype_size(e->dtype), wide = 16 / size;
+        FewArgs f{};
+        f.dy = dy->data_dev;
+        f.dy_row = dy->row;
+        f.dtable = dtable->data_dev;
+        f.table_row = dtable->row;
+        f.table_matrix = dtable->matrix;
+        f.tokens = tokens->data_dev;
+        f.token_stride = tokens->stride;
+        f.offsets = e->offsets_dev;
+        f.vocab = e->vocab;
+        f.rows = (int32_t)e->rows;
+        f.dim = (int32_t)e->dim;
+        f.col_blocks = (int32_t)up(e->dim, 64 * wide);  // (shorter rows: one, of 64 columns)
+        f.scale = (float)e->scale;
+        // blocks of 64 KB, or fewer where that leaves less than four of them to a compute unit
+        const int64_t most = std::min<int64_t>(DIGITS, FEW_BYTES / std::min<int64_t>(e->dim * size, 1024));
+        const int64_t each = std::max<int64_t>(1, std::min(most, e->n_groups * e->vocab * f.col_blocks / (4 * COMPUTE_UNITS)));
+        while (e->vocab > each << f.shift) ++f.shift;
+        const uint32_t blocks = (uint32_t)((e->n_groups << f.shift) * f.col_blocks);
+        with_types(e->dtype, tokens->bytes, [&](auto t, auto token) {
+            using T = decltype(t);
+            const auto kernel = e->dim < wide ? few_rows_kernel<decltype(token), T, 1> : few_rows_kernel<decltype(token), T, 16 / sizeof(T)>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(FEW_WAVES * 64), (uint32_t)e->rows * 2, s, f);
+        });
+        return tokens_launched(call);
+    }
     char* const base = static_cast<char*>(workspace);
     const uint32_t none = (uint32_t)(e->n_groups * e->vocab);
     const uint32_t* keys = nullptr;

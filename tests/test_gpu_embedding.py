@@ -183,6 +183,55 @@ def test_gradient_in_groups(tk, rows, vocab, dim, groups):
         assert torch.equal(alone, got[k])
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,vocab,dim", [(1, 1, 1), (16, 300, 7), (17, 2, 9), (64, 70000, 513), (255, 3, 1031), (300, 255, 64), (512, 256, 8), (512, 4097, 2049)])
+def test_few_rows_and_many_give_the_same_bits(tk, kind, rows, vocab, dim):
+    """The same rows with others of no token behind them, which take another way."""
+    import torch
+    g = gen(rows + dim)
+    tok = some_tokens(kind, rows, vocab, g)
+    more = torch.cat([tok, torch.full((600,), -1, device="cuda")])
+    for dtype in TYPES:
+        dy = torch.randn(rows + 600, dim, device="cuda", generator=g).to(getattr(torch, dtype))
+        few, many = tk.ps_embedding_backward(dy[:rows], tok, vocab, 0.7), tk.ps_embedding_backward(dy, more, vocab, 0.7)
+        assert torch.equal(few, many)
+        want, off = gradient64(dy[:rows].cpu(), tok.cpu(), vocab, 0.7, owner_of(rows, None), 1)
+        close(few.cpu(), want[0], off[0], f"{kind} {dtype}")
+
+
+@pytest.mark.parametrize("vocab,dim,groups", [(1, 3, 70), (300, 40, 7), (1000, 520, 3), (5000, 4, 1)])
+def test_few_rows_in_groups_and_many_give_the_same_bits(tk, vocab, dim, groups):
+    """With groups without rows and rows before and behind all groups, in tokens and rows that are apart."""
+    import torch
+    g, rows = gen(vocab), 410
+    cuts = sorted(torch.randint(5, rows - 9, (groups + 1,), generator=torch.Generator().manual_seed(groups)).tolist())
+    if groups > 2:
+        cuts[1] = cuts[2]
+    offsets = torch.tensor(cuts, dtype=torch.int32).cuda()
+    tok = some_tokens("zipf", rows + 200, vocab, g)[:, None].repeat(1, 3)[:, 1]
+    dy = torch.randn(rows + 200, dim + 3, device="cuda", generator=g)[:, 1:dim + 1]
+    few, many = tk.ps_grouped_embedding_backward(dy[:rows], tok[:rows], offsets, vocab), tk.ps_grouped_embedding_backward(dy, tok, offsets, vocab)
+    assert torch.equal(few, many)
+    want, off = gradient64(dy[:rows].cpu(), tok[:rows].cpu(), vocab, 1.0, owner_of(rows, cuts), groups)
+    close(few.cpu(), want, off, "gradients")
+
+
+def test_few_rows_in_a_graph(tk):
+    import torch
+    g = gen(6)
+    tok, dy = torch.randint(0, 90, (200,), device="cuda", generator=g), torch.randn(200, 24, device="cuda", generator=g)
+    tk.ps_embedding_backward(dy, tok, 90)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = tk.ps_embedding_backward(dy, tok, 90)
+    for _ in range(3):
+        tok.copy_(torch.randint(-1, 91, (200,), device="cuda", generator=g))
+        dy.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, tk.ps_embedding_backward(dy, tok, 90))
+
+
 def test_keys_of_more_than_24_bits(tk):
     """Workers' tokens whose numbers, with the workers', pass what 32-bit floats hold."""
     import torch

@@ -99,11 +99,12 @@ def test_workspace_of_a_gradient():
         assert lib().ps_embedding_workspace_bytes(ctypes.byref(embedding(**kw)), ctypes.byref(n)) == ps.PS_OK
         return n.value
     assert need(rows=0) == 0
-    # keys and order of 8 rows, twice, and counts in 256 bytes each, two partial rows of 16 floats
-    assert need() == 6 * 256
+    assert need(rows=512) == 0  # one launch
+    # keys and order of 513 rows, twice, counts in two parts, two partial rows of 16 floats for every 16 rows, each to 256 bytes
+    assert need(rows=513) == 4 * 2304 + 2304 + 2 * 33 * 16 * 4 + 128
     assert need(rows=100000) > 4 * 4 * 100000
-    e = embedding()
-    assert gradient(e, size=need() - 1) == ps.PS_ENOMEM
+    e = embedding(rows=600)
+    assert gradient(e, size=need(rows=600) - 1) == ps.PS_ENOMEM
     assert gradient(e, ws=None) == ps.PS_EINVAL and gradient(e, ws=SOMEWHERE + 8) == ps.PS_EINVAL
     assert lib().ps_embedding_workspace_bytes(ctypes.byref(e), None) == ps.PS_EINVAL
     assert lib().ps_embedding_workspace_bytes(None, None) == ps.PS_EINVAL
