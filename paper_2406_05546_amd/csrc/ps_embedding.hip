@@ -421,7 +421,7 @@ struct Held<T, 1> {
 // Wavefronts [chunk][64 * E columns]: the pieces that begin in the chunk's PIECE places; they end within PIECE - 1 places behind.  A lane
 // whose columns would go past the row's end takes the last E of the row, which others have too (E is 1 for rows shorter than 16 bytes).  Bound by
 // memory: SUM_AHEAD rows are asked for while as many are added up, without a branch between them, at which the compiler would wait.
-// 16384 rows of 2048 in bf16 over 50257 tokens 24 us, 3.7 TB/s (28 beside what the clearing left to be written).
+// 16384 rows of 2048 in bf16 over 50257 tokens 24 us, 3.7 TB/s (28 where its rows of the table are not in the caches).
 template <class T, int E>
 __global__ __launch_bounds__(256) void sum_runs_kernel(SumArgs a)
 {
@@ -785,6 +785,28 @@ ps_status check_embedding(const char* call, const ps_embedding* e, bool forward)
     return PS_OK;
 }
 
+// One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 14.9 19.7, 512 of
+// 1024 over 50257 27.1 33.2, all of one token 41.8 32.6, 512 of 4096 over 30000 55.6 60.6, 59.1 59.6; fp32 256 of 192 in 64 groups over 4096 39.4
+// 50.5, all in one group 37.7 50.4.  For 1024 of 1024 over 32000 22.6 30.3, but 53.0 30.6.)
+struct Few {
+    uint32_t blocks;  // 0: not so
+    int shift, col_blocks;
+};
+Few few(const ps_embedding& e)
+{
+    if (!e.rows || e.rows > FEW_MOST) return {};
+    const int64_t size = dtype_size(e.dtype);
+    Few f{};
+    f.col_blocks = (int)up(e.dim, 1024 / size);
+    // blocks of 64 KB, or fewer where that leaves less than four of them to a compute unit
+    const int64_t most = std::min<int64_t>(DIGITS, FEW_BYTES / std::min<int64_t>(e.dim * size, 1024));
+    const int64_t each = std::max<int64_t>(1, std::min(most, e.n_groups * e.vocab * f.col_blocks / (4 * COMPUTE_UNITS)));
+    while (e.vocab > each << f.shift) ++f.shift;
+    const int64_t blocks = (e.n_groups << f.shift) * f.col_blocks;
+    if (blocks < 1 << 22) f.blocks = (uint32_t)blocks;  // (a launch has less than 2^32 threads)
+    return f;
+}
+
 struct GradientSpace {
     uint64_t keys[2], order[2], counts, partial, total;
     int passes, tiles, chunks, parts;
@@ -793,7 +815,7 @@ struct GradientSpace {
 GradientSpace gradient_space(const ps_embedding& e)
 {
     GradientSpace g{};
-    if (e.rows <= FEW_MOST) return g;
+    if (few(e).blocks) return g;
     const uint64_t none = (uint64_t)e.n_groups * e.vocab;
     while (none >> (8 * g.passes)) ++g.passes;
     g.chunks = (int)up(e.rows, PIECE);
@@ -953,11 +975,7 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
     if (space.total && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return dense_fail(PS_EINVAL, "%s: null or misaligned workspace", call);
     if (workspace_bytes < space.total) return dense_fail(PS_ENOMEM, "%s: workspace too small", call);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    // One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 14.9 19.7, 512 of
-    // 1024 over 50257 27.1 33.2, all of one token 41.8 32.6, 512 of 4096 over 30000 55.6 60.6, 59.1 59.6; fp32 256 of 192 in 64 groups over 4096 39.4
-    // 50.5, all in one group 37.7 50.4.  For 1024 of 1024 over 32000 22.6 30.3, but 53.0 30.6.)
-    if (e->rows && e->rows <= FEW_MOST) {
-        const int size = dtype_size(e->dtype), wide = 16 / size;
+    if (const Few one = few(*e); one.blocks) {
         FewArgs f{};
         f.dy = dy->data_dev;
         f.dy_row = dy->row;
@@ -970,17 +988,14 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
         f.vocab = e->vocab;
         f.rows = (int32_t)e->rows;
         f.dim = (int32_t)e->dim;
-        f.col_blocks = (int32_t)up(e->dim, 64 * wide);  // (shorter rows: one, of 64 columns)
+        f.shift = one.shift;
+        f.col_blocks = one.col_blocks;
         f.scale = (float)e->scale;
-        // blocks of 64 KB, or fewer where that leaves less than four of them to a compute unit
-        const int64_t most = std::min<int64_t>(DIGITS, FEW_BYTES / std::min<int64_t>(e->dim * size, 1024));
-        const int64_t each = std::max<int64_t>(1, std::min(most, e->n_groups * e->vocab * f.col_blocks / (4 * COMPUTE_UNITS)));
-        while (e->vocab > each << f.shift) ++f.shift;
-        const uint32_t blocks = (uint32_t)((e->n_groups << f.shift) * f.col_blocks);
         with_types(e->dtype, tokens->bytes, [&](auto t, auto token) {
             using T = decltype(t);
-            const auto kernel = e->dim < wide ? few_rows_kernel<decltype(token), T, 1> : few_rows_kernel<decltype(token), T, 16 / sizeof(T)>;
-            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(FEW_WAVES * 64), (uint32_t)e->rows * 2, s, f);
+            constexpr int E = 16 / sizeof(T);
+            const auto kernel = e->dim < E ? few_rows_kernel<decltype(token), T, 1> : few_rows_kernel<decltype(token), T, E>;
+            hipLaunchKernelGGL(kernel, dim3(one.blocks), dim3(FEW_WAVES * 64), (uint32_t)e->rows * 2, s, f);
         });
         return tokens_launched(call);
     }

@@ -100,6 +100,7 @@ def test_workspace_of_a_gradient():
         return n.value
     assert need(rows=0) == 0
     assert need(rows=512) == 0  # one launch
+    assert need(n_groups=300, offsets_dev=SOMEWHERE, vocab=4194304, dim=1) > 0  # which would have too many threads
     # keys and order of 513 rows, twice, counts in two parts, two partial rows of 16 floats for every 16 rows, each to 256 bytes
     assert need(rows=513) == 4 * 2304 + 2304 + 2 * 33 * 16 * 4 + 128
     assert need(rows=100000) > 4 * 4 * 100000
