@@ -587,16 +587,17 @@ struct FewArgs {
 };
 
 // A block has rows of one group's table, evenly apart so that frequent tokens, which are often the first ones, are many blocks'; of wide rows 64 * E
-// columns.  It looks at all of the group's tokens, puts the rows that have its own in their order (in LDS: counts, then places, equal
-// ones as they were), clears what nothing is added to and adds up the rest.  Sums are formed in the order that the kernels above have:
-// the same bits.  Bound by trips to memory, offsets, tokens, rows, and by the clearing; a token that all rows have, by the one block that adds them up, for
-// which there are eight wavefronts (four: 64 rows 13 us, 16 there; 256 equal ones 41, 32) and registers for six of them to a SIMD.
-constexpr int FEW_WAVES = 8, FEW_MOST = 512, FEW_UNITS = 16, FEW_BYTES = 65536, FEW_AHEAD = 8;
+// columns.  It asks for all of the group's tokens, one to a thread, clears its rows meanwhile (512 rows of 512 in fp32 over 32000 tokens 16 us; 19.5 where only those
+// that nothing is added to are cleared, once that is known), puts the rows that have its own tokens in their order and writes their sums over what it cleared.  Sums are
+// formed in the order that the kernels above have: the same bits.  Bound by the clearing, and by trips to memory, offsets, tokens, rows, that wait for
+// each other; a token that all rows have, by the one block that adds them up, for which there are eight wavefronts (256 equal rows of 1024 in
+// bf16 32 us, with four 41) and registers for six of them to a SIMD.  Blocks of 64 KB: 512 rows of 4096 in bf16 over 30000 tokens 51 us, of 32 KB 54, of 128 KB 51.
+constexpr int FEW_WAVES = 8, FEW_MOST = FEW_WAVES * 64, FEW_UNITS = 16, FEW_BYTES = 65536, FEW_AHEAD = 8;
 
 template <class TOKEN, class T, int E>
 __global__ __launch_bounds__(FEW_WAVES * 64, 6) void few_rows_kernel(FewArgs a)
 {
-    extern __shared__ uint16_t order[];  // rows, counted from the group's first, in the order of their tokens
+    __shared__ uint16_t order[FEW_MOST];  // rows, counted from the group's first, in the order of their tokens
     __shared__ union {
         uint32_t at[FEW_WAVES][DIGITS];
         float meet[FEW_UNITS][E][64];
@@ -610,83 +611,59 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 6) void few_rows_kernel(FewArgs a)
     const int begin = a.offsets ? min(max(a.offsets[g], 0), a.rows) : 0, end = a.offsets ? min(max(a.offsets[g + 1], 0), a.rows) : a.rows;
     T* const table = static_cast<T*>(a.dtable) + g * a.table_matrix + v0 * a.table_row;
     const int64_t table_row = a.table_row << a.shift;
+    const int row = wave * 64 + lane, rows = end - begin;
+    int64_t t = -1;
+    if (rows > 0) t = static_cast<const TOKEN*>(a.tokens)[(int64_t)(begin + min(row, rows - 1)) * a.token_stride];
     for (int i = threadIdx.x; i < FEW_WAVES * DIGITS; i += FEW_WAVES * 64) s.at[0][i] = 0;
 
-    // A wavefront has one stretch of the group's rows, and visits those of the block's tokens 64 rows at a time: with the token's place among the block's,
-    // which lanes have the same, and the row.
-    const int per = (int)up(max(end - begin, 0), FEW_WAVES * 64) * 64, w0 = begin + wave * per, w1 = min(w0 + per, end);
-    auto visit = [&](auto f) __attribute__((always_inline)) {
-        for (int first = w0; first < w1; first += 64 * TILE_EACH) {
-            int64_t t[TILE_EACH];
-#pragma unroll
-            for (int i = 0; i < TILE_EACH; ++i) t[i] = static_cast<const TOKEN*>(a.tokens)[(int64_t)min(first + i * 64 + lane, w1 - 1) * a.token_stride];
-#pragma unroll
-            for (int i = 0; i < TILE_EACH; ++i) {
-                const int row = first + i * 64 + lane;
-                const bool in = row < w1 && t[i] >= 0 && t[i] < a.vocab && (t[i] & others) == v0;
-                unsigned long long same = __ballot(in);
-                if (!same) continue;
-                const uint32_t d = in ? (uint32_t)(t[i] >> a.shift) : 0;
-#pragma unroll
-                for (int b = 0; b < 8; ++b) {
-                    const bool bit = d >> b & 1;
-                    const unsigned long long set = __ballot(bit);
-                    same &= bit ? set : ~set;
-                }
-                if (in) f(d, same, row);
-                wave_meets();
-            }
-        }
-    };
-    const unsigned long long below = (1ull << lane) - 1;
-    bool some = false;
-    __syncthreads();
-    visit([&](uint32_t d, unsigned long long same, int) __attribute__((always_inline)) {
-        some = true;
-        if (!(same & below)) s.at[wave][d] += __popcll(same);
-    });
-    some = __syncthreads_or(some);
-    if (some) {
-        uint32_t total = 0;
-        if (threadIdx.x < DIGITS)
-            for (int w = 0; w < FEW_WAVES; ++w) total += s.at[w][threadIdx.x];
-        uint32_t upto = total;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t other = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += other;
-        }
-        if (lane == 63 && wave < DIGITS / 64) wave_sum[wave] = upto;
-        __syncthreads();
-        if (threadIdx.x < DIGITS) {
-            uint32_t to = upto - total;
-            for (int w = 0; w < wave; ++w) to += wave_sum[w];
-            begins[threadIdx.x] = to;
-            if (threadIdx.x == DIGITS - 1) begins[DIGITS] = to + total;
-            for (int w = 0; w < FEW_WAVES; ++w) {
-                const uint32_t here = s.at[w][threadIdx.x];
-                s.at[w][threadIdx.x] = to;
-                to += here;
-            }
-        }
-        __syncthreads();
-        visit([&](uint32_t d, unsigned long long same, int row) __attribute__((always_inline)) {
-            const uint32_t first = s.at[wave][d];
-            wave_meets();  // all have read before one of them counts on
-            if (!(same & below)) s.at[wave][d] = first + __popcll(same);
-            order[first + __popcll(same & below)] = (uint16_t)(row - begin);
-        });
-        __syncthreads();
-    }
-
-    // the rows of the table that nothing is added to
+    // All of it is cleared: what is added up is written over it, behind a wait.
     constexpr int WIDE = 64 * E * (int)sizeof(T);
     const int64_t from_byte = (int64_t)col_block * WIDE, to_byte = min(from_byte + WIDE, (int64_t)a.dim * (int)sizeof(T));
     const int pieces = (int)((to_byte - from_byte + 15) / 16), together = FEW_WAVES * 64 / pieces;
-    for (int i = threadIdx.x / pieces; i < n; i += together)
-        if ((int)threadIdx.x < together * pieces && !(some && begins[i + 1] > begins[i]))
+    if ((int)threadIdx.x < together * pieces)
+        for (int i = threadIdx.x / pieces; i < n; i += together)
             clear_line(reinterpret_cast<char*>(table + i * table_row), from_byte, to_byte, sizeof(T), threadIdx.x % pieces, pieces);
-    if (!some) return;
+
+    // Rows of this block's tokens, their places among them, and which lanes have the same
+    const bool in = row < rows && t >= 0 && t < a.vocab && (t & others) == v0;
+    if (!__syncthreads_or(in)) return;
+    const uint32_t d = in ? (uint32_t)(t >> a.shift) : 0;
+    unsigned long long same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const bool bit = d >> b & 1;
+        const unsigned long long set = __ballot(bit);
+        same &= bit ? set : ~set;
+    }
+    const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+    if (in && !before) s.at[wave][d] = __popcll(same);
+    __syncthreads();
+    uint32_t total = 0;
+    if (threadIdx.x < DIGITS)
+        for (int w = 0; w < FEW_WAVES; ++w) total += s.at[w][threadIdx.x];
+    uint32_t upto = total;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const uint32_t other = __shfl_up(upto, k, 64);
+        if (lane >= k) upto += other;
+    }
+    if (lane == 63 && wave < DIGITS / 64) wave_sum[wave] = upto;
+    __syncthreads();
+    if (threadIdx.x < DIGITS) {
+        uint32_t to = upto - total;
+        for (int w = 0; w < wave; ++w) to += wave_sum[w];
+        begins[threadIdx.x] = to;
+        if (threadIdx.x == DIGITS - 1) begins[DIGITS] = to + total;
+        for (int w = 0; w < FEW_WAVES; ++w) {
+            const uint32_t here = s.at[w][threadIdx.x];
+            s.at[w][threadIdx.x] = to;
+            to += here;
+        }
+    }
+    __syncthreads();
+    if (in) order[s.at[wave][d] + before] = (uint16_t)row;
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront has cleared
+    __syncthreads();
 
     const int own = col_block * 64 * E + lane * E, col = min(own, a.dim - E);
     // Rows from .. to of a run that begins at `run`: `sum` of the last piece, `sums` of all of them.
@@ -785,9 +762,9 @@ ps_status check_embedding(const char* call, const ps_embedding* e, bool forward)
     return PS_OK;
 }
 
-// One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 14.9 19.7, 512 of
-// 1024 over 50257 27.1 33.2, all of one token 41.8 32.6, 512 of 4096 over 30000 55.6 60.6, 59.1 59.6; fp32 256 of 192 in 64 groups over 4096 39.4
-// 50.5, all in one group 37.7 50.4.  For 1024 of 1024 over 32000 22.6 30.3, but 53.0 30.6.)
+// One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 12.7 19.7, 512 of
+// 1024 over 50257 22.5 33.2, all of one token 40.1 32.6, 512 of 4096 over 30000 51.1 60.6, of one token 58.7 59.6; fp32 256 of 192 in 64 groups over 4096
+// 38.2 50.5, all in one group 37.2 50.4.  1024 rows of one token, of 1024 over 32000, took 53 and 30.6.)
 struct Few {
     uint32_t blocks;  // 0: not so
     int shift, col_blocks;
@@ -995,7 +972,7 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
             using T = decltype(t);
             constexpr int E = 16 / sizeof(T);
             const auto kernel = e->dim < E ? few_rows_kernel<decltype(token), T, 1> : few_rows_kernel<decltype(token), T, E>;
-            hipLaunchKernelGGL(kernel, dim3(one.blocks), dim3(FEW_WAVES * 64), (uint32_t)e->rows * 2, s, f);
+            hipLaunchKernelGGL(kernel, dim3(one.blocks), dim3(FEW_WAVES * 64), 0, s, f);
         });
         return tokens_launched(call);
     }
