@@ -157,6 +157,19 @@ def test_many_rows_and_long_ones(tk, dtype):
         check_forward(tk, z, torch.randint(0, vocab, (rows,), device="cuda", generator=g), 1.0, top)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_of_a_few_rounds(tk, dtype, kind):
+    """A wavefront for each; rows around eight rounds, and of fewer rows by one."""
+    import torch
+    t = getattr(torch, dtype)
+    round_ = 4096 // t.itemsize
+    for rows, vocab, top in ((2048, 8 * round_, 5), (2051, 8 * round_ - 3, 32), (2048, 8 * round_ + 1, 7), (2047, 3 * round_ + 5, 20), (3001, round_ + 1, 1), (2500, 2 * round_ + 9, 0)):
+        g = gen(rows + vocab)
+        z = logits_of(kind, rows, vocab, t, g)
+        check_forward(tk, z, torch.randint(-1, vocab + 1, (rows,), device="cuda", generator=g), 0.8, top)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,vocab", [(5, 2000), (3, 8192), (2, 50000), (300, 20000), (2, 131072)])
 def test_large_values_that_few_lanes_have(tk, dtype, rows, vocab):
