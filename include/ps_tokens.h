@@ -38,7 +38,8 @@ typedef struct {
 
 /* Groups as in ps_linear: group g has rows offsets[g] .. offsets[g+1] - 1 and uses table table_of_group[g] (NULL: g);
  * offsets_dev NULL: one group of all rows.  Their contents are read by the kernels and cannot be refused: offsets are taken
- * into 0 .. rows, of groups that overlap a row is in one, and a table's number is taken to the nearest. */
+ * into 0 .. rows, and a table's number to the nearest.  Where offsets do not ascend, a row is in one of the groups that have it or in
+ * none, the same to every call: among up to 64 groups in the last one that begins at it or before, if that ends behind it. */
 typedef struct {
     int32_t dtype; /* ps_dtype of table, rows and gradients */
     int32_t n_groups, n_tables;

@@ -27,8 +27,8 @@ struct LookupArgs {
     Groups groups;
 };
 
-// A block takes `each` rows (up to 64).  Its first wavefront finds where they come from, one row to a lane; then every thread takes
-// pieces of E columns, LOOKUP_AHEAD of them asked for together.  A row's last piece ends with the row, and so covers columns of the one
+// A block takes `each` rows (up to 64).  Its first two wavefronts find where they come from, one row to a lane, each among the 64 rows from a
+// multiple of 64 on that groups are looked for in; then every thread takes pieces of E columns, LOOKUP_AHEAD of them asked for together.  A row's last piece ends with the row, and so covers columns of the one
 // before again: no piece is partial (E is 1 for rows shorter than 16 bytes).  Bound by memory: 16384 rows of 2048 in bf16 from eight tables for 64
 // groups 22.7 us, 5.9 TB/s.
 constexpr int LOOKUP_AHEAD = 4;
@@ -40,13 +40,14 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a)
     __shared__ int64_t source[64];
     for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
         const int each = (int)min((int64_t)a.each, a.rows - first);
-        if (threadIdx.x < 64) {
-            const int64_t r = min(first + threadIdx.x, (int64_t)a.rows - 1);
-            const int64_t token = static_cast<const TOKEN*>(a.tokens)[r * a.token_stride];
-            const int g = groups_of_rows(a.groups, first);
+        const int64_t look = (first & ~63ll) + scalar(threadIdx.x & ~63);
+        if (threadIdx.x < 128 && look < first + each) {
+            const int64_t r = look + (threadIdx.x & 63);
+            const int64_t token = static_cast<const TOKEN*>(a.tokens)[min(max(r, first), first + each - 1) * a.token_stride];
+            const int g = groups_of_rows(a.groups, look);
             int64_t from = NO_GROUP;
             if (g >= 0) from = token >= 0 && token < a.vocab ? group_matrix(a.groups, g) * a.table_matrix + token * a.table_row : NO_TOKEN;
-            source[threadIdx.x] = from;
+            if (r >= first && r < first + each) source[r - first] = from;
         }
         __syncthreads();
         const int items = each * a.pieces;
@@ -86,7 +87,7 @@ struct SortArgs {
     Groups groups;
 };
 
-// The key of row `first` + lane, for a whole wavefront; `behind` for rows past the last.
+// The key of row `first` (a multiple of 64) + lane, for a whole wavefront; `behind` for rows past the last.
 template <class TOKEN>
 __device__ __forceinline__ uint32_t key_of_row(const SortArgs& a, int64_t first, uint32_t behind)
 {
@@ -580,10 +581,10 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_runs_kernel(SumArgs a)
 struct FewArgs {
     const void *dy, *tokens;
     void* dtable;
-    const int32_t* offsets;
     int64_t dy_row, table_row, table_matrix, token_stride, vocab;
     int32_t rows, dim, shift, col_blocks;  // a block has every (2^shift)-th row of a group's table
     float scale;
+    Groups groups;
 };
 
 // A block has rows of one group's table, evenly apart so that frequent tokens, which are often the first ones, are many blocks'; of wide rows 64 * E
@@ -608,12 +609,17 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 6) void few_rows_kernel(FewArgs a)
     const int64_t others = (1ll << a.shift) - 1, v0 = block & others;
     const int n = (int)((a.vocab - v0 + others) >> a.shift);
     if (n <= 0) return;
-    const int begin = a.offsets ? min(max(a.offsets[g], 0), a.rows) : 0, end = a.offsets ? min(max(a.offsets[g + 1], 0), a.rows) : a.rows;
+    const GroupRows of = group_rows(a.groups, g);
+    const int begin = of.begin, end = of.end;
     T* const table = static_cast<T*>(a.dtable) + g * a.table_matrix + v0 * a.table_row;
     const int64_t table_row = a.table_row << a.shift;
     const int row = wave * 64 + lane, rows = end - begin;
     int64_t t = -1;
     if (rows > 0) t = static_cast<const TOKEN*>(a.tokens)[(int64_t)(begin + min(row, rows - 1)) * a.token_stride];
+    // Whether offsets ascend: every wavefront sees 64 of them.  (One group: something that is there, not in a branch, where the compiler would wait.)
+    const int groups = a.groups.n;
+    const int32_t* const some = groups > 1 ? a.groups.offsets + min(lane, groups - 1) : static_cast<const int32_t*>(a.tokens);
+    const int one = some[0], next = some[groups > 1];
     for (int i = threadIdx.x; i < FEW_WAVES * DIGITS; i += FEW_WAVES * 64) s.at[0][i] = 0;
 
     // All of it is cleared: what is added up is written over it, behind a wait.
@@ -625,8 +631,28 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 6) void few_rows_kernel(FewArgs a)
             clear_line(reinterpret_cast<char*>(table + i * table_row), from_byte, to_byte, sizeof(T), threadIdx.x % pieces, pieces);
 
     // Rows of this block's tokens, their places among them, and which lanes have the same
-    const bool in = row < rows && t >= 0 && t < a.vocab && (t & others) == v0;
+    bool in = row < rows && t >= 0 && t < a.vocab && (t & others) == v0;
     if (!__syncthreads_or(in)) return;
+    bool disorder = __ballot(one > next) != 0;
+    if (groups > 64) {
+        for (int i = 64 + threadIdx.x; i < groups; i += 4 * FEW_WAVES * 64) {
+            int begins[4], ends[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int32_t* const at = a.groups.offsets + min(i + k * FEW_WAVES * 64, groups - 1);
+                begins[k] = at[0], ends[k] = at[1];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) disorder |= begins[k] > ends[k];
+        }
+        disorder = __syncthreads_or(disorder);
+    }
+    if (disorder) {
+        // Of rows of several groups those that groups_of_rows gives to this one.
+        if (wave * 64 < a.rows) order[wave * 64 + lane] = groups_of_rows(a.groups, wave * 64) == g;
+        __syncthreads();
+        in = in && order[begin + row];
+    }
     const uint32_t d = in ? (uint32_t)(t >> a.shift) : 0;
     unsigned long long same = __ballot(in);
 #pragma unroll
@@ -961,7 +987,7 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
         f.table_matrix = dtable->matrix;
         f.tokens = tokens->data_dev;
         f.token_stride = tokens->stride;
-        f.offsets = e->offsets_dev;
+        f.groups = groups_of(*e);
         f.vocab = e->vocab;
         f.rows = (int32_t)e->rows;
         f.dim = (int32_t)e->dim;

@@ -116,7 +116,8 @@ __device__ __forceinline__ int count_tiles(const Groups& gs, int size, int bound
 
 // The group that has row `first` + lane, for a whole wavefront: the last one that begins there or before, if it ends behind it; -1 for
 // rows of none.  One look at the offsets for every power of 64 groups, and one for 64 that begin among the rows: next to kernels that
-// fill the memory's queues, each one takes microseconds.
+// fill the memory's queues, each one takes microseconds.  Where more than 64 offsets do not ascend, the search need not find the last one, and
+// what it finds goes by `first`: a multiple of 64, so that every call has the same.
 __device__ __forceinline__ int groups_of_rows(const Groups& gs, int64_t first)
 {
     const int lane = threadIdx.x & 63;
@@ -125,9 +126,12 @@ __device__ __forceinline__ int groups_of_rows(const Groups& gs, int64_t first)
     auto begins = [&](int g) __attribute__((always_inline)) { return min(max(gs.offsets[g], 0), gs.rows); };
     const int end_of_all = begins(gs.n);
     int lo = 0, hi = gs.n;  // groups before lo begin at `first` or before, those from hi on behind it
+    bool disorder = false;
     while (lo < hi) {
         const int step = (hi - lo + 63) >> 6, g = lo + lane * step;
-        const int before = __popcll(__ballot(g < hi && begins(min(g, gs.n)) <= first));
+        const unsigned long long set = __ballot(g < hi && begins(min(g, gs.n)) <= first);
+        const int before = __popcll(set);
+        disorder |= (set & (set + 1)) != 0;  // not the first lanes'
         if (before == 0) break;
         hi = min(hi, lo + before * step);
         lo = lo + (before - 1) * step + 1;
@@ -143,7 +147,9 @@ __device__ __forceinline__ int groups_of_rows(const Groups& gs, int64_t first)
         }
         if (__builtin_amdgcn_readlane(begin, 63) > first + 63) break;
     }
-    return group >= 0 && r < gs.rows && (group + 1 < gs.n || r < end_of_all) ? group : -1;
+    bool in = group >= 0 && r < gs.rows && (group + 1 < gs.n || r < end_of_all);
+    if (disorder && in) in = begins(group) <= r && r < begins(group + 1);  // (else both were seen)
+    return in ? group : -1;
 }
 
 // The group and the first row of the `tile`-th piece of `size` rows when the groups are cut up one after the other; false
