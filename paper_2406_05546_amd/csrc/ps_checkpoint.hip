@@ -9,13 +9,11 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <class T>
 __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
 {
-    __shared__ int inside[64];  // whether a row is in a group
-    for (int64_t first = (int64_t)blockIdx.x * a.each; first < a.rows; first += (int64_t)gridDim.x * a.each) {
-        const int items = (int)min((int64_t)a.each, a.rows - first) * a.pieces;
-        if (a.groups.offsets) {
-            if (threadIdx.x < 64) inside[threadIdx.x] = groups_of_rows(a.groups, first) >= 0;
-            __syncthreads();
-        }
+    // A group's rows are shared by `parts` blocks, up to 64 at a time, as they come: one group may have those of all.
+    const GroupRows of = group_rows(a.groups, blockIdx.x / a.parts);
+    const int each = min((of.end - of.begin + a.parts - 1) / a.parts, 64);
+    for (int64_t first = of.begin + (int64_t)(blockIdx.x % a.parts) * each; first < of.end; first += (int64_t)a.parts * each) {
+        const int items = (int)min((int64_t)each, of.end - first) * a.pieces;
         for (int at = threadIdx.x; at - (int)threadIdx.x < items; at += 256 * CODE_AHEAD) {
             T raw[CODE_AHEAD][8];
             Piece p[CODE_AHEAD];
@@ -34,11 +32,10 @@ __global__ __launch_bounds__(256) void encode_kernel(CodeArgs a)
                     for (int e = 0; e < 8; ++e) v[e] = to_float(raw[i][e]);
                 }
                 // (all four lanes of a block are there or none is: pieces are whole blocks)
-                const bool there = at + i * 256 < items && (!a.groups.offsets || inside[p[i].row - first]);
+                const bool there = at + i * 256 < items;
                 checkpoint_store<T>(a.codes + p[i].row * a.row, a.scales + p[i].row * a.scale_row, p[i].col, there ? p[i].n : 0, v);
             }
         }
-        if (a.groups.offsets) __syncthreads();  // inside is written again
     }
 }
 
@@ -112,8 +109,10 @@ ps_status check_checkpoint(const char* call, const char* name, const ps_checkpoi
 void launch_checkpoint_encode(int dtype, const Groups& groups, int64_t rows, int64_t cols, const ps_matrix& x, const ps_checkpoint& to, hipStream_t s)
 {
     CodeArgs a = code_args(groups, rows, cols, x, to);
-    const dim3 grid(code_blocks(a));
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(encode_kernel<decltype(t)>, grid, dim3(256), 0, s, a); });
+    const int64_t blocks = code_blocks(a);
+    // Of several groups four blocks to a compute unit at least, of which most may be of groups without rows.
+    a.parts = (int32_t)(groups.n > 1 ? std::min(rows, up(std::max<int64_t>(blocks, 4 * COMPUTE_UNITS), groups.n)) : blocks);
+    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(encode_kernel<decltype(t)>, dim3((uint32_t)(groups.n * a.parts)), dim3(256), 0, s, a); });
 }
 
 CodeArgs decode_args(int64_t rows, int64_t cols, const ps_checkpoint& from, int activation, const ps_matrix& x, int64_t cols_to, uint32_t* blocks)
@@ -139,7 +138,7 @@ extern "C" ps_status ps_checkpoint_encode(int32_t dtype, int64_t rows, int64_t c
     static const char call[] = "ps_checkpoint_encode";
     const ps_status st = check_matrix_of_codes(call, dtype, rows, cols, x, to);
     if (st != PS_OK || !rows) return st;
-    launch_checkpoint_encode(dtype, Groups{}, rows, cols, *x, *to, static_cast<hipStream_t>(hip_stream));
+    launch_checkpoint_encode(dtype, Groups{nullptr, nullptr, 1, 1, (int32_t)rows}, rows, cols, *x, *to, static_cast<hipStream_t>(hip_stream));
     return launched(call);
 }
 
