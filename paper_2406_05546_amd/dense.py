@@ -236,8 +236,9 @@ def _code_call(call: str, dtype: int, x, device, shape, kept, encode: bool, act:
 
 
 def ps_checkpoint_encode(x, out: Optional[Checkpoint] = None) -> Checkpoint:
-    """x [rows, cols] (float32, bfloat16 or float16, contiguous rows) in 8 bits: half a step of 2^-4 of a value off at most, for values from
-    2^-15 of their block's largest on.  What is not 0 is not held as 0; what is not finite is held as NaN."""
+    """x [rows, cols] (float32, bfloat16 or float16, contiguous rows) in 8 bits: a value is off by at most 2^-4 of itself from 2^-13 of its block's
+    largest (and from 2^-132) on, below by less than 2^-16 of that largest (or 2^-135).  What is not 0 is not held as 0; what is not finite is
+    held as NaN."""
     call = "ps_checkpoint_encode"
     dtype = _dtype(call, "x", x)
     device, shape = x.device, x.shape
