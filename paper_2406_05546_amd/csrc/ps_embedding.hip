@@ -1050,7 +1050,7 @@ extern "C" ps_status ps_embedding_backward(const ps_embedding* e, const ps_token
     b.col_blocks = (int32_t)up(e->dim, 64 * 16 / dtype_size(e->dtype));  // (shorter rows: one, of 64 columns)
     b.none = none;
     b.scale = (float)e->scale;
-    const int64_t waves = (int64_t)b.chunks * b.col_blocks;  // (below 2^24: dy fits the memory)
+    const int64_t waves = (int64_t)b.chunks * b.col_blocks;  // below 2^26, as a launch needs: 2^24 chunks at most, and 16 KB of dy for each one more
     with_types(e->dtype, 4, [&](auto t, auto) {
         using T = decltype(t);
         auto sum = [&](auto sum_runs, auto join_runs) {
