@@ -49,15 +49,15 @@ typedef struct {
     double scale; /* finite; taken to 32 bits */
 } ps_embedding;
 
-/* out[r] [dim] = scale * table[token of r] [dim], the product rounded once; a row without a token is 0.  Rows in no group
+/* out[r] [dim] = scale * table[token of r] [dim], the product of 32 bits rounded once; a row without a token is 0.  Rows in no group
  * are left as they are.  table [n_tables][vocab][dim], out [rows][dim], which may not overlap. */
 PS_API ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens* tokens, const ps_matrix* table, const ps_matrix* out,
                                       void* hip_stream);
 
 /* dtable[g][v] = scale * sum of dy[r] over the rows r of group g with token v, [n_groups][vocab][dim], summed in 32 bits, 16
- * rows after each other and these sums after each other (so a group's gradient has the same bits whatever else is in the
- * call), and rounded once; tokens that no row has get 0.  n_tables and table_of_group_dev are not looked at.  dtable
- * may not overlap dy or the tokens. */
+ * rows after each other and these sums after each other, more than eight of them in up to sixteen shares (so a group's gradient has the
+ * same bits whatever else is in the call), times the scale in 32 bits, and rounded once; tokens that no row has get 0.  n_tables and
+ * table_of_group_dev are not looked at.  dtable may not overlap dy or the tokens. */
 PS_API ps_status ps_embedding_workspace_bytes(const ps_embedding* e, uint64_t* bytes_out);
 PS_API ps_status ps_embedding_backward(const ps_embedding* e, const ps_tokens* tokens, const ps_matrix* dy, const ps_matrix* dtable,
                                        void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
@@ -78,7 +78,8 @@ typedef struct {
  *                             among equals; behind the last token with a probability, -infinity and -1.
  * A logit of -infinity has probability 0.  A row of nothing else has -infinity, -infinity and 0 in norm, -infinity as log
  * probability, and no alternatives.  A row with a NaN or +infinity has NaN in what is a number (the largest excepted; NaN is no
- * alternative).  The sums' order goes by the number of rows and by where a row begins in its 16 bytes.  logp, top_logp and top_tokens may be NULL (the last two for top = 0 only), tokens without logp. */
+ * alternative).  z less the row's largest is formed in 32 bits before the scale.  The sums' order goes by the number of rows and by where
+ * a row begins in its 16 bytes.  logp, top_logp and top_tokens may be NULL (the last two for top = 0 only), tokens without logp. */
 PS_API ps_status ps_logprob_workspace_bytes(const ps_logprob* l, uint64_t* bytes_out);
 PS_API ps_status ps_logprob_forward(const ps_logprob* l, const ps_tokens* tokens, const ps_matrix* logits, float* logp_dev, float* norm_dev,
                                     float* top_logp_dev, int32_t* top_tokens_dev, void* workspace_dev, uint64_t workspace_bytes,

@@ -587,12 +587,14 @@ struct FewArgs {
     Groups groups;
 };
 
-// A block has rows of one group's table, evenly apart so that frequent tokens, which are often the first ones, are many blocks'; of wide rows 64 * E
-// columns.  It asks for all of the group's tokens, one to a thread, clears its rows meanwhile (512 rows of 512 in fp32 over 32000 tokens 16 us; 19.5 where only those
-// that nothing is added to are cleared, once that is known), puts the rows that have its own tokens in their order and writes their sums over what it cleared.  Sums are
-// formed in the order that the kernels above have: the same bits.  Bound by the clearing, and by trips to memory, offsets, tokens, rows, that wait for
-// each other; a token that all rows have, by the one block that adds them up, for which there are eight wavefronts (256 equal rows of 1024 in
-// bf16 32 us, with four 41) and registers for six of them to a SIMD.  Blocks of 64 KB: 512 rows of 4096 in bf16 over 30000 tokens 51 us, of 32 KB 54, of 128 KB 51.
+// A block has rows of one group's table, evenly apart so that frequent tokens, which are often the first ones, are many blocks'; of wide
+// rows 64 * E columns.  It asks for all of the group's tokens, one to a thread, clears its rows meanwhile, puts the rows that have its own
+// tokens in their order and writes their sums over what it cleared.  Sums are formed in the order that the kernels above have: the same bits.
+// Bound by the clearing, and by trips to memory, offsets, tokens, rows, that wait for each other; a token that all rows have, by the
+// one block that adds them up, for which there are eight wavefronts and registers for six of them to a SIMD.  us:
+//   all rows cleared, or once it is known those that nothing is added to   fp32 512 rows of 512 over 32000 tokens   16, 19.5
+//   eight wavefronts, or four                                              bf16 256 equal rows of 1024              32, 41
+//   blocks of 64 KB, of 32, of 128                                         bf16 512 rows of 4096 over 30000         51, 54, 51
 constexpr int FEW_WAVES = 8, FEW_MOST = FEW_WAVES * 64, FEW_UNITS = 16, FEW_BYTES = 65536, FEW_AHEAD = 8;
 
 template <class TOKEN, class T, int E>
@@ -788,9 +790,11 @@ ps_status check_embedding(const char* call, const ps_embedding* e, bool forward)
     return PS_OK;
 }
 
-// One launch up to FEW_MOST rows.  (One, and four, us, tokens spread evenly in their logarithm: bf16 64 rows of 512 over 32000 tokens 12.7 19.7, 512 of
-// 1024 over 50257 22.5 33.2, all of one token 40.1 32.6, 512 of 4096 over 30000 51.1 60.6, of one token 58.7 59.6; fp32 256 of 192 in 64 groups over 4096
-// 38.2 50.5, all in one group 37.2 50.4.  1024 rows of one token, of 1024 over 32000, took 53 and 30.6.)
+// One launch up to FEW_MOST rows.  us of one, and of four (tokens spread evenly in their logarithm, or one that all rows have; four results in turn):
+//   bf16   16 rows of 64 over 1000 tokens 5.5, 11.0   64 of 512 over 32000 11.7, 19.5   512 of 1024 over 50257 21.7, 34.4   512 of 4096 over 30000 47.9, 60.6
+//          one token: 256 of 1024 over 32000 23.6, 26.0   512 of 1024 over 50257 36.6, 34.6   512 of 4096 over 30000 55, 60   1024 of 1024 over 32000 53, 31
+//          512 of 64 in 64 groups over 500 12.0, 26.4   500 of 64 in 500 groups over 1000 17.9, 42.6   500 of 16 in 5000 over 300 38, 148
+//   fp32   512 of 512 over 32000 15.9, 29.8   256 of 192 in 64 groups over 4096 37.7, 49.5   all in one of them 37.1, 50.7
 struct Few {
     uint32_t blocks;  // 0: not so
     int shift, col_blocks;
@@ -937,8 +941,8 @@ extern "C" ps_status ps_embedding_forward(const ps_embedding* e, const ps_tokens
     a.dim = (int32_t)e->dim;
     const int wide = 16 / dtype_size(e->dtype);
     a.pieces = (int32_t)(e->dim < wide ? e->dim : up(e->dim, wide));
-    // Rows of 32 KB together, or fewer where that leaves less than four blocks to a compute unit.  (bf16, us: one to a
-    // block for 64 rows of 4096 7.0, 64 34.5; eight for 16384 of 2048 in 64 groups 22.1, one 31.2, 64 26.4; 64 for 65536 of 64 8.4, one 56.8.)
+    // Rows of 32 KB together, or fewer where that leaves less than four blocks to a compute unit.  bf16, us:
+    //   64 rows of 4096 one to a block 7.0, 64 34.5   16384 of 2048 in 64 groups eight 22.1, one 31.2, 64 26.4   65536 of 64 64 8.4, one 56.8
     a.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2048 / a.pieces), e->rows / (4 * COMPUTE_UNITS)));
     a.scale = (float)e->scale;
     a.groups = groups_of(*e);

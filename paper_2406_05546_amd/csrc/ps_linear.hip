@@ -39,11 +39,11 @@ struct SlopeArgs {
 // fourth row each; their sums meet in LDS in order.  Bound by memory, and next to it by the vector ALU (GELU's slope:
 // 30 instructions a value): rows are asked for AHEAD at a time, before those that came are worked on (bf16 8192 x 8192 with GELU
 // 114 -> 88-104 us, 3.9-4.6 TB/s; 8192 x 512 13.8 -> 9.6).
-constexpr int SLOPE_COLS = 512;
-
 //
 // CODES: pre comes in 8 bits, and blocks with a blockIdx.y from `slopes` on decode x, of which the weight gradient is made, where that is in 8
 // bits, too (backward of 16384 rows 512 -> 2048 138 -> 132 us).
+constexpr int SLOPE_COLS = 512;
+
 template <class T, bool CODES>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, CodeArgs x8, uint32_t slopes, uint32_t x8_blocks)
 {
@@ -360,7 +360,10 @@ bool direct_possible(const ps_linear& l, int kind)
 // Where rows are no multiples of 16 bytes, operands come through registers, in 1.5 (fp32) to 4 times the time, or are copied
 // first to rows that are; then the copies come straight to LDS.  Copied if the plans differ by more than copying takes: backward of 7335 rows
 // 949 -> 4658 with GELU in bf16 1076 -> 285 us, in fp32 1370 -> 1035, forward 168 -> 124 and 576 -> 405; of 3414 rows 1665 -> 605 in bf16 121 -> 63.
-// (The kernels for few rows take any alignment.)
+// (The kernels for few rows take any alignment.)  Where x comes in 8 bits it is decoded to such rows anyway, which the estimate does not
+// know: it counts a copy of x, and so leaves some weight gradients to the registers that would be faster straight from LDS (backward without dx,
+// us, through registers as the rule has it, and straight: bf16 GELU 14973 rows 7038 -> 104 265, 174, without activation 228, 145; 64 groups of
+// 125 rows 949 -> 500 without activation 74, 55; GELU 100 rows 1001 -> 999 25.4, 22.3; fp32 14973 rows 1001 -> 104 84, 78).
 struct Padded {
     int64_t in, out;  // features, up to multiples of 16 bytes
     uint64_t x, w, dz;  // bytes of the copies

@@ -151,9 +151,10 @@ struct Range {
 // The best `top` values of a range.  Each lane knows the largest of its own values; the top-th largest of these is a value that at least
 // `top` values reach, and only lanes whose largest reaches it can have one of the best: these lanes' vectors, few, are read again, and
 // what reaches it (but for its lower bits) is listed.  Where more than LIST do (equal values), what is above it is listed, and then the first that
-// equal it (4096 rows of 50257 equal values in bf16 take 4 times as long as random ones); where that is too much as well (an order made for
-// it), the top-th value itself is found bit by bit.  A value's place is the number of
-// listed keys above its own, so the order in which they were listed does not matter.
+// equal it; where that is too much as well (large values that fewer lanes have than there are alternatives), the top-th value itself is
+// found bit by bit, in 32 passes over the row.  4096 rows of 50257 in bf16 with 5 alternatives: 95 us, masks of the lowest value 93, all equal
+// 341, large values in three lanes only 3017.  A value's place is the number of listed keys above its own, so the order in which they were
+// listed does not matter.
 constexpr int LIST = 256;
 template <int WAVES>
 struct Scratch {
@@ -496,7 +497,8 @@ struct BackwardArgs {
 
 // dz = scale (gl ([j is the token] - p) - gh p (log p + H)), so scale p (A + B t) and for the token scale gl more, with t = log2 p, A = -(gl + gh H),
 // B = -gh ln 2.  The scale comes last: with it A may be infinite, and 0 where p is 0 would be NaN, or among the smallest numbers, and lose bits.
-// Bound by memory: bf16 8192 rows of 32768 184 us, 5.8 TB/s.
+// Bound by memory: bf16 8192 rows of 32768 184 us, 5.8 TB/s; of 32767, whose rows begin anywhere, 224, 4.8 TB/s (fp32 372 and 389); 4096 of
+// 50257 146 us, 5.6 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(BackwardArgs a)
 {
@@ -587,9 +589,12 @@ ps_status check_numbers(const char* call, const char* name, const void* p, int64
 // launch (256 rows of 50257 in bf16 with 5 alternatives 20.8 us in parts, 15.4 this way; one of 131072 with 20 17.3 and 17.3, alone 33 and 37).
 bool sixteen(const ps_logprob& l) { return l.rows <= COMPUTE_UNITS && l.vocab <= 65536; }
 
-// Parts of a row, so many rounds of four wavefronts each: as many as make two blocks for a compute unit of all rows, one where there are as
-// many rows.  (Two blocks, and eight, with 5 alternatives, us: bf16 512 rows of 20000 13.0 and 17.6, of 131072 31.3 and 36.7, 128 of 131072 16.7
-// and 20.4, one 16.7 and 15.8; fp32 512 of 50000 21.5 and 30.2.)
+// Parts of a row, so many rounds of four wavefronts each: as many as make two blocks for a compute unit of all rows, one from 257 rows on.  us:
+//   two blocks, and eight, 5 alternatives   bf16 512 rows of 20000 13.0, 17.6   of 131072 31.3, 36.7   128 of 131072 16.7, 20.4   one 16.7, 15.8
+//                                           fp32 512 of 50000 21.5, 30.2
+//   one part, and two, no alternatives      bf16 260 rows of 20000 7.0, 9.5     of 50257 11.8, 14.2    of 131072 25.6, 23.1      fp32 of 50000 14.5, 16.0
+//                                           384 of 20000 7.2, 9.7               of 50257 13.5, 15.2    of 131072 26.9, 24.7      16.0, 19.3
+//                                           511 of 20000 7.5, 11.2              of 50257 14.9, 18.5    of 131072 27.9, 29.9      19.0, 23.4
 struct Cut {
     int parts, rounds;
 };
@@ -607,9 +612,11 @@ template <class T, bool TOP>
 void start_forward(const ForwardArgs& a, hipStream_t s)
 {
     // One wavefront to a row that it takes in one round, and in up to eight where there are rows for two wavefronts to a SIMD: no row waits for
-    // four.  (One, and four, without and with 5 alternatives, us: bf16 2048 rows of 8000 10.3 13.3, 11.0 17.8; 8192 of 4000 17.9 22.7, 26.1 53.5, of
-    // 16000 47.7 61.6, 52.0 73.2; 2048 of 20000 as long; 4096 of 50257 with alternatives 98, 91; fp32 16384 of 4000 42.3 56.5, 44.5 99.9, 8192 of 8000 43.5 59.8, 41.2
-    // 61.8.)
+    // four.  us of one, and of four, without and with 5 alternatives:
+    //   bf16   2048 rows of 8000 10.3, 13.3 and 11.0, 17.8    8192 of 4000 17.9, 22.7 and 26.1, 53.5    8192 of 16000 47.7, 61.6 and 52.0, 73.2
+    //          2048 of 20000 as long                          4096 of 50257 with alternatives 98, 91
+    //   fp32   16384 of 4000 42.3, 56.5 and 44.5, 99.9        8192 of 8000 43.5, 59.8 and 41.2, 61.8
+    // (A row of a few values leaves most lanes without one: 8192 rows of 10 classes in fp32 7.5 us, for the call's 10.)
     constexpr int ROUND = 64 * VECTORS * 16 / (int)sizeof(T);  // of a wavefront
     const int64_t most = 1 << 20;
     if (a.vocab <= ROUND || (a.vocab <= 8 * ROUND && a.rows >= 8 * COMPUTE_UNITS)) {
