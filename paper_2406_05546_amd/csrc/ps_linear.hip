@@ -180,18 +180,19 @@ __global__ __launch_bounds__(BIAS_COLS * BIAS_SHARES) void bias_sum_kernel(const
 }
 
 // Threads for a row, eight columns each; whole blocks of them where it is kept in 8 bits.
-__host__ __device__ inline int join_pieces(int cols, const void* codes) { return codes ? (cols + PS_CHECKPOINT_BLOCK - 1) / PS_CHECKPOINT_BLOCK * CHECKPOINT_LANES : (cols + 7) / 8; }
+__host__ __device__ inline int join_pieces(int cols, bool kept) { return kept ? (cols + PS_CHECKPOINT_BLOCK - 1) / PS_CHECKPOINT_BLOCK * CHECKPOINT_LANES : (cols + 7) / 8; }
 
-// Adds up the parts of a contraction, in order, and finishes the sums.  (There are parts only where there is one group.)
-template <class T>
+// Adds up the parts of a contraction, in order, and finishes the sums.  (There are parts only where there is one group.)  KEPT: pre in 8 bits, a kernel of
+// its own, as the others would wait half a microsecond longer with it.
+template <class T, bool KEPT>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int parts, int rows, int cols, Groups groups, Epilogue epi)
 {
-    const int per_row = join_pieces(cols, epi.codes);
+    const int per_row = join_pieces(cols, KEPT);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
     if (row >= rows) return;
     const int col = (int)(i % per_row) * 8, n = min(8, cols - col);
     float v[8], x[8];
-    for (int k = 0; k < parts && n > 0; ++k) {
+    for (int k = 0; k < parts && (!KEPT || n > 0); ++k) {
         const float* p = partial + ((int64_t)k * rows + row) * cols + col;
         if (n == 8)
             load_n(p, x);
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict
     float bias[8], residual[8];
     load_bias<T>(epi, group_matrix(groups, 0), col, n, bias);
     load_residual<T>(epi, row, col, n, residual);
-    if (epi.codes) keep<T>(epi, bias, row, col, n, v);
+    if constexpr (KEPT) keep<T>(epi, bias, row, col, n, v);
     if (epi.residual)
         finish<T, true>(epi, bias, residual, row, col, n, v);
     else
@@ -535,9 +536,10 @@ void run_product(const ps_linear& l, int kind, bool direct, bool copied, const p
     else
         (kind == FORWARD ? (epi.codes ? launch_linear_forward_kept : launch_linear_forward) : kind == DX ? launch_linear_dx : launch_linear_dw)(p, l.dtype, direct, plan.tile, s);
     if (plan.parts > 1) {
-        const int64_t threads = (int64_t)join_pieces(p.out_cols, epi.codes) * p.out_rows;
+        const int64_t threads = (int64_t)join_pieces(p.out_cols, epi.codes != nullptr) * p.out_rows;
         with_type(l.dtype, [&](auto t) {
-            hipLaunchKernelGGL((join_parts_kernel<decltype(t)>), dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, p.groups, epi);
+            const auto join = epi.codes ? join_parts_kernel<decltype(t), true> : join_parts_kernel<decltype(t), false>;
+            hipLaunchKernelGGL(join, dim3((uint32_t)up(threads, 256)), dim3(256), 0, s, partial, plan.parts, p.out_rows, p.out_cols, p.groups, epi);
         });
     }
 }
