@@ -77,3 +77,57 @@ def test_more_rows_than_blocks(tk):
     assert torch.equal(y[:, 1], tok.clamp(min=0).float() * 2)
     got = tk.ps_embedding_backward(torch.ones(rows, 3, device="cuda"), tok, 5)
     assert torch.equal(got[:, 2].long(), torch.bincount(tok + 1, minlength=6)[1:])  # whole numbers below 2^24
+
+
+def test_calls_at_once_from_threads_on_streams(tk):
+    """Each with its results and workspaces: gradients in one launch, by ranks and sorted, rows cut into parts, layers that keep 8 bits."""
+    import threading
+    import torch
+    from paper_2406_05546_amd import dense
+    g = gen(8)
+    offsets = torch.tensor([0, 90, 30, 200], dtype=torch.int32).cuda()
+    tok = torch.randint(-1, 300, (20000,), device="cuda", generator=g)
+    dy, z = torch.randn(20000, 40, device="cuda", generator=g), torch.randn(3, 90001, device="cuda", generator=g)
+    x, w = torch.randn(70, 96, device="cuda", generator=g).bfloat16(), torch.randn(200, 96, device="cuda", generator=g).bfloat16()
+
+    def step():
+        out = [tk.ps_grouped_embedding_backward(dy[:200], tok[:200], offsets, 300)] + [tk.ps_embedding_backward(dy[:n], tok[:n], 300) for n in (300, 9000, 20000)]
+        p = tk.ps_logprob_forward(z, tok[:3], 1.0, 20)
+        out += [p.logp, p.norm, p.top_logp, p.top_tokens, tk.ps_logprob_backward(z, tok[:3], p.norm, dy[:3, 0], dy[:3, 1])]
+        for rows in (5, 70):
+            pre = dense.ps_checkpoint_empty(rows, 200, "cuda:0")
+            out.append(dense.ps_linear_forward(x[:rows], w, activation="gelu", pre=pre))
+            out += [pre.codes.view(torch.uint8), pre.scales.view(torch.uint8)]
+            out += dense.ps_linear_backward(out[-3], dense.ps_checkpoint_encode(x[:rows]), w, "gelu", pre=pre)
+        return out
+    want, bad = step(), []
+    torch.cuda.synchronize()
+
+    def run(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                if not all(torch.equal(a, b) for a, b in zip(step(), want)):
+                    bad.append(k)
+        stream.synchronize()
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+def test_in_place_in_rows_of_any_place(tk):
+    """The gradient over the logits where rows begin between multiples of 16 bytes, and nothing beside them."""
+    import torch
+    for t in (torch.float32, torch.bfloat16, torch.float16):
+        for vocab, first in ((1, 1), (7, 3), (33, 5), (4097, 1), (20001, 7)):
+            wide = torch.randn(9, vocab + 11, device="cuda", generator=gen(vocab)).to(t)
+            z, before = wide[:, first:first + vocab], wide.clone()
+            tok = torch.arange(9, device="cuda") % vocab
+            p, a = tk.ps_logprob_forward(z, tok, 0.7), torch.randn(9, device="cuda", generator=gen(1))
+            want = tk.ps_logprob_backward(z.contiguous(), tok, p.norm, a, a, 0.7)
+            got = tk.ps_logprob_backward(z, tok, p.norm, a, a, 0.7, out=z)
+            assert got is z and torch.equal(z, want)
+            assert torch.equal(wide[:, :first], before[:, :first]) and torch.equal(wide[:, first + vocab:], before[:, first + vocab:])
